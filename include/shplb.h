@@ -14,6 +14,10 @@
  *   shplb_recovery_curves       recovery ratio per head and budget from that profile (host)
  *   shplb_token_recovery        offline recovery ratio at token granularity, per query
  *   shplb_token_recovery_heads  its mean per head (host)
+ *   shplb_cache_append          the prompt's and later tokens' keys and values into an 8-bit cache
+ *   shplb_cache_load            tokens of the cache back in 16 bits
+ *   shplb_cache_attn            attention of the next tokens over the cache, and the weight every cached token gets
+ *   shplb_cache_evict           a smaller cache of the tokens with the most accumulated weight, budgets per head
  *
  * Conventions
  *   - Every function returns an int32 status: 0 = OK, negative = error (see
@@ -268,6 +272,118 @@ SHPLB_API int32_t shplb_token_recovery(const shplb_problem* p, const void* q, co
  * Errors: SHPLB_E_NULL, SHPLB_E_UNSUPPORTED (n_budgets out of range). */
 SHPLB_API int32_t shplb_token_recovery_heads(const shplb_problem* p, const float* recovery,
                                    int32_t n_budgets, double* heads_out);
+
+/* ---- 8-bit key/value cache --------------------------------------------------- */
+
+/* Behind the prompt: keys and values of a layer in 8 bits, attention of the tokens that
+ * follow over them, and eviction to a budget per head.  (The paper ends with the prompt;
+ * budgets that differ between heads, Section 3.2, here become lengths that do.)
+ *
+ * The cache is a pool of pages.  A page holds `block` tokens of ONE KV head of one
+ * sequence, [block][128] bytes of keys and as many of values, with one scale each: a
+ * code times the page's scale is the value.  page_table[s][h][i] is the page of tokens
+ * i * block .. of head h of sequence s, lens[s][h] how many tokens the head holds.
+ * Both are on the device and are read when a kernel runs: a captured HIP graph of a
+ * step stays right while they change.
+ *   - A scale is the smallest power of two (at least 2^-126) with which the page's
+ *     largest value fits the format, 448 in SHPLB_CACHE_E4M3, 127 in SHPLB_CACHE_INT8
+ *     (two's complement, -128 is not used): a code is one rounding, to nearest, ties to
+ *     even, of its value (near the largest float to the code below, where the next one would stand for 2^128).  A page into which a value comes that is not finite gets the
+ *     scale NaN, and everything read from it is NaN.
+ *   - What lies in a page behind its head's last token is never used, whatever it is, nor
+ *     is a page table entry without tokens.
+ *   - A page number outside 0 .. n_pages-1 where a token needs one: nothing is
+ *     read or written there, what is computed from it is NaN.  A length below 0 or above
+ *     max_pages * block: the head's outputs are NaN, nothing is written into it, read out of
+ *     it or counted for it, and eviction hands it on as length -1.
+ *   - Pages may be shared (a common prefix) by heads that only read them. */
+#define SHPLB_CACHE_E4M3 0
+#define SHPLB_CACHE_INT8 1
+
+typedef struct {
+  int32_t n_seq, n_kv_heads;     /* n_seq * n_kv_heads <= SHPLB_MAX_SEQ_HEADS (n_seq alone is not limited) */
+  int32_t head_dim;              /* 128 */
+  int32_t block;                 /* 64 or 128: tokens of a page */
+  int32_t format;                /* SHPLB_CACHE_E4M3 or SHPLB_CACHE_INT8 */
+  int32_t max_pages;             /* entries of a row of the page table, 1..SHPLB_MAX_BLOCKS */
+  int32_t n_pages;               /* pages of the pool */
+  void* k_pages;                 /* device [n_pages][block][128] bytes, 16-byte aligned */
+  void* v_pages;
+  float* k_scale;                /* device [n_pages] */
+  float* v_scale;
+  const int32_t* page_table;     /* device [n_seq][n_kv_heads][max_pages] */
+  int32_t* lens;                 /* device [n_seq][n_kv_heads] */
+} shplb_cache;
+
+/* The tokens that a call is about, token-major like those of a shplb_problem: rows
+ * cu_tokens[s] .. cu_tokens[s+1]-1 are the LAST tokens of sequence s, positions
+ * lens[s][h]-n .. lens[s][h]-1 of every head: lens count them already, before they are
+ * appended. */
+typedef struct {
+  int32_t n_tokens;              /* rows of the tensors, >= 0; those behind the last sequence are left as they are */
+  int32_t max_tokens;            /* no sequence has more */
+  const int32_t* cu_tokens;      /* device [n_seq+1], not decreasing, or NULL: max_tokens of every sequence
+                                  * (n_tokens = n_seq * max_tokens) */
+  int32_t n_q_heads;             /* attention only: heads of Q, a multiple of n_kv_heads unless kv_head_of is given */
+  int64_t q_stride_t, q_stride_h;   /* element strides of Q and the output (attention) */
+  int64_t kv_stride_t, kv_stride_h; /* ... of K and V (append, load) */
+  float softmax_scale;           /* > 0, or 0 for 1/sqrt(head_dim) */
+  const int32_t* kv_head_of;     /* host [n_q_heads], or NULL, as in shplb_problem */
+} shplb_step;
+
+/* Writes the step's keys and values into their pages.  A page that holds older tokens of
+ * the head keeps its scale unless a new value needs a larger one, with which the older
+ * codes are rounded again.  Rows whose position is negative are not stored.
+ *   k, v: device bf16 [n_tokens, n_kv_heads, 128].  No page of two heads, or twice of one,
+ *   may be written to. */
+SHPLB_API int32_t shplb_cache_append(const shplb_cache* cache, const shplb_step* step, const void* k, const void* v,
+                           void* stream);
+
+/* The mirror image: the step's tokens out of their pages, as bf16 (exact: a code times a power of two; below
+ * bf16's smallest normal value rounded).  Rows whose position is negative are left as they were, so a step with n = the
+ * longest head's tokens reads heads of different lengths, the last token in the last row.
+ *   k_out, v_out: device bf16 [n_tokens, n_kv_heads, 128]. */
+SHPLB_API int32_t shplb_cache_load(const shplb_cache* cache, const shplb_step* step, void* k_out, void* v_out,
+                         void* stream);
+
+/* Attention of the step's queries over the cache (Eq. 1 over the tokens the head holds):
+ * the j-th of a sequence's n queries sees the head's first lens - n + 1 + j tokens, the
+ * last one all of them.  Products of bf16 queries and 8-bit codes are exact, sums,
+ * softmax and its statistics fp32, probabilities are rounded to fp16 before they meet the
+ * values.  A query that sees no token has the output 0 and the denominator's logarithm -inf.
+ *   q: device bf16 [n_tokens, n_q_heads, 128]; out: likewise, strides as Q.
+ *   lse_out: device fp32 [n_q_heads, n_tokens], natural logarithm of the softmax denominators, or NULL.
+ *   weight_in, weight_out: device fp32 [n_seq][n_kv_heads][max_pages * block]:
+ *     weight_out[s][h][t] = weight_in[s][h][t] + the attention weights that all rows of the
+ *     step (all its queries, all heads that read h) give token t, t < lens[s][h]; nothing is
+ *     written behind.  weight_in may be weight_out, or NULL for zeros; both NULL: not computed.
+ *   workspace: device, shplb_cache_attn_workspace_bytes() (of this step or of one with at least as many n_tokens and
+ *     max_tokens of the same heads), 256-byte aligned; needs no clearing; must not be shared with a call in flight on another
+ *     stream.
+ * Any number of queries is taken; the kernel is made for few (a decoding step, a draft of some tokens, a window of the
+ * prompt's last ones): all rows of a KV head read its keys again for every 64 of them. */
+SHPLB_API int32_t shplb_cache_attn_workspace_bytes(const shplb_cache* cache, const shplb_step* step,
+                                         int64_t* bytes_out /*host*/);
+SHPLB_API int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const void* q, void* out,
+                         float* lse_out, const float* weight_in, float* weight_out, void* workspace, void* stream);
+
+/* Evicts every head to its budget: of its tokens stay the first n_sink, the last
+ * n_recent and, of the others, those of the largest weight (equal weights: the lower
+ * position; +0 = -0, NaN above all), in the order of their positions,
+ *     n = min(lens, capacity of `to`, max(keep, n_sink + n_recent))
+ * in all (where that is fewer than n_sink + n_recent: the first ones before the last ones).
+ * They go to the pages of another cache, `to`, whose scales are taken afresh, and whose lens are written.  `to` may be in
+ * the same pool; its pages must be others than those in use here, its page table and lens other arrays.  Its block
+ * may be another, its format not.
+ *   weight: device fp32 [n_seq][n_kv_heads][max_pages * block]; keep: device int32 [n_seq][n_kv_heads].
+ *   weight_out, kept_out: device fp32 and int32 [n_seq][n_kv_heads][to->max_pages * to->block]: weights and former
+ *   positions of the tokens that stay; nothing is written behind them.  workspace:
+ *   device, shplb_cache_evict_workspace_bytes(cache), 256-byte aligned; no clearing.
+ * Errors: SHPLB_E_BUDGET (negative n_sink or n_recent). */
+SHPLB_API int32_t shplb_cache_evict_workspace_bytes(const shplb_cache* cache, int64_t* bytes_out /*host*/);
+SHPLB_API int32_t shplb_cache_evict(const shplb_cache* cache, const float* weight, const int32_t* keep,
+                          int32_t n_sink, int32_t n_recent, const shplb_cache* to, float* weight_out,
+                          int32_t* kept_out, void* workspace, void* stream);
 
 /* ---- host step ------------------------------------------------------------ */
 

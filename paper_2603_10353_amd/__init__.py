@@ -6,14 +6,24 @@ arguments; every step of the path runs in the library's kernels.  There is no CP
 fallback: importing works without the library, calling does not.
 """
 from .binding import (  # noqa: F401
+    SHPLB_CACHE_E4M3,
+    SHPLB_CACHE_INT8,
+    Cache,
     Problem,
     ShplbError,
+    Step,
     WgStats,
     lib_path,
     load_library,
     shplb_balance_heads,
     shplb_block_mass,
     shplb_block_scores,
+    shplb_cache_append,
+    shplb_cache_attn,
+    shplb_cache_attn_workspace_bytes,
+    shplb_cache_evict,
+    shplb_cache_evict_workspace_bytes,
+    shplb_cache_load,
     shplb_max_blocks,
     shplb_num_rows,
     shplb_probe_mfma_rate,

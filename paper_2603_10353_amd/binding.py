@@ -16,6 +16,8 @@ EXPORTS = [
     "shplb_sparse_attn_prefill", "shplb_sparse_attn_prefill_static", "shplb_split_workspace_bytes", "shplb_sparse_attn_prefill_split",
     "shplb_balance_heads", "shplb_shift_budgets", "shplb_block_mass",
     "shplb_recovery_curves", "shplb_token_recovery", "shplb_token_recovery_heads", "shplb_probe_mfma_rate",
+    "shplb_cache_append", "shplb_cache_load", "shplb_cache_attn_workspace_bytes", "shplb_cache_attn",
+    "shplb_cache_evict_workspace_bytes", "shplb_cache_evict",
     "shplb_strerror",
 ]
 
@@ -41,6 +43,42 @@ class _CProblem(C.Structure):
         ("softmax_scale", C.c_float),
         ("kv_head_of", C.POINTER(C.c_int32)),
     ]
+
+
+class _CCache(C.Structure):
+    _fields_ = [
+        ("n_seq", C.c_int32),
+        ("n_kv_heads", C.c_int32),
+        ("head_dim", C.c_int32),
+        ("block", C.c_int32),
+        ("format", C.c_int32),
+        ("max_pages", C.c_int32),
+        ("n_pages", C.c_int32),
+        ("k_pages", C.c_void_p),
+        ("v_pages", C.c_void_p),
+        ("k_scale", C.c_void_p),
+        ("v_scale", C.c_void_p),
+        ("page_table", C.c_void_p),
+        ("lens", C.c_void_p),
+    ]
+
+
+class _CStep(C.Structure):
+    _fields_ = [
+        ("n_tokens", C.c_int32),
+        ("max_tokens", C.c_int32),
+        ("cu_tokens", C.c_void_p),
+        ("n_q_heads", C.c_int32),
+        ("q_stride_t", C.c_int64),
+        ("q_stride_h", C.c_int64),
+        ("kv_stride_t", C.c_int64),
+        ("kv_stride_h", C.c_int64),
+        ("softmax_scale", C.c_float),
+        ("kv_head_of", C.POINTER(C.c_int32)),
+    ]
+
+
+SHPLB_CACHE_E4M3, SHPLB_CACHE_INT8 = 0, 1
 
 
 class WgStats(C.Structure):
@@ -96,6 +134,13 @@ def load_library():
     lib.shplb_token_recovery_heads.argtypes = [pp, C.POINTER(C.c_float), i32, C.POINTER(C.c_double)]
     lib.shplb_shift_budgets.argtypes = [C.POINTER(C.c_double), i32, i32, i64, i32, i32, C.POINTER(i32),
                                         C.POINTER(i64)]
+    cc, cs = C.POINTER(_CCache), C.POINTER(_CStep)
+    lib.shplb_cache_append.argtypes = [cc, cs, vp, vp, vp]
+    lib.shplb_cache_load.argtypes = [cc, cs, vp, vp, vp]
+    lib.shplb_cache_attn_workspace_bytes.argtypes = [cc, cs, C.POINTER(i64)]
+    lib.shplb_cache_attn.argtypes = [cc, cs, vp, vp, vp, vp, vp, vp, vp]
+    lib.shplb_cache_evict_workspace_bytes.argtypes = [cc, C.POINTER(i64)]
+    lib.shplb_cache_evict.argtypes = [cc, vp, vp, i32, i32, cc, vp, vp, vp, vp]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = i32
     lib.shplb_strerror.argtypes = [i32]
@@ -131,6 +176,44 @@ class Problem:
     @property
     def n_q_heads(self) -> int:
         return self.c.n_q_heads
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+class Cache:
+    """Host-side mirror of the C struct shplb_cache (keeps the buffers alive): pools of 8-bit pages, their scales, the
+    page table and the lengths, all on the device (anything with data_ptr(), or an address)."""
+
+    def __init__(self, k_pages, v_pages, k_scale, v_scale, page_table, lens, n_seq: int, n_kv_heads: int, block: int,
+                 max_pages: int, n_pages: int, format: int = SHPLB_CACHE_E4M3, head_dim: int = 128):
+        self.buffers = (k_pages, v_pages, k_scale, v_scale, page_table, lens)
+        self.c = _CCache(n_seq, n_kv_heads, head_dim, block, format, max_pages, n_pages, *(_dev(x) for x in self.buffers))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+class Step:
+    """Host-side mirror of the C struct shplb_step (keeps cu_tokens and kv_head_of alive): the last tokens of every
+    sequence.  cu_tokens: device int32 [n_seq + 1], or None where every sequence has max_tokens."""
+
+    def __init__(self, n_seq: int, n_q_heads: int, n_kv_heads: int, n_tokens: Optional[int] = None, max_tokens: int = 1,
+                 cu_tokens=None, head_dim: int = 128, q_stride_t: Optional[int] = None, q_stride_h: Optional[int] = None,
+                 kv_stride_t: Optional[int] = None, kv_stride_h: Optional[int] = None, softmax_scale: float = 0.0,
+                 kv_head_of: Optional[Sequence[int]] = None):
+        self.cu_tokens = cu_tokens
+        self.kv_head_of = None if kv_head_of is None else np.ascontiguousarray(np.asarray(kv_head_of, dtype=np.int32))
+        if self.kv_head_of is not None and self.kv_head_of.size != n_q_heads:
+            raise ValueError("kv_head_of must hold n_q_heads entries")
+        q_stride_h = head_dim if q_stride_h is None else q_stride_h
+        kv_stride_h = head_dim if kv_stride_h is None else kv_stride_h
+        q_stride_t = n_q_heads * q_stride_h if q_stride_t is None else q_stride_t
+        kv_stride_t = n_kv_heads * kv_stride_h if kv_stride_t is None else kv_stride_t
+        n_tokens = n_seq * max_tokens if n_tokens is None else n_tokens
+        self.c = _CStep(n_tokens, max_tokens, _dev(cu_tokens), n_q_heads, q_stride_t, q_stride_h, kv_stride_t, kv_stride_h,
+                        softmax_scale,
+                        None if self.kv_head_of is None else self.kv_head_of.ctypes.data_as(C.POINTER(C.c_int32)))
 
     def ref(self):
         return C.byref(self.c)
@@ -318,3 +401,38 @@ def shplb_token_recovery_heads(p: Problem, recovery_host) -> np.ndarray:
 def shplb_probe_mfma_rate(random_operands: bool, iters: int, n_workgroups: int, scratch, stream=None) -> None:
     _check(load_library().shplb_probe_mfma_rate(int(bool(random_operands)), int(iters), int(n_workgroups),
                                                 _dev(scratch), _stream(stream)), "shplb_probe_mfma_rate")
+
+
+def shplb_cache_append(cache: Cache, step: Step, k, v, stream=None) -> None:
+    _check(load_library().shplb_cache_append(cache.ref(), step.ref(), _dev(k), _dev(v), _stream(stream)), "shplb_cache_append")
+
+
+def shplb_cache_load(cache: Cache, step: Step, k_out, v_out, stream=None) -> None:
+    _check(load_library().shplb_cache_load(cache.ref(), step.ref(), _dev(k_out), _dev(v_out), _stream(stream)),
+           "shplb_cache_load")
+
+
+def shplb_cache_attn_workspace_bytes(cache: Cache, step: Step) -> int:
+    out = C.c_int64()
+    _check(load_library().shplb_cache_attn_workspace_bytes(cache.ref(), step.ref(), C.byref(out)),
+           "shplb_cache_attn_workspace_bytes")
+    return out.value
+
+
+def shplb_cache_attn(cache: Cache, step: Step, q, out, lse_out=None, weight_in=None, weight_out=None, workspace=None,
+                     stream=None) -> None:
+    _check(load_library().shplb_cache_attn(cache.ref(), step.ref(), _dev(q), _dev(out), _dev(lse_out), _dev(weight_in),
+                                           _dev(weight_out), _dev(workspace), _stream(stream)), "shplb_cache_attn")
+
+
+def shplb_cache_evict_workspace_bytes(cache: Cache) -> int:
+    out = C.c_int64()
+    _check(load_library().shplb_cache_evict_workspace_bytes(cache.ref(), C.byref(out)), "shplb_cache_evict_workspace_bytes")
+    return out.value
+
+
+def shplb_cache_evict(cache: Cache, weight, keep, n_sink: int, n_recent: int, to: Cache, weight_out, kept_out,
+                      workspace=None, stream=None) -> None:
+    _check(load_library().shplb_cache_evict(cache.ref(), _dev(weight), _dev(keep), int(n_sink), int(n_recent), to.ref(),
+                                            _dev(weight_out), _dev(kept_out), _dev(workspace), _stream(stream)),
+           "shplb_cache_evict")

@@ -12,8 +12,10 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 BUILD = os.path.join(PKG_DIR, "_build")
 LIB = os.path.join(PKG_DIR, "libshplb.so")
 SOURCES = ["api.hip", "score_kernels.hip", "select_kernel.hip", "sched_kernels.hip",
-           "attn_pipe_kernel.hip", "profile_kernel.hip", "probe_kernels.hip"]
+           "attn_pipe_kernel.hip", "profile_kernel.hip", "probe_kernels.hip", "cache_api.hip", "cache_pages_kernels.hip",
+           "cache_attn_kernel.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+HONOR_NANS = ("cache_",)            # sources whose kernels compute with NaN where the inputs have it
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-fno-honor-nans",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
@@ -21,7 +23,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD, src.replace(".hip", ".o"))
-    cmd = [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+    more = ["-fhonor-nans"] if src.startswith(HONOR_NANS) else []
+    cmd = [HIPCC, *FLAGS, *more, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
     err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)

@@ -1,0 +1,152 @@
+// Shared by the kernels of the 8-bit key/value cache (gfx950): what the launchers take, and the two formats.
+//
+// A page is `block` tokens x 128 dims of one KV head, a byte a value.  Its scale is the smallest power of two 2^e, e >= -126,
+// with which the largest magnitude of the page fits the format (448 in e4m3, 127 in int8).  A power of two makes value /
+// scale and code * scale exact, so a code is one rounding of its value, the same whoever computes it; it costs e4m3 nothing and
+// int8 at most one bit against a scale of largest / 127.  A value that is not finite has no such scale: its page's becomes NaN, and
+// so does everything read from the page.
+#pragma once
+#include "attn_common.h"
+
+namespace shplb {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+struct CacheArgs {
+  int32_t n_seq, n_kv_heads, max_pages, n_pages;
+  int32_t block_log2;              // 6 or 7
+  int32_t format;
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  const int32_t* table;
+  int32_t* lens;
+};
+
+// The step's tokens: rows of Q, K, V and the output.
+struct StepArgs {
+  int32_t n_tokens, max_tokens;
+  const int32_t* cu;
+  int64_t stride_t, stride_h;
+};
+
+// The query heads of every KV head: groups of equal size, or listed head after head.
+struct HeadGroups {
+  int32_t mapped, group;                              // mapped = 0: KV head h has heads h * group .. + group - 1
+  uint16_t begin[SHPLB_MAX_MAPPED_HEADS + 1];
+  uint8_t head[SHPLB_MAX_MAPPED_HEADS];
+};
+
+struct CacheAttnArgs {
+  CacheArgs c;
+  StepArgs t;                      // strides of Q and the output
+  HeadGroups groups;
+  int32_t n_q_heads;
+  float scale_log2;                // softmax scale * log2(e)
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;                      // or null
+  const float* weight_in;          // or null
+  float* weight_out;               // or null
+  // workspace
+  float *part_o, *part_ml;         // partial results: [2 workgroups][rows][128], [2 workgroups][2][rows]
+  int32_t* pieces;                 // [workgroups][4]: items that begin in a workgroup and end in another one
+  float* stats;                    // [n_tokens][n_q_heads][2]: reference exponent and 1 / denominator, for the weights
+};
+
+constexpr int kCacheMaxWg = 1024;  // workgroups of an attention launch at most (the workspace is sized for them)
+
+int32_t launch_cache_append(const CacheArgs& c, const StepArgs& t, const void* k, const void* v, hipStream_t stream);
+int32_t launch_cache_load(const CacheArgs& c, const StepArgs& t, void* k, void* v, hipStream_t stream);
+int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int32_t* keep, int32_t n_sink, int32_t n_recent,
+                           const CacheArgs& dst, float* weight_out, int32_t* kept, hipStream_t stream);
+// Rows (query token, head of the group) that a workgroup works on together.
+int32_t cache_attn_rows(int64_t most_rows);
+int32_t launch_cache_attn(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
+
+
+// The rows of sequence s in this step.
+__device__ __forceinline__ void step_tokens(const StepArgs& t, int s, int& row0, int& n) {
+  if (t.cu == nullptr) {
+    row0 = s * t.max_tokens;
+    n = t.max_tokens;
+  } else {
+    row0 = min(max(t.cu[s], 0), t.n_tokens);
+    n = min(max(min(t.cu[s + 1], t.n_tokens) - row0, 0), t.max_tokens);
+  }
+}
+
+// Whether a head's length is one that its page table row can hold.
+__device__ __forceinline__ bool good_length(const CacheArgs& c, int len) { return len >= 0 && len <= c.max_pages << c.block_log2; }
+
+constexpr uint32_t kNanBits = 0x7fc00000u;
+
+// Scale for a page whose largest magnitude is the float of these bits (sign clear): its bits.
+template <int FMT>
+__device__ __forceinline__ uint32_t scale_bits(uint32_t amax) {
+  if (amax >= 0x7f800000u) return kNanBits;
+  // amax = 1.m * 2^e: 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6
+  const int below = FMT == SHPLB_CACHE_E4M3 ? 8 : 6;
+  const uint32_t m = FMT == SHPLB_CACHE_E4M3 ? 0x600000u : 0x7e0000u;
+  const int e = int(amax >> 23) - below + ((amax & 0x7fffffu) > m ? 1 : 0);
+  return uint32_t(max(e, 1)) << 23;
+}
+// 1 / scale, exact; of NaN: 0 (codes of such a page are zeros)
+__device__ __forceinline__ float inverse_scale(uint32_t bits) {
+  return __uint_as_float(bits >= 0x7f800000u ? 0u : 0x7f000000u - bits);
+}
+// The larger of two scales; NaN stays.
+__device__ __forceinline__ uint32_t larger_scale(uint32_t a, uint32_t b) {
+  if ((a & 0x7fffffffu) > 0x7f800000u) return kNanBits;
+  return max(int32_t(a), int32_t(b));
+}
+
+// The largest magnitude (divided by the scale) that may be rounded: at the largest scale codes stay at those whose
+// values are finite.  (240 * 2^120 and 63 * 2^122; one step more is 2^128.)
+template <int FMT>
+__device__ __forceinline__ float code_limit(uint32_t scale) {
+  if constexpr (FMT == SHPLB_CACHE_E4M3) return scale >= (247u << 23) ? 240.0f : 448.0f;
+  return scale >= (249u << 23) ? 63.0f : 127.0f;
+}
+
+// Four codes of values that are already divided by the scale, to nearest, ties to even.
+template <int FMT>
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d, float limit) {
+  a = __builtin_amdgcn_fmed3f(a, -limit, limit);
+  b = __builtin_amdgcn_fmed3f(b, -limit, limit);
+  c = __builtin_amdgcn_fmed3f(c, -limit, limit);
+  d = __builtin_amdgcn_fmed3f(d, -limit, limit);
+  if constexpr (FMT == SHPLB_CACHE_E4M3) {
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+  } else {
+    const uint32_t x = int(__builtin_rintf(a)), y = int(__builtin_rintf(b)), z = int(__builtin_rintf(c)), w = int(__builtin_rintf(d));
+    return (x & 0xff) | (y & 0xff) << 8 | (z & 0xff) << 16 | w << 24;
+  }
+}
+// Four codes as numbers.
+template <int FMT>
+__device__ __forceinline__ void from_codes(uint32_t w, float (&x)[4]) {
+  if constexpr (FMT == SHPLB_CACHE_E4M3) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+  } else {
+    x[0] = float(int(w << 24) >> 24); x[1] = float(int(w << 16) >> 24); x[2] = float(int(w << 8) >> 24); x[3] = float(int(w) >> 24);
+  }
+}
+// Two codes, the low or the high half of w, as fp16 (exact in both formats).
+template <int FMT, bool HIGH>
+__device__ __forceinline__ uint32_t half_codes(uint32_t w) {
+  if constexpr (FMT == SHPLB_CACHE_E4M3) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
+  } else {
+    // 0x6400 | u is 1024 + u in fp16: u = code + 128 (w comes with the sign bits turned), less 1152
+    const uint32_t u = __builtin_amdgcn_perm(0x64646464u, w, HIGH ? 0x04030402u : 0x04010400u);
+    const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, u) - bias);
+  }
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t turned(uint32_t w) { return FMT == SHPLB_CACHE_E4M3 ? w : w ^ 0x80808080u; }
+
+}  // namespace shplb

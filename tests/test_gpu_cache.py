@@ -1,0 +1,543 @@
+"""GPU parity of the 8-bit key/value cache through the C ABI against the oracle: codes and scales byte for byte, attention within
+tolerances made of its roundings (cache_harness.check_attn)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_10353_amd as S
+from cache_harness import D, DEV, Device, attn_workspace, bf16, check_attn, filled, state, step_of, strided
+from oracle import cache_oracle as orc
+
+pytestmark = pytest.mark.gpu
+FORMATS = pytest.mark.parametrize("fmt", [orc.E4M3, orc.INT8], ids=["e4m3", "int8"])
+BLOCKS = pytest.mark.parametrize("block", [128, 64])
+
+
+def stream():
+    return torch.cuda.current_stream()
+
+
+# ---- append and load ----------------------------------------------------------------------------------------------------
+
+# tokens held after the call, and how many of them are new
+APPENDS = {
+    "one_of_one": ([1], [1]),
+    "prompts": ([1, 63, 64, 65, 127, 128, 129, 300], [1, 63, 64, 65, 127, 128, 129, 300]),
+    "steps": ([1, 2, 64, 65, 128, 129, 200, 256], [1] * 8),
+    "pieces": ([200, 65, 128, 129, 500, 3, 64, 300], [100, 64, 1, 2, 0, 3, 63, 290]),
+    "none_but_one": ([100, 0, 70], [0, 0, 6]),
+}
+
+
+@FORMATS
+@BLOCKS
+@pytest.mark.parametrize("name", APPENDS)
+def test_append_and_load(name, block, fmt):
+    lens, new = (np.array(x) for x in APPENDS[name])
+    rng = np.random.default_rng([block, fmt, len(name)])
+    hkv, packed = 3, name in ("prompts", "pieces")
+    c = filled(rng, np.repeat((lens - new)[:, None], hkv, 1), block, fmt, max_pages=-(-int(lens.max()) // block) + 1)
+    used = set(c.table[c.table >= 0].tolist())
+    for s in range(lens.size):                           # pages for what comes
+        for h in range(hkv):
+            for i in range(-(-int(lens[s]) // block)):
+                if c.table[s, h, i] < 0:
+                    c.table[s, h, i] = max(used) + 1
+                    used.add(int(c.table[s, h, i]))
+    more = max(used) + 1 - c.n_pages
+    if more > 0:
+        pad = lambda a: np.concatenate([a, rng.integers(0, 256, size=(more, block, D)).astype(np.uint8)])
+        c.k_pages, c.v_pages = pad(c.k_pages), pad(c.v_pages)
+        c.k_scale, c.v_scale = np.concatenate([c.k_scale, np.ones(more)]), np.concatenate([c.v_scale, np.ones(more)])
+    c.lens[:] = lens[:, None]
+    dev = Device(c)
+    ragged = len(set(new.tolist())) > 1
+    size = np.exp(rng.normal(size=(int(new.sum()), 1, 1)) * 2)       # some scales grow by a lot
+    (k, k64), (v, v64) = (bf16(size * rng.standard_normal((int(new.sum()), hkv, D))) for _ in "kv")
+    kd, wide = strided(k, 4 if packed else 0)
+    vd, _ = strided(v, 4 if packed else 0)
+    step, cu = step_of(dev, new, 6, ragged, kv_stride_t=wide.shape[1] * D)
+    S.shplb_cache_append(dev.cache, step, kd, vd, stream())
+    torch.cuda.synchronize()
+    orc.append(c, k64, v64, cu)
+    dev.check_same(c)
+    S.shplb_cache_append(dev.cache, step, kd, vd, stream())          # again: nothing changes
+    dev.check_same(c)
+    # all that is held, the last token of every head in the sequence's last row, three rows behind the last sequence
+    total = int(lens.sum())
+    back = torch.full((total + 3, hkv + 2, D), 5.0, dtype=torch.bfloat16, device=DEV)
+    want = [np.full((total + 3, hkv, D), 5.0) for _ in "kv"]
+    kb, vb = back[:, 1:1 + hkv], torch.full((total + 3, hkv + 2, D), 5.0, dtype=torch.bfloat16, device=DEV)[:, 1:1 + hkv]
+    step, cu = step_of(dev, lens, 6, True, kv_stride_t=(hkv + 2) * D, behind=3)
+    S.shplb_cache_load(dev.cache, step, kb, vb, stream())
+    orc.load(c, *want, cu)
+    np.testing.assert_array_equal(kb.double().cpu().numpy(), want[0])
+    np.testing.assert_array_equal(vb.double().cpu().numpy(), want[1])
+    assert (back[:, 0] == 5).all() and (back[:, -1] == 5).all()
+
+
+@FORMATS
+def test_append_token_after_token(fmt):
+    # forty tokens one by one, now larger, now smaller, through the end of a page
+    rng = np.random.default_rng(fmt)
+    c = state(rng, [[100, 40]], 64, fmt, spare=2)
+    (k0, k64), (v0, v64) = (bf16(rng.standard_normal((100, 2, D))) for _ in "kv")
+    dev = Device(c)
+    step, cu = step_of(dev, [100], 4, False)
+    S.shplb_cache_append(dev.cache, step, k0.to(DEV), v0.to(DEV), stream())
+    orc.append(c, k64, v64, cu)
+    step, cu = step_of(dev, [1], 4, False)
+    for t in range(40):
+        size = [0.1, 1, 3, 2, 30][t % 5] * (1 + t / 10)
+        (k, k64), (v, v64) = (bf16(size * rng.standard_normal((1, 2, D))) for _ in "kv")
+        c.lens += 1
+        dev.lens += 1
+        S.shplb_cache_append(dev.cache, step, k.to(DEV), v.to(DEV), stream())
+        orc.append(c, k64, v64, cu)
+        dev.check_same(c)
+
+
+@FORMATS
+def test_append_of_extreme_values(fmt):
+    # zeros, the smallest and the largest bf16 numbers, values at the border between two scales, and one that is not finite
+    rng = np.random.default_rng(11)
+    border = orc.LARGEST[fmt] * 2.0 ** -5
+    sizes = [0.0, 1e-38, 9.2e-41, 3.3e38, border, border * (1 + 2.0 ** -7), 1.0, 1.0]
+    c = state(rng, [[20]] * len(sizes), 64, fmt)
+    x = rng.uniform(-1, 1, size=(len(sizes), 20, 1, D))
+    x[:, 3, 0, 5] = 1.0
+    x *= np.array(sizes)[:, None, None, None]
+    x[6, 7, 0, 9], x[7, 1, 0, 0] = np.inf, np.nan
+    k, k64 = bf16(x.reshape(-1, 1, D))
+    v, v64 = bf16(-x.reshape(-1, 1, D))
+    dev = Device(c)
+    step, cu = step_of(dev, [20] * len(sizes), 1, False)
+    S.shplb_cache_append(dev.cache, step, k.to(DEV), v.to(DEV), stream())
+    orc.append(c, k64, v64, cu)
+    dev.check_same(c)
+    # finite tokens that follow do not mend the page; one that is not finite takes the others of its page along
+    c.lens += 1
+    dev.lens += 1
+    k, k64 = bf16(np.where(np.arange(len(sizes)) == 4, np.nan, 1.0)[:, None, None] * np.ones((1, 1, D)))
+    step, cu = step_of(dev, [1] * len(sizes), 1, False)
+    S.shplb_cache_append(dev.cache, step, k.to(DEV), k.to(DEV), stream())
+    orc.append(c, k64, k64, cu)
+    dev.check_same(c)
+    out = torch.zeros((len(sizes) * 21, 1, D), dtype=torch.bfloat16, device=DEV)
+    out2 = torch.zeros_like(out)
+    step, cu = step_of(dev, [21] * len(sizes), 1, False)
+    S.shplb_cache_load(dev.cache, step, out, out2, stream())
+    got = out.double().cpu().numpy().reshape(len(sizes), 21, D)
+    assert np.isnan(got[[4, 6, 7]]).all() and np.isfinite(got[[0, 1, 2, 3, 5]]).all()
+
+
+# ---- attention ----------------------------------------------------------------------------------------------------------
+
+ATTNS = {
+    # tokens held per sequence, new ones, query heads, KV heads
+    "one_token": ([1], [1], 4, 1),
+    "short": ([777], [1], 32, 8),
+    "ragged": ([1, 0, 63, 64, 65, 127, 128, 129, 1000, 301], [1] * 10, 8, 2),
+    "mha": ([300, 77], [1, 1], 3, 3),
+    "one_kv_head": ([500], [1], 16, 1),
+    "some_without": ([300, 20, 0, 200], [2, 0, 3, 5], 8, 2),
+    "sees_nothing": ([2, 5, 130], [5, 5, 5], 4, 2),
+    "rows_17": ([400], [17], 2, 2),
+    "rows_32": ([333, 90], [8, 8], 8, 2),
+    "rows_60": ([333, 90], [15, 3], 8, 2),
+    "rows_200": ([333, 90, 700], [50, 1, 37], 8, 2),
+    "prompt": ([260], [260], 4, 2),
+}
+
+
+def run_attn(c, q, cu, dev, step, weight_in=None, packed=0):
+    qd, wide = strided(q, packed)
+    out = torch.full_like(wide, 9.0)
+    lse = torch.full((q.shape[1], step.c.n_tokens), 9.0, device=DEV)
+    ws = attn_workspace(dev, step)
+    w_out = None
+    if weight_in is not None:
+        w_out = torch.full(weight_in.shape, 9.0, device=DEV)
+        weight_in = torch.from_numpy(weight_in).to(DEV)
+    lo = packed // 2
+    S.shplb_cache_attn(dev.cache, step, qd, out[:, lo:lo + q.shape[1]], lse, weight_in, w_out, ws, stream())
+    torch.cuda.synchronize()
+    n = int(cu[-1])
+    assert (out[n:] == 9).all() and (lse[:, n:] == 9).all()          # rows behind the last sequence
+    if packed:
+        assert (out[:, :lo] == 9).all() and (out[:, lo + q.shape[1]:] == 9).all()
+    got = out[:, lo:lo + q.shape[1]].double().cpu().numpy(), lse.double().cpu().numpy()
+    return got + (None if w_out is None else w_out.double().cpu().numpy(),)
+
+
+@FORMATS
+@BLOCKS
+@pytest.mark.parametrize("name", ATTNS)
+def test_attn(name, block, fmt):
+    lens, new, hq, hkv = ATTNS[name]
+    print("case", name, block, fmt, flush=True)
+    rng = np.random.default_rng([block, fmt, len(name)])
+    lens = np.repeat(np.array(lens)[:, None], hkv, 1)
+    if name in ("ragged", "rows_60"):                    # heads of lengths of their own
+        lens = np.maximum(np.minimum(lens, 1), (lens * rng.uniform(0.3, 1, size=lens.shape)).astype(int))
+    c = filled(rng, lens, block, fmt)
+    ragged = len(set(new)) > 1
+    behind = 2 if ragged else 0
+    q, q64 = bf16(2 * rng.standard_normal((sum(new) + behind, hq, D)))
+    dev = Device(c)
+    packed = 6 if name in ("short", "rows_60", "mha") else 0
+    step, cu = step_of(dev, new, hq, ragged, **(dict(behind=behind) if ragged else {}), q_stride_t=(hq + packed) * D)
+    kv_of = [h // (hq // hkv) for h in range(hq)]
+    w = rng.random((*lens.shape, c.capacity)).astype(np.float32)
+    out, lse, w_out = run_attn(c, q, cu, dev, step, w, packed)
+    check_attn(c, out, lse, q64, cu, kv_of, got_weight=w_out, weight_in=w)
+    behind_len = np.arange(c.capacity) >= c.lens[..., None]
+    assert (w_out[behind_len] == 9).all()
+    # without weights and denominators: the same output, bit for bit, also on a second call
+    for _ in range(2):
+        again, _, _ = run_attn(c, q, cu, dev, step, None, packed)
+        np.testing.assert_array_equal(again, out)
+    dev.check_same(c)                                    # it only reads
+
+
+@FORMATS
+def test_attn_long_heads_in_many_pieces(fmt):
+    # two heads of 40000 and 25 tokens, far more pieces than items, and of 64 rows of which some are of another tile
+    rng = np.random.default_rng(5)
+    c = filled(rng, [[40000, 25]], 128, fmt)
+    dev = Device(c)
+    for n in (1, 20):
+        q, q64 = bf16(2 * rng.standard_normal((n, 8, D)))
+        step, cu = step_of(dev, [n], 8, False)
+        w = np.zeros((1, 2, c.capacity), np.float32)
+        out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+        check_attn(c, out, lse, q64, cu, [h // 4 for h in range(8)], got_weight=w_out, weight_in=w)
+
+
+def test_attn_many_short_sequences():
+    # 700 sequences x 6 heads: every workgroup has several items, and finds them behind hundreds of others
+    rng = np.random.default_rng(6)
+    lens = rng.integers(0, 90, size=(700, 6))
+    new = rng.integers(0, 3, size=700)
+    c = filled(rng, lens, 64, orc.E4M3)
+    q, q64 = bf16(rng.standard_normal((int(new.sum()), 12, D)))
+    dev = Device(c)
+    step, cu = step_of(dev, new, 12, True)
+    w = rng.random((700, 6, c.capacity)).astype(np.float32)
+    out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+    check_attn(c, out, lse, q64, cu, [h // 2 for h in range(12)], got_weight=w_out, weight_in=w)
+
+
+def test_attn_mapped_heads_and_scale():
+    rng = np.random.default_rng(7)
+    kv_of = [2, 0, 2, 2, 0, 2]                           # the second KV head has no query head
+    c = filled(rng, [[200, 150, 330], [64, 1, 0]], 64, orc.INT8)
+    q, q64 = bf16(rng.standard_normal((4, 6, D)))
+    dev = Device(c)
+    step, cu = step_of(dev, [2, 2], 6, False, kv_head_of=kv_of, softmax_scale=0.03)
+    w = rng.random((2, 3, c.capacity)).astype(np.float32)
+    out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+    check_attn(c, out, lse, q64, cu, kv_of, scale=float(np.float32(0.03)), got_weight=w_out, weight_in=w)
+
+
+@FORMATS
+def test_attn_of_extreme_sizes(fmt):
+    # queries and keys of very different size: scales far apart, scores near 0 and in the hundreds, values of 1e30 beside 1e-30
+    rng = np.random.default_rng(8)
+    c = state(rng, [[200]] * 4, 64, fmt)
+    sizes = np.array([1e-30, 1e-3, 1.0, 1e3])
+    k, k64 = bf16((sizes[:, None, None, None] * rng.standard_normal((4, 200, 1, D))).reshape(-1, 1, D))
+    per_page = np.exp(rng.uniform(-60, 60, size=(4, 4)))[:, np.arange(200) // 64]
+    v, v64 = bf16((per_page[..., None, None] * rng.standard_normal((4, 200, 1, D))).reshape(-1, 1, D))
+    orc.append(c, k64, v64, np.arange(5) * 200)
+    q, q64 = bf16((np.array([1e25, 1e3, 10.0, 3e-4])[:, None, None] * rng.standard_normal((4, 4, D))))
+    dev = Device(c)
+    step, cu = step_of(dev, [1] * 4, 4, False)
+    out, lse, _ = run_attn(c, q, cu, dev, step)
+    check_attn(c, out, lse, q64, cu, [0] * 4)
+
+
+def test_attn_nothing_to_do():
+    # a step without a token: nothing but the weights, which are copied
+    rng = np.random.default_rng(9)
+    c = filled(rng, [[100, 64], [0, 3]], 64, orc.E4M3)
+    dev = Device(c)
+    step = S.Step(2, 4, 2, 0, 0)
+    w = torch.rand((2, 2, c.capacity), device=DEV)
+    w_out = torch.full_like(w, 9.0)
+    ws = attn_workspace(dev, step)
+    S.shplb_cache_attn(dev.cache, step, None, None, None, w, w_out, ws, stream())
+    here = torch.arange(c.capacity, device=DEV) < dev.lens[..., None]
+    assert torch.equal(w_out, torch.where(here, w, 9.0))
+    # weights in place, from none
+    step = S.Step(2, 4, 2)
+    q = torch.randn((2, 4, D), device=DEV).to(torch.bfloat16)
+    out, first = torch.empty_like(q), torch.zeros_like(w)
+    S.shplb_cache_attn(dev.cache, step, q, out, None, None, first, attn_workspace(dev, step), stream())
+    twice = first.clone()
+    S.shplb_cache_attn(dev.cache, step, q, out, None, twice, twice, attn_workspace(dev, step), stream())
+    assert torch.equal(twice, first + first)
+    np.testing.assert_allclose(first.sum(2).cpu().numpy(), [[2, 2], [0, 2]], rtol=1e-5)
+
+
+# ---- eviction -----------------------------------------------------------------------------------------------------------
+
+
+def evict_case(rng, lens, keep, sink, recent, block, to_block, fmt, to_pages, kind="heavy"):
+    c = filled(rng, lens, block, fmt)
+    lens = c.lens
+    w = np.exp(2 * rng.standard_normal((*lens.shape, c.capacity))).astype(np.float32)
+    if kind == "ties":                                   # few distinct values, zeros of both signs, NaN, infinities, negative ones
+        w = rng.choice(np.array([0.0, -0.0, 1.0, 2.0, np.nan, np.inf, -1.0, -np.inf, 1e-42], np.float32), size=w.shape)
+    if kind == "zeros":
+        w[:] = 0
+    keep = np.broadcast_to(np.asarray(keep, np.int32), lens.shape)
+    to = state(rng, np.full(lens.shape, to_pages * to_block), to_block, fmt, spare=0)
+    dev, dto = Device(c), Device(to)
+    wd, kd = torch.from_numpy(w).to(DEV), torch.from_numpy(keep.copy()).to(DEV)
+    w_out = torch.zeros((*lens.shape, to.capacity), device=DEV)
+    kept = torch.zeros((*lens.shape, to.capacity), dtype=torch.int32, device=DEV)
+    ws = torch.empty(S.shplb_cache_evict_workspace_bytes(dev.cache), dtype=torch.uint8, device=DEV).fill_(0xff)
+    for _ in range(2):                                   # twice: the workspace needs no clearing, results are the same
+        S.shplb_cache_evict(dev.cache, wd, kd, sink, recent, dto.cache, w_out, kept, ws, stream())
+    torch.cuda.synchronize()
+    want_w, want_kept = orc.evict(c, w, keep, sink, recent, to)
+    np.testing.assert_array_equal(kept.cpu().numpy(), want_kept)
+    np.testing.assert_array_equal(w_out.cpu().numpy(), want_w)
+    dto.check_same(to)
+    dev.check_same(c)
+
+
+@FORMATS
+@pytest.mark.parametrize("kind", ["heavy", "ties", "zeros"])
+@pytest.mark.parametrize("blocks", [(128, 128), (64, 128), (128, 64)])
+def test_evict(kind, blocks, fmt):
+    rng = np.random.default_rng([fmt, len(kind), blocks[1]])
+    lens = rng.integers(0, 500, size=(6, 3))
+    lens[0, 0], lens[1, 1], lens[2, 2] = 0, 1, 499
+    keep = rng.integers(0, 300, size=(6, 3))
+    keep[0], keep[3, 0], keep[4, 0] = 1000, 0, -5
+    evict_case(rng, lens, keep, 5, 9, *blocks, fmt, 512 // blocks[1], kind)
+
+
+@pytest.mark.parametrize("sink,recent", [(0, 0), (0, 3), (70, 0), (400, 400), (1, 1), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_evict_sinks_and_recents(sink, recent):
+    # ... where those alone are more than the head holds, and more than there is room for (two pages of 64)
+    rng = np.random.default_rng(3)
+    evict_case(rng, [[300, 40], [128, 129]], [[0, 100], [3, 64]], sink, recent, 64, 64, orc.E4M3, 2)
+
+
+def test_evict_long_head():
+    rng = np.random.default_rng(4)
+    evict_case(rng, [[70001, 2000, 64]], [[9000, 1999, 1]], 128, 128, 128, 128, orc.INT8, 80)
+    evict_case(rng, [[70001, 2000, 64]], [[9000, 1999, 1]], 128, 128, 128, 128, orc.E4M3, 80, "ties")
+
+
+def test_evict_inside_one_pool():
+    rng = np.random.default_rng(14)
+    c = filled(rng, [[200, 130]], 64, orc.E4M3, spare=0, extra_pages=6)
+    to = c.copy()
+    free = sorted(set(range(c.n_pages)) - set(c.table[c.table >= 0].tolist()))
+    to.table = np.array(free[:6], np.int32).reshape(1, 2, 3)
+    to.k_pages, to.v_pages, to.k_scale, to.v_scale = c.k_pages, c.v_pages, c.k_scale, c.v_scale      # one pool
+    to.lens = np.zeros((1, 2), np.int32)
+    dev = Device(c)
+    dto = S.Cache(dev.k_pages, dev.v_pages, dev.k_scale, dev.v_scale, (tt := torch.from_numpy(to.table).to(DEV)),
+                  (tl := torch.zeros((1, 2), dtype=torch.int32, device=DEV)), 1, 2, 64, 3, c.n_pages)
+    w = rng.random((1, 2, c.capacity)).astype(np.float32)
+    w_out = torch.zeros((1, 2, 192), device=DEV)
+    kept = torch.zeros((1, 2, 192), dtype=torch.int32, device=DEV)
+    ws = torch.empty(S.shplb_cache_evict_workspace_bytes(dev.cache), dtype=torch.uint8, device=DEV)
+    S.shplb_cache_evict(dev.cache, torch.from_numpy(w).to(DEV), torch.tensor([[70, 130]], dtype=torch.int32, device=DEV), 1, 2, dto,
+                        w_out, kept, ws, stream())
+    orc.evict(c, w, np.array([[70, 130]]), 1, 2, to)
+    dev.check_same(c)
+    assert tl.tolist() == to.lens.tolist() == [[70, 130]] and tt is not None
+
+
+# ---- what should not happen, and what else a program does ---------------------------------------------------------------
+
+
+def test_damaged_pages_lengths_and_offsets():
+    # pages outside the pool, lengths outside the table, offsets outside the rows: nothing is touched outside, results say NaN
+    rng = np.random.default_rng(21)
+    c = filled(rng, [[200, 200], [200, 200], [90, 90]], 64, orc.E4M3)
+    c.table[0, 0, 1], c.table[0, 1, 0], c.table[1, 0, 3] = -7, c.n_pages, 2 ** 31 - 1
+    c.lens[1, 1], c.lens[2, 0] = c.capacity + 1, -1
+    dev = Device(c)
+    q, q64 = bf16(rng.standard_normal((3, 4, D)))
+    step, cu = step_of(dev, [1] * 3, 4, False)
+    w = rng.random((3, 2, c.capacity)).astype(np.float32)
+    out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+    check_attn(c, out, lse, q64, cu, [0, 0, 1, 1], got_weight=w_out, weight_in=w)
+    assert np.isnan(out[0]).all() and np.isnan(out[1]).all() and np.isnan(out[2, :2]).all() and np.isfinite(out[2, 2:]).all()
+    k, k64 = bf16(rng.standard_normal((3, 2, D)))
+    S.shplb_cache_append(dev.cache, step, k.to(DEV), k.to(DEV), stream())
+    orc.append(c, k64, k64, cu)
+    dev.check_same(c)
+    back = torch.full((300, 2, D), 5.0, dtype=torch.bfloat16, device=DEV)
+    back2, want = back.clone(), [np.full((300, 2, D), 5.0) for _ in "kv"]
+    step, cu = step_of(dev, [100] * 3, 4, False)
+    S.shplb_cache_load(dev.cache, step, back, back2, stream())
+    orc.load(c, *want, cu)
+    np.testing.assert_array_equal(back.double().cpu().numpy(), want[0])
+    to = state(rng, np.full((3, 2), 128), 64, orc.E4M3, spare=0)
+    to.table[2, 1, 0] = -1
+    dto = Device(to)
+    w_out = torch.zeros((3, 2, 128), device=DEV)
+    kept = torch.zeros((3, 2, 128), dtype=torch.int32, device=DEV)
+    ws = torch.empty(S.shplb_cache_evict_workspace_bytes(dev.cache), dtype=torch.uint8, device=DEV)
+    S.shplb_cache_evict(dev.cache, torch.from_numpy(w).to(DEV), torch.full((3, 2), 100, dtype=torch.int32, device=DEV), 1, 1, dto.cache,
+                        w_out, kept, ws, stream())
+    _, want_kept = orc.evict(c, w, np.full((3, 2), 100), 1, 1, to)
+    np.testing.assert_array_equal(kept.cpu().numpy(), want_kept)
+    dto.check_same(to)
+    # rows that cu_tokens leaves outside: below 0, behind the last, backwards
+    bad = torch.tensor([-5, 2, 1, 90], dtype=torch.int32, device=DEV)
+    step = S.Step(3, 4, 2, 3, 2, bad)
+    o = torch.full((3, 4, D), 9.0, dtype=torch.bfloat16, device=DEV)
+    S.shplb_cache_attn(dev.cache, step, q.to(DEV), o, None, None, None, attn_workspace(dev, step), stream())
+    torch.cuda.synchronize()
+
+
+def test_pages_far_into_a_pool():
+    # byte offsets beyond 32 bits: a pool of 4.9 GB of keys and as much of values, of which the last pages are used
+    n_pages = 300000
+    rng = np.random.default_rng(22)
+    c = filled(rng, [[300, 200]], 128, orc.E4M3, extra_pages=0, spare=0)
+    k_pages = torch.empty((n_pages, 128, D), dtype=torch.uint8, device=DEV)
+    v_pages = torch.empty_like(k_pages)
+    k_scale, v_scale = torch.ones(n_pages, device=DEV), torch.ones(n_pages, device=DEV)
+    at = n_pages - c.n_pages
+    small = Device(c)
+    for big, mine in ((k_pages, small.k_pages), (v_pages, small.v_pages), (k_scale, small.k_scale), (v_scale, small.v_scale)):
+        big[at:] = mine
+    table = torch.where(small.table >= 0, small.table + at, small.table).contiguous()
+    cache = S.Cache(k_pages, v_pages, k_scale, v_scale, table, small.lens, 1, 2, 128, small.max_pages, n_pages)
+    q, q64 = bf16(rng.standard_normal((1, 4, D)))
+    step, cu = step_of(small, [1], 4, False)
+    out = torch.empty((1, 4, D), dtype=torch.bfloat16, device=DEV)
+    k, k64 = bf16(rng.standard_normal((1, 2, D)))
+    S.shplb_cache_append(cache, step, k.to(DEV), k.to(DEV), stream())
+    S.shplb_cache_attn(cache, step, q.to(DEV), out, None, None, None, attn_workspace(small, step), stream())
+    orc.append(c, k64, k64, cu)
+    check_attn(c, out.double().cpu().numpy(), None, q64, cu, [0, 0, 1, 1])
+    back, back2 = (torch.zeros((300, 2, D), dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    step, cu = step_of(small, [300], 4, False)
+    S.shplb_cache_load(cache, step, back, back2, stream())
+    want = [np.zeros((300, 2, D)) for _ in "kv"]
+    orc.load(c, *want, cu)
+    np.testing.assert_array_equal(back2.double().cpu().numpy(), want[1])
+
+
+def test_shared_pages_and_another_stream():
+    # three sequences read one prefix; on a stream that is not the current one
+    rng = np.random.default_rng(23)
+    c = filled(rng, [[256 + 10, 256 + 10]] * 3, 128, orc.INT8)
+    c.table[1:, :, :2] = c.table[0, :, :2]
+    q, q64 = bf16(rng.standard_normal((3, 8, D)))
+    dev = Device(c)
+    step, cu = step_of(dev, [1] * 3, 8, False)
+    qd, out, ws = q.to(DEV), torch.empty((3, 8, D), dtype=torch.bfloat16, device=DEV), attn_workspace(dev, step)
+    w = torch.zeros((3, 2, c.capacity), device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(stream())
+    S.shplb_cache_attn(dev.cache, step, qd, out, None, None, w, ws, side)
+    side.synchronize()
+    check_attn(c, out.double().cpu().numpy(), None, q64, cu, [h // 4 for h in range(8)], got_weight=w.double().cpu().numpy(),
+               weight_in=np.zeros(w.shape, np.float32))
+
+
+def test_decoding_step_in_a_hip_graph():
+    # one token of three sequences appended and attended to, captured once and replayed while lengths and inputs change; with eager
+    # calls and other use of the workspace in between
+    rng = np.random.default_rng(24)
+    c = filled(rng, [[60, 60], [130, 90], [1, 2]], 64, orc.E4M3, spare=2)
+    dev = Device(c)
+    hq = 8
+    step, cu = step_of(dev, [1] * 3, hq, False)
+    k, v = (torch.zeros((3, 2, D), dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    q = torch.zeros((3, hq, D), dtype=torch.bfloat16, device=DEV)
+    out, lse, w = torch.zeros_like(q), torch.zeros((hq, 3), device=DEV), torch.zeros((3, 2, c.capacity), device=DEV)
+    ws = attn_workspace(dev, step)
+    side = torch.cuda.Stream()
+    side.wait_stream(stream())
+    graph = torch.cuda.CUDAGraph()
+
+    def both(st):
+        S.shplb_cache_append(dev.cache, step, k, v, st)
+        S.shplb_cache_attn(dev.cache, step, q, out, lse, w, w, ws, st)
+
+    with torch.cuda.stream(side):
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            both(side)
+    torch.cuda.synchronize()
+    w64 = np.zeros(w.shape)
+    for t in range(8):
+        (kt, k64), (vt, v64) = (bf16((1 + t) * rng.standard_normal((3, 2, D))) for _ in "kv")
+        qt, q64 = bf16(rng.standard_normal((3, hq, D)))
+        k.copy_(kt), v.copy_(vt), q.copy_(qt)
+        dev.lens += 1
+        c.lens += 1
+        ws.random_(0, 255)
+        torch.cuda.synchronize()
+        if t == 5:
+            both(stream())
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        orc.append(c, k64, v64, cu)
+        dev.check_same(c)
+        kv_of = [h // 4 for h in range(hq)]
+        check_attn(c, out.double().cpu().numpy(), lse.double().cpu().numpy(), q64, cu, kv_of, got_weight=w.double().cpu().numpy(),
+                   weight_in=w64)
+        w64 = w.double().cpu().numpy()
+
+
+def test_prompt_window_eviction_and_steps():
+    """The operators together: a prompt through the sparse prefill and into the cache, its last 32 queries weigh its tokens, every
+    head is evicted to its own budget, and decoding goes on behind that."""
+    from harness import DevicePass
+    from workloads import make_workload
+    T, hq, hkv, window = 900, 32, 8, 32
+    wl = make_workload(1, seqlens=[T])
+    run = DevicePass(wl).run_all()                       # the prompt's own attention
+    rng = np.random.default_rng(30)
+    c = state(rng, np.full((1, hkv), T), 128, orc.E4M3)
+    dev = Device(c)
+    step, cu = step_of(dev, [T], hq, False)
+    S.shplb_cache_append(dev.cache, step, run.k, run.v, stream())
+    orc.append(c, run.k.double().cpu().numpy(), run.v.double().cpu().numpy(), cu)
+    kv_of = [h // (hq // hkv) for h in range(hq)]
+    step, cu = step_of(dev, [window], hq, False)
+    w = torch.zeros((1, hkv, c.capacity), device=DEV)
+    out = torch.empty((window, hq, D), dtype=torch.bfloat16, device=DEV)
+    S.shplb_cache_attn(dev.cache, step, run.q[T - window:], out, None, None, w, attn_workspace(dev, step), stream())
+    check_attn(c, out.double().cpu().numpy(), None, run.q[T - window:].double().cpu().numpy(), cu, kv_of,
+               got_weight=w.double().cpu().numpy(), weight_in=np.zeros(w.shape, np.float32))
+    keep = rng.integers(100, 600, size=(1, hkv)).astype(np.int32)
+    to = state(rng, np.full((1, hkv), 700), 128, orc.E4M3, spare=0)
+    dto = Device(to)
+    w2 = torch.zeros((1, hkv, to.capacity), device=DEV)
+    kept = torch.zeros((1, hkv, to.capacity), dtype=torch.int32, device=DEV)
+    ws = torch.empty(S.shplb_cache_evict_workspace_bytes(dev.cache), dtype=torch.uint8, device=DEV)
+    S.shplb_cache_evict(dev.cache, w, torch.from_numpy(keep).to(DEV), 16, window, dto.cache, w2, kept, ws, stream())
+    want_w, want_kept = orc.evict(c, w.cpu().numpy(), keep, 16, window, to)
+    np.testing.assert_array_equal(kept.cpu().numpy(), want_kept)
+    np.testing.assert_array_equal(w2.cpu().numpy(), want_w)
+    dto.check_same(to)
+    step, cu = step_of(dto, [1], hq, False)
+    ws = attn_workspace(dto, step)
+    for t in range(3):
+        (k, k64), (v, v64) = (bf16(rng.standard_normal((1, hkv, D))) for _ in "kv")
+        q, q64 = bf16(rng.standard_normal((1, hq, D)))
+        to.lens += 1
+        dto.lens += 1
+        before = w2.cpu().numpy()
+        o = torch.empty((1, hq, D), dtype=torch.bfloat16, device=DEV)
+        S.shplb_cache_append(dto.cache, step, k.to(DEV), v.to(DEV), stream())
+        S.shplb_cache_attn(dto.cache, step, q.to(DEV), o, None, w2, w2, ws, stream())
+        orc.append(to, k64, v64, cu)
+        dto.check_same(to)
+        check_attn(to, o.double().cpu().numpy(), None, q64, cu, kv_of, got_weight=w2.double().cpu().numpy(), weight_in=before)
