@@ -60,23 +60,27 @@ int32_t check_queries(const shplb_cache* c, const shplb_step* t, HeadGroups* g, 
     }
   }
   *most_rows = int64_t(most) * t->max_tokens;
-  // (more query heads than any sequence x head limit elsewhere would allow, or rows that 32 bits do not count)
   if (t->n_q_heads > SHPLB_MAX_SEQ_HEADS || *most_rows > (1 << 24)) return SHPLB_E_UNSUPPORTED;
+  // places in the list of all units of 64 keys are 32-bit numbers
+  const int rows = cache_attn_rows(*most_rows);
+  const int64_t tiles = *most_rows > rows ? (*most_rows + rows - 1) / rows : 1;
+  if (int64_t(c->n_seq) * c->n_kv_heads * (int64_t(c->max_pages) * c->block / 64) * tiles >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
   return SHPLB_OK;
 }
 
 int64_t align256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
 struct AttnLayout {
-  int64_t part_o, part_ml, pieces, stats, total;
+  int64_t part_o, part_ml, begun, stats, total, tiles;
 };
-AttnLayout attn_layout(const shplb_step* t, int64_t most_rows) {
-  const int64_t rows = cache_attn_rows(most_rows), slots = 2 * kCacheMaxWg;
+AttnLayout attn_layout(const shplb_cache* c, const shplb_step* t, int64_t most_rows) {
   AttnLayout w;
+  const int rows = cache_attn_rows(most_rows);
+  w.tiles = most_rows > rows ? (most_rows + rows - 1) / rows : 1;
   int64_t off = 0;
-  w.part_o = off; off += align256(slots * rows * kHeadDim * 4);
-  w.part_ml = off; off += align256(slots * rows * 2 * 4);
-  w.pieces = off; off += align256(kCacheMaxWg * 16);
+  w.part_o = off; off += align256(kCacheSlotRows * kHeadDim * 4);
+  w.part_ml = off; off += align256(kCacheSlotRows * 2 * 4);
+  w.begun = off; off += align256(int64_t(c->n_seq) * c->n_kv_heads * w.tiles * 8);
   w.stats = off; off += align256(int64_t(t->n_tokens) * t->n_q_heads * 8);
   w.total = off;
   return w;
@@ -120,7 +124,7 @@ int32_t shplb_cache_attn_workspace_bytes(const shplb_cache* cache, const shplb_s
   if (int32_t st = check_cache(cache, &c)) return st;
   if (int32_t st = check_queries(cache, step, &g, &most_rows)) return st;
   if (int32_t st = check_step(cache, step, step->n_q_heads, step->q_stride_t, step->q_stride_h, &t)) return st;
-  *bytes_out = attn_layout(step, most_rows).total;
+  *bytes_out = attn_layout(cache, step, most_rows).total;
   return SHPLB_OK;
 }
 
@@ -140,7 +144,8 @@ int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const
     return SHPLB_E_SHAPE;
   const int32_t n_wg = persistent_workgroups();   // two per compute unit
   if (n_wg < 0) return n_wg;
-  const AttnLayout w = attn_layout(step, most_rows);
+  const AttnLayout w = attn_layout(cache, step, most_rows);
+  a.tiles = int32_t(w.tiles);
   char* ws = static_cast<char*>(workspace);
   a.n_q_heads = step->n_q_heads;
   a.scale_log2 = (step->softmax_scale > 0.0f ? step->softmax_scale : 1.0f / std::sqrt(float(kHeadDim))) * 1.4426950408889634f;
@@ -151,7 +156,7 @@ int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const
   a.weight_out = weight_out;
   a.part_o = reinterpret_cast<float*>(ws + w.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
-  a.pieces = reinterpret_cast<int32_t*>(ws + w.pieces);
+  a.begun = reinterpret_cast<int32_t*>(ws + w.begun);
   a.stats = reinterpret_cast<float*>(ws + w.stats);
   return launch_cache_attn(a, int32_t(most_rows), n_wg / 2, static_cast<hipStream_t>(stream));
 }

@@ -43,6 +43,7 @@ struct CacheAttnArgs {
   StepArgs t;                      // strides of Q and the output
   HeadGroups groups;
   int32_t n_q_heads;
+  int32_t tiles;                   // of rows, of a KV head at most
   float scale_log2;                // softmax scale * log2(e)
   const uint16_t* q;
   uint16_t* out;
@@ -50,12 +51,15 @@ struct CacheAttnArgs {
   const float* weight_in;          // or null
   float* weight_out;               // or null
   // workspace
-  float *part_o, *part_ml;         // partial results: [2 workgroups][rows][128], [2 workgroups][2][rows]
-  int32_t* pieces;                 // [workgroups][4]: items that begin in a workgroup and end in another one
+  float *part_o, *part_ml;         // partial results: [2 shares][rows][128], [2 shares][2][rows]
+  int32_t* begun;                  // [sequences x KV heads][tiles][2]: the share that a tile of rows begins in, its pieces (0: it is whole)
   float* stats;                    // [n_tokens][n_q_heads][2]: reference exponent and 1 / denominator, for the weights
 };
 
-constexpr int kCacheMaxWg = 1024;  // workgroups of an attention launch at most (the workspace is sized for them)
+// Shares of an attention launch at most: of launches in 16 rows every wave's own, of others a workgroup's; and rows of partial results.
+constexpr int kCacheMaxWorkers = 4096;
+constexpr int64_t kCacheSlotRows = 2 * kCacheMaxWorkers * 16;
+static_assert(kCacheSlotRows == 2 * (kCacheMaxWorkers / 4) * 64, "as many of 64 rows as of 16");
 
 int32_t launch_cache_append(const CacheArgs& c, const StepArgs& t, const void* k, const void* v, hipStream_t stream);
 int32_t launch_cache_load(const CacheArgs& c, const StepArgs& t, void* k, void* v, hipStream_t stream);
@@ -66,14 +70,22 @@ int32_t cache_attn_rows(int64_t most_rows);
 int32_t launch_cache_attn(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
 
 
-// The rows of sequence s in this step.
+// A load of what no kernel of the launch writes, at an address that is the same in all lanes: by way of the scalar cache, which leaves
+// the vector loads in flight alone.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) T*>(reinterpret_cast<uintptr_t>(p));
+}
+
+// The rows of sequence s in this step (SCALAR: s is the same in all lanes).
+template <bool SCALAR = false>
 __device__ __forceinline__ void step_tokens(const StepArgs& t, int s, int& row0, int& n) {
   if (t.cu == nullptr) {
     row0 = s * t.max_tokens;
     n = t.max_tokens;
   } else {
-    row0 = min(max(t.cu[s], 0), t.n_tokens);
-    n = min(max(min(t.cu[s + 1], t.n_tokens) - row0, 0), t.max_tokens);
+    row0 = min(max(SCALAR ? scalar_load(t.cu + s) : t.cu[s], 0), t.n_tokens);
+    n = min(max(min(SCALAR ? scalar_load(t.cu + s + 1) : t.cu[s + 1], t.n_tokens) - row0, 0), t.max_tokens);
   }
 }
 
