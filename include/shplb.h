@@ -361,7 +361,7 @@ SHPLB_API int32_t shplb_cache_load(const shplb_cache* cache, const shplb_step* s
  *     max_tokens of the same heads), 256-byte aligned; needs no clearing; must not be shared with a call in flight on another
  *     stream.
  * Any number of queries is taken; the kernel is made for few (a decoding step, a draft of some tokens, a window of the
- * prompt's last ones): all rows of a KV head read its keys again for every 64 of them. */
+ * prompt's last ones): all rows of a KV head read its keys again for every 32 of them. */
 SHPLB_API int32_t shplb_cache_attn_workspace_bytes(const shplb_cache* cache, const shplb_step* step,
                                          int64_t* bytes_out /*host*/);
 SHPLB_API int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const void* q, void* out,

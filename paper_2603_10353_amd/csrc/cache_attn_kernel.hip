@@ -5,7 +5,8 @@
 //
 //   y_t = (q . k_t) * scale * log2(e) * a,   m = max y,   l = sum 2^(y_t - m),   out = sum 2^(y_t - m) b v_t / l,   lse = (m + log2 l) ln 2,
 //
-// in one pass over the keys with a running m (rescaling l and the output when it grows).  Bound by reading the codes once: a
+// in one pass over the keys with a running m: a reference exponent, raised to the largest y (and l and the output scaled down) only where a y
+// is more than 8 above it, which after the first keys is hardly ever.  Bound by reading the codes once: a
 // token of a KV head is 256 bytes and, for a group of four heads, 4 KFLOP.  So the matrix instructions are used for what they save in
 // registers and lanes, with most of their rows empty in a plain decoding step.
 //
@@ -19,7 +20,8 @@
 // inside a product is free, as long as V's are taken alike).  Codes come straight from global memory into registers, are turned to fp16
 // there (exact in both formats), V's after a byte transposition of key pairs; nothing goes through LDS.
 // Q is brought to fp16 by a power of two per row, so that its largest magnitude lies in [2^13, 2^14): exact down to 2^-27 of it.
-// Probabilities are rounded to fp16 at 2^15 times their size: eleven bits down to 2^-29 of the largest.  All sums are fp32.
+// Probabilities are rounded to fp16 at 2^7 times their size: eleven bits down to 2^-21 of the reference, steps of 2^-31 of it below.  Values are
+// fp16 numbers, too, scale and all, where the scale lies between 2^-15 and 2^7.  All sums are fp32.
 #include "cache_common.h"
 
 namespace shplb {
@@ -30,7 +32,8 @@ constexpr int kThreads = 256, kWaves = 4, kUnit = 64;
 // the queries, the first keys, the results, all of them waited for.  For a batch of 128 sequences x 8 heads of lengths between 100 and
 // 16000, where a wave has one to five items, 121 us without, 112 with three.
 constexpr int kStart = 3;
-constexpr float kLift = 15.0f;                 // log2 of what probabilities are multiplied by
+constexpr float kLift = 7.0f;                  // log2 of what probabilities are multiplied by, beside their reference ...
+constexpr float kHeadroom = 8.0f;              // ... and how far, in the exponent, they may be above it: 2^15 in fp16
 constexpr int kLdsRow = kHeadDim + 4;          // floats of a row in LDS: rows four banks apart
 
 struct Item {                                  // a place in the list of units
@@ -188,13 +191,12 @@ __device__ __forceinline__ float load_queries(const CacheAttnArgs& a, int row0, 
   return there ? a.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23) : 0.0f;
 }
 
-// Sixteen bytes of a K row: two operands of eight dims.
+// Eight bytes of a K row as operand.
 template <int FMT>
-__device__ __forceinline__ void key_operands(u32x4 w, f16x8& a, f16x8& b) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = turned<FMT>(w[e]);
-  a = __builtin_bit_cast(f16x8, u32x4{half_codes<FMT, false>(w.x), half_codes<FMT, true>(w.x), half_codes<FMT, false>(w.y), half_codes<FMT, true>(w.y)});
-  b = __builtin_bit_cast(f16x8, u32x4{half_codes<FMT, false>(w.z), half_codes<FMT, true>(w.z), half_codes<FMT, false>(w.w), half_codes<FMT, true>(w.w)});
+__device__ __forceinline__ f16x8 key_operand(uint32_t x, uint32_t y) {
+  x = turned<FMT>(x);
+  y = turned<FMT>(y);
+  return __builtin_bit_cast(f16x8, u32x4{half_codes<FMT, false>(x), half_codes<FMT, true>(x), half_codes<FMT, false>(y), half_codes<FMT, true>(y)});
 }
 
 // The page of a unit of a head: its number in the table, not looked at yet.
@@ -232,16 +234,16 @@ __device__ __forceinline__ SlotBuffer unit_buffer(const uint8_t* base, int64_t b
 // (kOnce: the codes are read by no other tile of rows, and stay in no cache: for the batch of 128 above 121 -> 104 us, for one
 // sequence of 131072 tokens 52 -> 46)
 template <bool kOnce>
-__device__ __forceinline__ void load_keys(const CacheAttnArgs& a, const Page& page, bool there, int n16, int g, Keys& x) {
+__device__ __forceinline__ void load_keys(const CacheAttnArgs& a, const Page& page, bool there, int lane_byte, Keys& x) {
   const SlotBuffer k = unit_buffer(a.c.k, page.byte, there);
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      x.code[t][e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k, n16 * kHeadDim + g * 16 + (t & 1) * 16 * kHeadDim + e * 64, (t >> 1) * 32 * kHeadDim, kOnce ? 2 : 0));
+      x.code[t][e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k, lane_byte, t * 16 * kHeadDim + e * 64, kOnce ? 2 : 0));
 }
 template <bool kOnce>
-__device__ __forceinline__ void load_values(const CacheAttnArgs& a, const Page& page, bool there, int n16, int g, Values& x) {
+__device__ __forceinline__ void load_values(const CacheAttnArgs& a, const Page& page, bool there, int lane_byte, Values& x) {
   const SlotBuffer v = unit_buffer(a.c.v, page.byte, there);
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk)
@@ -249,23 +251,36 @@ __device__ __forceinline__ void load_values(const CacheAttnArgs& a, const Page& 
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        x.code[kk][half][i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(v, g * 4 * kHeadDim + n16 * 8 + (half * 16 + i) * kHeadDim, kk * 32 * kHeadDim, kOnce ? 2 : 0));
+        x.code[kk][half][i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(v, lane_byte, (kk * 32 + half * 16 + i) * kHeadDim, kOnce ? 2 : 0));
 }
 
+// Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a workgroup, which
+// take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.  (For 128 rows x 8 heads x
+// 32768 int8 tokens 54 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.  A wave of 64 rows needs half of that but
+// more registers than there are without moving them about, 84 us; tiles side by side in a workgroup, to read the codes from memory
+// once, 53 for 64 rows, 61 for 128.)
 template <int NT, int WAVES, int FMT>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(CacheAttnArgs a, int least) {
-  constexpr int kRows = 16 * NT, kShare = WAVES;                 // waves that work on one share
-  constexpr int kJoined = kShare == 1 ? 1 : kWaves;              // waves whose results meet in LDS
-  __shared__ float lds_o[kJoined][16][kLdsRow];
-  __shared__ float lds_m[kJoined][kRows], lds_l[kJoined][kRows];
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a, int least) {
+  constexpr bool kOwn = WAVES == 1;
+  constexpr int kRows = 16 * NT;
+  static_assert(kOwn || WAVES == kWaves, "one, or all of a workgroup");
+  // queries, as each lane needs them: what it reads it wrote itself, and they cost no registers
+  __shared__ f16x8 lds_q[kOwn ? kWaves : 1][NT][4][64];
+  __shared__ float lds_o[WAVES][16][kLdsRow];
+  __shared__ float lds_m[WAVES][kRows], lds_l[WAVES][kRows];
   __shared__ int lds_i[kWaves + kThreads];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   int at, end;
   Shares shares;
   // neighbouring shares in different workgroups, on different compute units
-  const int worker = kShare == 1 ? int(blockIdx.x) + wave * int(gridDim.x) : int(blockIdx.x);
-  Item it = locate<false, kRows>(a, worker, int(gridDim.x) * (kWaves / kShare), least, lds_i, at, end, shares);
+  const int worker = kOwn ? int(blockIdx.x) + wave * int(gridDim.x) : int(blockIdx.x);
+  Item it = locate<false, kRows>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, lds_i, at, end, shares);
   while (at < end) {
+    // (the lane as a number of which the compiler knows nothing: what follows from it is worked out here and again at the item's end, and
+    // takes no registers in between)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int n16 = lane & 15, g = lane >> 4, k_byte = n16 * kHeadDim + g * 16, v_byte = g * 4 * kHeadDim + n16 * 8;
     const int pair = it.pair, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads;
     int row0, n, tiles, units;
     step_tokens<true>(a.t, s, row0, n);
@@ -278,28 +293,29 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(C
     const bool good = good_length(a.c, len);
     const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
     if (u1 <= u0) break;                                         // the share ends before the item's first unit
-    // the first unit is asked for before the queries, every other one while the one before it is worked on, its place in
-    // the page table one more ahead
-    const int u_first = u0 + (kShare == 1 ? 0 : wave), u_end = good && len > 0 ? u1 : 0;
-    // With 64 rows there are registers for the keys of two units but the values of one, which then come while the scores are worked on.
-    constexpr bool kAhead = NT < 4;
-    Keys k_even, k_odd;
-    Values v_even, v_odd;
+    // Keys are asked for as soon as those of the unit before are operands, values when those are: either come while the other
+    // half of the work is done, and one set of registers is enough.  A place in the page table is read one unit more ahead.
+    const int first_row = it.tile * kRows, u_first = u0 + (kOwn ? 0 : wave), u_end = good && len > 0 ? u1 : 0;
+    Keys kc;
+    Values vc;
     Page here = page_at(a.c, page_number(a.c, pair, min(u_first, u1 - 1)), min(u_first, u1 - 1));
-    int page_next = page_number(a.c, pair, min(u_first + kShare, u1 - 1));
-    load_keys<NT == 1>(a, here, u_first < u_end, n16, g, k_even);
-    if (kAhead) load_values<NT == 1>(a, here, u_first < u_end, n16, g, v_even);
+    int page_next = page_number(a.c, pair, min(u_first + WAVES, u1 - 1));
+    load_keys<kOwn>(a, here, u_first < u_end, k_byte, kc);
+    load_values<kOwn>(a, here, u_first < u_end, v_byte, vc);
     __builtin_amdgcn_sched_barrier(0);
 
-    f16x8 q[NT][4];
     float to_log2[NT], m[NT], l[NT];
     int seen[NT];                                                // keys that the lane's row sees
     f32x4 acc[NT][8];
-    const int seen_first = len - n + 1 + it.tile * kRows / group;     // by the tile's first row: the fewest
+    const int seen_first = len - n + 1 + first_row / group;      // by the tile's first row: the fewest
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int row = it.tile * kRows + nt * 16 + n16;
-      to_log2[nt] = load_queries(a, row0, n, h, group, row, q[nt]);
+      const int row = first_row + nt * 16 + n16;
+      f16x8 q[4];
+      to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
+      // (waves of one share write the same)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds_q[kOwn ? wave : 0][nt][e][lane] = q[e];
       seen[nt] = row < n * group && good ? len - n + 1 + row / group : 0;
       m[nt] = -INFINITY;
       l[nt] = 0.0f;
@@ -307,72 +323,78 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(C
       for (int t = 0; t < 8; ++t) acc[nt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    const auto work = [&](int u, Keys& kc, Values& vc, Keys& k_next, Values& v_next) __attribute__((always_inline)) {
-      const float k_scale = here.bad ? __uint_as_float(kNanBits) : here.k_scale, v_scale_here = here.bad ? k_scale : here.v_scale;
-      const Page ahead = page_at(a.c, page_next, min(u + kShare, u1 - 1));
-      const bool more = u + kShare < u_end;
-      if (!kAhead) load_values<NT == 1>(a, here, true, n16, g, vc);
-      load_keys<NT == 1>(a, ahead, more, n16, g, k_next);
-      if (kAhead) load_values<NT == 1>(a, ahead, more, n16, g, v_next);
-      here = ahead;
-      page_next = page_number(a.c, pair, min(u + 2 * kShare, u1 - 1));
-      __builtin_amdgcn_sched_barrier(0);
+    for (int u = u_first; u < u_end; u += WAVES) {
+      const float k_scale = here.bad ? __uint_as_float(kNanBits) : here.k_scale, v_scale = here.bad ? k_scale : here.v_scale;
+      const bool more = u + WAVES < u_end;
+      const Page ahead = page_at(a.c, page_next, min(u + WAVES, u1 - 1));
+      page_next = page_number(a.c, pair, min(u + 2 * WAVES, u1 - 1));
       const int key0 = u * kUnit;
       f32x4 sc[NT][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        f16x8 k0, k1, k2, k3;
-        key_operands<FMT>(kc.code[t][0], k0, k1);
-        key_operands<FMT>(kc.code[t][1], k2, k3);
+      for (int e = 0; e < 4; ++e) {
+        f16x8 q[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-          x = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[nt][0], x, 0, 0, 0);
-          x = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[nt][1], x, 0, 0, 0);
-          x = __builtin_amdgcn_mfma_f32_16x16x32_f16(k2, q[nt][2], x, 0, 0, 0);
-          sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k3, q[nt][3], x, 0, 0, 0);
+        for (int nt = 0; nt < NT; ++nt) q[nt] = lds_q[kOwn ? wave : 0][nt][e][lane];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const f16x8 k = key_operand<FMT>(kc.code[t][e >> 1][2 * (e & 1)], kc.code[t][e >> 1][2 * (e & 1) + 1]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[nt], e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[nt][t], 0, 0, 0);
         }
-        __builtin_amdgcn_sched_barrier(0);                       // operands of one tile at a time, or the registers do not suffice
+        __builtin_amdgcn_sched_barrier(0);
       }
-      f16x8 p[NT][2];
-      float alpha[NT], v_scale[NT];
+      __builtin_amdgcn_sched_barrier(0);
+      load_keys<kOwn>(a, ahead, more, k_byte, kc);
+      __builtin_amdgcn_sched_barrier(0);
+      // the reference exponent, raised where a score is more than 2^kHeadroom above it
+      float to[NT], top[NT];
+      bool raise = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float c = to_log2[nt] * k_scale;
-        float top = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sc[nt][t][i] *= c;
+        to[nt] = to_log2[nt] * k_scale;
         if (key0 + kUnit > seen_first) {
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (key0 + t * 16 + g * 4 + i >= seen[nt]) sc[nt][t][i] = -INFINITY;
+            for (int i = 0; i < 4; ++i) sc[nt][t][i] = key0 + t * 16 + g * 4 + i < seen[nt] ? sc[nt][t][i] * to[nt] : -INFINITY;
+          to[nt] = 1.0f;
         }
+        top[nt] = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[nt][t][i]);
-        const float m_new = fmaxf(m[nt], quad_max(top));
-        const float ref = m_new == -INFINITY ? 0.0f : m_new;
-        alpha[nt] = __builtin_amdgcn_exp2f(m[nt] - ref);
-        m[nt] = m_new;
-        float sum = 0.0f;
+          for (int i = 0; i < 4; ++i) top[nt] = fmaxf(top[nt], sc[nt][t][i]);
+        top[nt] = quad_max(top[nt] * to[nt]);
+        raise |= top[nt] > m[nt] + kHeadroom;
+      }
+      if (__ballot(raise)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float m_new = top[nt] > m[nt] + kHeadroom ? top[nt] : m[nt];
+          const float alpha = m_new == m[nt] ? 1.0f : __builtin_amdgcn_exp2f(m[nt] - m_new);
+          m[nt] = m_new;
+          l[nt] *= alpha;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) acc[nt][t] *= alpha;
+        }
+      }
+      f16x8 p[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float off = kLift - (m[nt] == -INFINITY ? 0.0f : m[nt]);
         f16x2 two[8];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           float e[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(sc[nt][t][i] - ref + kLift);
-            sum += e[i];
+            e[i] = __builtin_amdgcn_exp2f(sc[nt][t][i] * to[nt] + off);
+            l[nt] += e[i];
           }
           two[2 * t] = f16x2{(_Float16)e[0], (_Float16)e[1]};
           two[2 * t + 1] = f16x2{(_Float16)e[2], (_Float16)e[3]};
         }
-        l[nt] = l[nt] * alpha[nt] + sum;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           u32x4 w;
@@ -380,7 +402,6 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(C
           for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, two[4 * kk + e]);
           p[nt][kk] = __builtin_bit_cast(f16x8, w);
         }
-        v_scale[nt] = key0 < seen[nt] ? v_scale_here : 0.0f;      // a scale of NaN does not reach rows that see none of the page
       }
       if (key0 + kUnit > len) {
         // codes behind the last token may be anything, NaN among them
@@ -392,9 +413,14 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(C
             for (int i = 0; i < 4; ++i)
               if (key0 + kk * 32 + half * 16 + g * 4 + i >= len) vc.code[kk][half][i] = u32x2{0, 0};
       }
-      // V^T: dim 8 n16 + t of key pairs; two bytes of a pair lie side by side after one permutation
+      // V^T: dim 8 n16 + t of key pairs; two bytes of a pair lie side by side after one permutation.  With a scale that leaves
+      // them fp16 numbers the values themselves are multiplied, and the sums go on where they are; else the codes, and the products
+      // are scaled (a scale of NaN does not reach rows that see none of the page).
+      const bool fp16 = fp16_scale<FMT>(v_scale);
+      const float factor = fp16 ? v_scale : 1.0f;
 #pragma unroll
       for (int t2 = 0; t2 < 4; ++t2) {                           // dims 2 t2 and 2 t2 + 1
+        __builtin_amdgcn_sched_barrier(0);
         f16x8 lo[2], hi[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -403,75 +429,88 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(C
           for (int e = 0; e < 4; ++e) {                          // pairs of keys
             const uint32_t x = vc.code[kk][e >> 1][2 * (e & 1)][t2 >> 1], y = vc.code[kk][e >> 1][2 * (e & 1) + 1][t2 >> 1];
             const uint32_t w = turned<FMT>(__builtin_amdgcn_perm(y, x, t2 & 1 ? 0x07030602u : 0x05010400u));
-            wl[e] = half_codes<FMT, false>(w);
-            wh[e] = half_codes<FMT, true>(w);
+            wl[e] = half_codes<FMT, false>(w, factor);
+            wh[e] = half_codes<FMT, true>(w, factor);
           }
           lo[kk] = __builtin_bit_cast(f16x8, wl);
           hi[kk] = __builtin_bit_cast(f16x8, wh);
         }
+        if (fp16) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = {0.0f, 0.0f, 0.0f, 0.0f};
-          x = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[0], p[nt][0], x, 0, 0, 0);
-          x = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[1], p[nt][1], x, 0, 0, 0);
-          y = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[0], p[nt][0], y, 0, 0, 0);
-          y = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[1], p[nt][1], y, 0, 0, 0);
-          acc[nt][2 * t2] = acc[nt][2 * t2] * alpha[nt] + x * v_scale[nt];
-          acc[nt][2 * t2 + 1] = acc[nt][2 * t2 + 1] * alpha[nt] + y * v_scale[nt];
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+              acc[nt][2 * t2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[kk], p[nt][kk], acc[nt][2 * t2], 0, 0, 0);
+              acc[nt][2 * t2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[kk], p[nt][kk], acc[nt][2 * t2 + 1], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+              x = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[kk], p[nt][kk], x, 0, 0, 0);
+              y = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[kk], p[nt][kk], y, 0, 0, 0);
+            }
+            const float scale = key0 < seen[nt] ? v_scale : 0.0f;
+            acc[nt][2 * t2] += x * scale;
+            acc[nt][2 * t2 + 1] += y * scale;
+          }
         }
-        if (t2 & 1) __builtin_amdgcn_sched_barrier(0);
       }
-    };
-    for (int u = u_first; u < u_end; u += 2 * kShare) {
-      work(u, k_even, v_even, k_odd, v_odd);
-      if (u + kShare >= u_end) break;
-      work(u + kShare, k_odd, v_odd, k_even, v_even);
+      __builtin_amdgcn_sched_barrier(0);
+      load_values<kOwn>(a, ahead, more, v_byte, vc);
+      here = ahead;
     }
 
-    // the four waves' results become one; dims 8 (4 g + i) + t of row n16 are the lane's
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int col = tid & 15, quad = (tid & 63) >> 4;
+    // a lane has dims 8 (4 quad + i) + t of rows 16 nt + col
     const bool whole = u0 == 0 && u1 == units;
-    const int slot = 2 * worker + (u0 == 0 ? 1 : 0);
+    const int64_t slot_row = (2 * int64_t(worker) + (u0 == 0 ? 1 : 0)) * kRows;
+    // what a whole row has beside its output; of a length that cannot be all is NaN
+    const auto row_done = [&](int j, int head, float top, float sum, float inv) {
+      if (a.lse != nullptr)
+        a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = good ? (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f : inv;
+      if (a.weight_out != nullptr)
+        *reinterpret_cast<f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head)) = f32x2{(top == -INFINITY ? 0.0f : top) - kLift, inv};
+    };
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) l[nt] = quad_sum(l[nt]);
-    if constexpr (kShare == 1) {
-      // one wave's own: a lane has 32 dims of a row
-      const int row = it.tile * kRows + n16;
-      if (row < n * group) {
-        const float sum = l[0], ref = m[0] == -INFINITY ? 0.0f : m[0];
+    if constexpr (kOwn) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int in_tile = nt * 16 + col, row = first_row + in_tile;
+        if (row >= n * group) continue;
         if (whole) {
           const int j = row / group, head = group_head(a.groups, h, row - j * group);
-          float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-          if (!good) inv = __uint_as_float(kNanBits);            // a length that cannot be
-          uint16_t* dst = a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + g * 32;
+          const float inv = !good ? __uint_as_float(kNanBits) : l[nt] == 0.0f ? 0.0f : 1.0f / l[nt];
+          uint16_t* dst = a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + quad * 32;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x4*>(dst + i * 8) = u32x4{pack_bf16(acc[0][0][i] * inv, acc[0][1][i] * inv), pack_bf16(acc[0][2][i] * inv, acc[0][3][i] * inv),
-                                                           pack_bf16(acc[0][4][i] * inv, acc[0][5][i] * inv), pack_bf16(acc[0][6][i] * inv, acc[0][7][i] * inv)};
-          if (g == 0) {
-            if (a.lse != nullptr)
-              a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = good ? (m[0] + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f : inv;
-            if (a.weight_out != nullptr)
-              *reinterpret_cast<f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head)) = f32x2{ref - kLift, inv};
-          }
+            *reinterpret_cast<u32x4*>(dst + i * 8) = u32x4{pack_bf16(acc[nt][0][i] * inv, acc[nt][1][i] * inv), pack_bf16(acc[nt][2][i] * inv, acc[nt][3][i] * inv),
+                                                           pack_bf16(acc[nt][4][i] * inv, acc[nt][5][i] * inv), pack_bf16(acc[nt][6][i] * inv, acc[nt][7][i] * inv)};
+          if (quad == 0) row_done(j, head, m[nt], l[nt], inv);
         } else {
-          float* dst = a.part_o + (int64_t(slot) * kRows + n16) * kHeadDim + g * 32;
+          float* dst = a.part_o + (slot_row + in_tile) * kHeadDim + quad * 32;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<f32x4*>(dst + i * 8) = f32x4{acc[0][0][i], acc[0][1][i], acc[0][2][i], acc[0][3][i]};
-            *reinterpret_cast<f32x4*>(dst + i * 8 + 4) = f32x4{acc[0][4][i], acc[0][5][i], acc[0][6][i], acc[0][7][i]};
+            *reinterpret_cast<f32x4*>(dst + i * 8) = f32x4{acc[nt][0][i], acc[nt][1][i], acc[nt][2][i], acc[nt][3][i]};
+            *reinterpret_cast<f32x4*>(dst + i * 8 + 4) = f32x4{acc[nt][4][i], acc[nt][5][i], acc[nt][6][i], acc[nt][7][i]};
           }
-          if (g == 0) {
-            a.part_ml[int64_t(slot) * 2 * kRows + n16] = m[0];
-            a.part_ml[int64_t(slot) * 2 * kRows + kRows + n16] = sum;
+          if (quad == 0) {
+            a.part_ml[slot_row * 2 + in_tile] = m[nt];
+            a.part_ml[slot_row * 2 + kRows + in_tile] = l[nt];
           }
         }
       }
     } else {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        if (g == 0) {
-          lds_m[wave][nt * 16 + n16] = m[nt];
-          lds_l[wave][nt * 16 + n16] = l[nt];
+        if (quad == 0) {
+          lds_m[wave][nt * 16 + col] = m[nt];
+          lds_l[wave][nt * 16 + col] = l[nt];
         }
       }
 #pragma unroll
@@ -479,20 +518,20 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(C
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float* dst = &lds_o[wave][n16][(g * 4 + i) * 8];
+          float* dst = &lds_o[wave][col][(quad * 4 + i) * 8];
           *reinterpret_cast<f32x4*>(dst) = f32x4{acc[nt][0][i], acc[nt][1][i], acc[nt][2][i], acc[nt][3][i]};
           *reinterpret_cast<f32x4*>(dst + 4) = f32x4{acc[nt][4][i], acc[nt][5][i], acc[nt][6][i], acc[nt][7][i]};
         }
         __syncthreads();
-        const int r = tid >> 4, d = (tid & 15) * 8, in_tile = nt * 16 + r, row = it.tile * kRows + in_tile;
+        const int r = tid >> 4, d = (tid & 15) * 8, in_tile = nt * 16 + r, row = first_row + in_tile;
         if (row < n * group) {
           float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_m[w][in_tile]);
+          for (int w = 0; w < WAVES; ++w) top = fmaxf(top, lds_m[w][in_tile]);
           const float ref = top == -INFINITY ? 0.0f : top;
           f32x4 o0 = {0.0f, 0.0f, 0.0f, 0.0f}, o1 = o0;
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) {
+          for (int w = 0; w < WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f(lds_m[w][in_tile] - ref);
             sum += f * lds_l[w][in_tile];
             o0 += f * *reinterpret_cast<const f32x4*>(&lds_o[w][r][d]);
@@ -500,31 +539,24 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 2 : 1) void cache_attn_kernel(C
           }
           if (whole) {
             const int j = row / group, head = group_head(a.groups, h, row - j * group);
-            float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            if (!good) inv = __uint_as_float(kNanBits);            // a length that cannot be
-            const u32x4 o = {pack_bf16(o0.x * inv, o0.y * inv), pack_bf16(o0.z * inv, o0.w * inv),
-                             pack_bf16(o1.x * inv, o1.y * inv), pack_bf16(o1.z * inv, o1.w * inv)};
-            *reinterpret_cast<u32x4*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d) = o;
-            if (d == 0) {
-              if (a.lse != nullptr)
-                a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = good ? (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f : inv;
-              if (a.weight_out != nullptr)
-                *reinterpret_cast<f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head)) = f32x2{ref - kLift, inv};
-            }
+            const float inv = !good ? __uint_as_float(kNanBits) : sum == 0.0f ? 0.0f : 1.0f / sum;
+            *reinterpret_cast<u32x4*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d) =
+                u32x4{pack_bf16(o0.x * inv, o0.y * inv), pack_bf16(o0.z * inv, o0.w * inv), pack_bf16(o1.x * inv, o1.y * inv), pack_bf16(o1.z * inv, o1.w * inv)};
+            if (d == 0) row_done(j, head, top, sum, inv);
           } else {
-            float* dst = a.part_o + (int64_t(slot) * kRows + in_tile) * kHeadDim + d;
+            float* dst = a.part_o + (slot_row + in_tile) * kHeadDim + d;
             *reinterpret_cast<f32x4*>(dst) = o0;
             *reinterpret_cast<f32x4*>(dst + 4) = o1;
             if (d == 0) {
-              a.part_ml[int64_t(slot) * 2 * kRows + in_tile] = top;
-              a.part_ml[int64_t(slot) * 2 * kRows + kRows + in_tile] = sum;
+              a.part_ml[slot_row * 2 + in_tile] = top;
+              a.part_ml[slot_row * 2 + kRows + in_tile] = sum;
             }
           }
         }
       }
       __syncthreads();
     }
-    if (u0 == 0 && (kShare == 1 ? lane == 0 : tid == 0))         // for the joining kernel: pieces of the item, if it ends in another share
+    if (u0 == 0 && (kOwn ? (tid & 63) == 0 : tid == 0))         // for the joining kernel: pieces of the item, if it ends in another share
       *reinterpret_cast<int2*>(a.begun + 2 * (int64_t(pair) * a.tiles + it.tile)) = int2{worker, whole ? 0 : shares.of(at - it.unit + units - 1) - worker + 1};
     at += u1 - it.unit;
     it.unit = -kStart;
@@ -621,8 +653,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
         u32x4 kc[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) kc[x] = *reinterpret_cast<const u32x4*>(a.c.k + page.byte + (t * 16 + n16) * kHeadDim + g * 16 + x * 64);
-        key_operands<FMT>(kc[0], k[t][0], k[t][1]);
-        key_operands<FMT>(kc[1], k[t][2], k[t][3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) k[t][e] = key_operand<FMT>(kc[e >> 1][2 * (e & 1)], kc[e >> 1][2 * (e & 1) + 1]);
       }
       f32x4 w[4];
 #pragma unroll
@@ -678,21 +710,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
 
 template <int FMT>
 int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compute_units, hipStream_t stream) {
-  static_assert(kCacheMaxWorkers % kWaves == 0, "");
-  const int two = min(kCacheMaxWorkers / kWaves, compute_units * 2), one = min(two, compute_units);
+  const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2);
   if (a.t.n_tokens > 0) {
-    if (rows == 16) cache_attn_kernel<1, 1, FMT><<<two, kThreads, 0, stream>>>(a, 1);
-    else if (rows == 32) cache_attn_kernel<2, kWaves, FMT><<<one, kThreads, 0, stream>>>(a, kWaves);
-    else cache_attn_kernel<4, kWaves, FMT><<<one, kThreads, 0, stream>>>(a, kWaves);
+    if (rows == 16) cache_attn_kernel<1, 1, FMT><<<grid, kThreads, 0, stream>>>(a, 1);
+    else cache_attn_kernel<2, kWaves, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
     cache_join_kernel<<<dim3(a.c.n_seq * a.c.n_kv_heads * a.tiles, min(rows, most_rows)), kThreads, 0, stream>>>(a, rows);
   }
-  if (a.weight_out != nullptr) cache_weight_kernel<FMT><<<two, kThreads, 0, stream>>>(a);
+  if (a.weight_out != nullptr) cache_weight_kernel<FMT><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
 }
 
 }  // namespace
 
-int32_t cache_attn_rows(int64_t most_rows) { return most_rows <= 16 ? 16 : most_rows <= 32 ? 32 : 64; }
+int32_t cache_attn_rows(int64_t most_rows) { return most_rows <= 16 ? 16 : 32; }
 
 int32_t launch_cache_attn(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream) {
   const int rows = cache_attn_rows(most_rows);

@@ -56,16 +56,16 @@ struct CacheAttnArgs {
   float* stats;                    // [n_tokens][n_q_heads][2]: reference exponent and 1 / denominator, for the weights
 };
 
-// Shares of an attention launch at most: of launches in 16 rows every wave's own, of others a workgroup's; and rows of partial results.
-constexpr int kCacheMaxWorkers = 4096;
-constexpr int64_t kCacheSlotRows = 2 * kCacheMaxWorkers * 16;
-static_assert(kCacheSlotRows == 2 * (kCacheMaxWorkers / 4) * 64, "as many of 64 rows as of 16");
+// Shares of an attention launch at most: of up to 16 rows every wave's own, of more a workgroup's; and rows of partial results, two tiles a share.
+constexpr int kCacheMaxWorkers = 2048;
+constexpr int64_t kCacheSlotRows = int64_t(2) * kCacheMaxWorkers * 16;
+static_assert(kCacheSlotRows >= int64_t(2) * (kCacheMaxWorkers / 4) * 32, "those of 32 rows, too");
 
 int32_t launch_cache_append(const CacheArgs& c, const StepArgs& t, const void* k, const void* v, hipStream_t stream);
 int32_t launch_cache_load(const CacheArgs& c, const StepArgs& t, void* k, void* v, hipStream_t stream);
 int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int32_t* keep, int32_t n_sink, int32_t n_recent,
                            const CacheArgs& dst, float* weight_out, int32_t* kept, hipStream_t stream);
-// Rows (query token, head of the group) that a workgroup works on together.
+// Rows (query token, head of the group) of an item of the list that the work is divided from.
 int32_t cache_attn_rows(int64_t most_rows);
 int32_t launch_cache_attn(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
 
@@ -146,19 +146,26 @@ __device__ __forceinline__ void from_codes(uint32_t w, float (&x)[4]) {
     x[0] = float(int(w << 24) >> 24); x[1] = float(int(w << 16) >> 24); x[2] = float(int(w << 8) >> 24); x[3] = float(int(w) >> 24);
   }
 }
-// Two codes, the low or the high half of w, as fp16 (exact in both formats).
+// Two codes, the low or the high half of w, as fp16, times a scale that is a power of two.  Exact wherever the results are fp16 numbers
+// (fp16_scale(); with 1 always).  int8 codes come with their sign bits turned (turned()): code + 128.
 template <int FMT, bool HIGH>
-__device__ __forceinline__ uint32_t half_codes(uint32_t w) {
+__device__ __forceinline__ uint32_t half_codes(uint32_t w, float scale = 1.0f) {
   if constexpr (FMT == SHPLB_CACHE_E4M3) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH));
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, HIGH));
   } else {
-    // 0x6400 | u is 1024 + u in fp16: u = code + 128 (w comes with the sign bits turned), less 1152
+    // 0x6400 | u is 1024 + u in fp16
     const uint32_t u = __builtin_amdgcn_perm(0x64646464u, w, HIGH ? 0x04030402u : 0x04010400u);
-    const f16x2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
-    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, u) - bias);
+    const _Float16 f = (_Float16)scale, bias = (_Float16)(-1152.0f * scale);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, u), f16x2{f, f}, f16x2{bias, bias}));
   }
 }
 template <int FMT>
 __device__ __forceinline__ uint32_t turned(uint32_t w) { return FMT == SHPLB_CACHE_E4M3 ? w : w ^ 0x80808080u; }
+// Whether all codes times this scale are fp16 numbers (in e4m3 448 * 2^7 and 2^-9 * 2^-15; in int8 so that the scale and 1152 times it are, too).
+template <int FMT>
+__device__ __forceinline__ bool fp16_scale(float scale) {
+  const uint32_t b = __float_as_uint(scale), lowest = FMT == SHPLB_CACHE_E4M3 ? 127 - 15 : 127 - 14, most = FMT == SHPLB_CACHE_E4M3 ? 127 + 7 : 127 + 5;
+  return (b & 0x7fffffu) == 0 && (b >> 23) - lowest <= most - lowest;
+}
 
 }  // namespace shplb

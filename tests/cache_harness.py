@@ -92,14 +92,14 @@ def check_attn(c, got_out, got_lse, q, cu, kv_of, scale=None, got_weight=None, w
     with intermediate roundings of the matrix pipe's own (two halves of a step each): 2 * 130 * 2^-24 of the sum of their magnitudes,
     and as much as 2^-23 of itself for each of three multiplications; a probability moves by as much as its score and the
     denominator's logarithm do, 2^-22 for each exponential, n additions of the denominator taken 64 apart; fp16
-    probabilities 2^-11, the result bf16 2^-8.  Probabilities are held at 2^15 of the largest one's size and fp16's steps end at 2^-24: half a
-    step is 2^-25 * 2^-15 = 2^-40 of the largest, at most 2^-40 of |v| for each key."""
+    probabilities 2^-11, the result bf16 2^-8.  Probabilities are held at 2^7 times their size against a reference that is never above the largest one, and
+    fp16's steps end at 2^-24: half a step is 2^-25 * 2^-7 = 2^-32 of the reference, at most 2^-32 of |v| for each key."""
     out, lse, weight, size, all_v, reach = orc.attn(c, q, cu, kv_of, scale, weight_in)
     n = max(1, int(np.maximum(c.lens, 0).max()))
     dz = reach * (2 * 130 * 2.0 ** -24 + 3 * 2.0 ** -23)
     dp = 2 * dz + 2.0 ** -21 + (n / 64 + 80) * 2.0 ** -24
     there = slice(0, int(cu[-1]))
-    tol = 2.0 ** -8 * np.abs(out) + (2.0 ** -11 + dp) * size * (1 + 2.0 ** -8) + 2.0 ** -40 * all_v + 1e-30
+    tol = 2.0 ** -8 * np.abs(out) + (2.0 ** -11 + dp) * size * (1 + 2.0 ** -8) + 2.0 ** -32 * all_v + 1e-30
     diff = np.abs(got_out[there] - out[there])
     assert (np.isnan(got_out[there]) == np.isnan(out[there])).all()
     worst = np.nanmax(np.where(np.isnan(diff), 0, diff / tol[there]), initial=0.0)
