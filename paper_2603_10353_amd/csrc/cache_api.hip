@@ -165,7 +165,7 @@ int32_t shplb_cache_evict_workspace_bytes(const shplb_cache* cache, int64_t* byt
   if (!bytes_out) return SHPLB_E_NULL;
   CacheArgs c;
   if (int32_t st = check_cache(cache, &c)) return st;
-  *bytes_out = 256;
+  *bytes_out = cache_evict_workspace(c);
   return SHPLB_OK;
 }
 
@@ -181,7 +181,7 @@ int32_t shplb_cache_evict(const shplb_cache* cache, const float* weight, const i
   if (weight == weight_out || misaligned(weight, 4) || misaligned(keep, 4) || misaligned(weight_out, 4) || misaligned(kept_out, 4) ||
       misaligned(workspace, 256))
     return SHPLB_E_SHAPE;
-  return launch_cache_evict(c, weight, keep, n_sink, n_recent, d, weight_out, kept_out, static_cast<hipStream_t>(stream));
+  return launch_cache_evict(c, weight, keep, n_sink, n_recent, d, weight_out, kept_out, workspace, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

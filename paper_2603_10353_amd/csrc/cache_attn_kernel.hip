@@ -626,12 +626,31 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a, i
   }
 }
 
+// Sums over the sixteen lanes of a row of lanes, of which lane j is left with that of x[j]: every step halves the values a lane looks after.
+__device__ __forceinline__ float sums_of_rows(float (&x)[16], int lane) {
+  const auto halve = [&](auto dpp, int n, bool upper) {
+#pragma unroll
+    for (int j = 0; j < n; ++j) {
+      const float keep = upper ? x[j + n] : x[j], give = upper ? x[j] : x[j + n];
+      x[j] = keep + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(give), decltype(dpp)::value, 0xf, 0xf, true));
+    }
+  };
+  halve(std::integral_constant<int, 0x128>{}, 8, lane & 8);     // from lane ^ 8
+  halve(std::integral_constant<int, 0x141>{}, 4, lane & 4);     // from lane ^ 7
+  halve(std::integral_constant<int, 0x4e>{}, 2, lane & 2);      // from lane ^ 2
+  halve(std::integral_constant<int, 0xb1>{}, 1, lane & 1);      // from lane ^ 1
+  return x[0];
+}
+
 // weight_out = weight_in + the probabilities that the step's rows put on each key, taken again from the keys and the rows' statistics: every
-// key belongs to one wave, so nothing is added up between workgroups.
-template <int FMT>
+// key belongs to one wave, so nothing is added up between workgroups.  16 NT rows at a time; where there are more, the keys are gone
+// through again for them (of a wave's share, one time right after the other).
+template <int NT, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs a) {
+  __shared__ f16x8 lds_q[kWaves][NT][4][64];
   __shared__ int lds_i[kWaves + kThreads];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+  const int k_byte = n16 * kHeadDim + g * 16;
   int at, end;
   Shares shares;
   Item it = locate<true, 1>(a, int(blockIdx.x) + wave * int(gridDim.x), int(gridDim.x) * kWaves, 1, lds_i, at, end, shares);
@@ -642,67 +661,90 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
     const int len = it.len, group = group_size(a.groups, h), rows = n * group;
     pair_units<true, 1>(a, rows, len, tiles, units);
     const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
-    const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
-    for (int u = u0; u < u1; ++u) {
-      const Page page = page_at(a.c, page_number(a.c, pair, u), u);
-      const float k_scale = page.bad ? __uint_as_float(kNanBits) : page.k_scale;
-      const int key0 = u * kUnit;
-      f16x8 k[4][4];
+    const int64_t weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
+    const float* before = a.weight_in;
+    int first_row = 0;
+    do {
+      const int groups = min(NT, (rows - first_row + 15) >> 4);   // of sixteen rows
+      Keys kc;
+      Page here = page_at(a.c, page_number(a.c, pair, max(min(u0, u1 - 1), 0)), max(min(u0, u1 - 1), 0));
+      int page_next = page_number(a.c, pair, max(min(u0 + 1, u1 - 1), 0));
+      load_keys<false>(a, here, u0 < u1, k_byte, kc);
+      __builtin_amdgcn_sched_barrier(0);
+      float to_log2[NT], m[NT], inv[NT];
+      int seen[NT];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        u32x4 kc[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) kc[x] = *reinterpret_cast<const u32x4*>(a.c.k + page.byte + (t * 16 + n16) * kHeadDim + g * 16 + x * 64);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) k[t][e] = key_operand<FMT>(kc[e >> 1][2 * (e & 1)], kc[e >> 1][2 * (e & 1) + 1]);
-      }
-      f32x4 w[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) w[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      for (int r0 = 0; r0 < rows; r0 += 16) {
+      for (int nt = 0; nt < NT; ++nt) {
+        const int row = first_row + nt * 16 + n16;
         f16x8 q[4];
-        const int row = r0 + n16;
-        const float c = load_queries(a, row0, n, h, group, row, q) * k_scale;
-        int seen = 0;
-        float m = 0.0f, inv = 0.0f;
-        if (row < rows) {
-          const int j = row / group, head = group_head(a.groups, h, row - j * group);
-          const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head));
-          seen = len - n + 1 + j;
-          m = st.x;
-          inv = st.y;
-        }
+        to_log2[nt] = m[nt] = inv[nt] = 0.0f;
+        seen[nt] = 0;
+        if (nt < groups) {
+          to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[t][e], q[e], x, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = __builtin_amdgcn_exp2f(x[i] * c - m) * inv;
-            w[t][i] += key0 + t * 16 + g * 4 + i < seen ? p : 0.0f;
+          for (int e = 0; e < 4; ++e) lds_q[wave][nt][e][lane] = q[e];
+          if (row < rows) {
+            const int j = row / group, head = group_head(a.groups, h, row - j * group);
+            const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head));
+            seen[nt] = len - n + 1 + j;
+            m[nt] = st.x;
+            inv[nt] = st.y;
           }
         }
       }
-      // over the sixteen rows; lane n16 == 0 of each group of keys writes
+      const int seen_first = len - n + 1 + first_row / max(group, 1);
+      for (int u = u0; u < u1; ++u) {
+        const float k_scale = here.bad ? __uint_as_float(kNanBits) : here.k_scale;
+        const Page ahead = page_at(a.c, page_next, min(u + 1, u1 - 1));
+        page_next = page_number(a.c, pair, min(u + 2, u1 - 1));
+        const int key0 = u * kUnit;
+        // this lane's key, once the sums over the rows are taken
+        const int key = key0 + (n16 >> 2) * 16 + g * 4 + (n16 & 3);
+        float old = 0.0f;
+        if (before != nullptr && key < len) old = before[weights + key];
+        f32x4 sc[NT][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+        for (int e = 0; e < 4; ++e) {
+          f16x8 k[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int t = 0; t < 4; ++t) k[t] = key_operand<FMT>(kc.code[t][e >> 1][2 * (e & 1)], kc.code[t][e >> 1][2 * (e & 1) + 1]);
 #pragma unroll
-          for (int d = 1; d < 16; d <<= 1) w[t][i] += __shfl_xor(w[t][i], d);
+          for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0 && nt >= groups) break;
+            const f16x8 q = lds_q[wave][nt][e][lane];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (n16 != t) continue;
-        const int key = key0 + t * 16 + g * 4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (key + i < len) {
-            const int64_t x = row_of_weights + key + i;
-            a.weight_out[x] = (a.weight_in != nullptr ? a.weight_in[x] : 0.0f) + w[t][i];
+            for (int t = 0; t < 4; ++t)
+              sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[t], q, e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[nt][t], 0, 0, 0);
           }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        load_keys<false>(a, ahead, u + 1 < u1, k_byte, kc);
+        __builtin_amdgcn_sched_barrier(0);
+        float w[16];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) w[x] = 0.0f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (nt >= groups) break;
+          const float c = to_log2[nt] * k_scale;
+          if (key0 + kUnit > seen_first) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const float p = __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - m[nt]) * inv[nt];
+              w[x] += key0 + (x >> 2) * 16 + g * 4 + (x & 3) < seen[nt] ? p : 0.0f;
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) w[x] += __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - m[nt]) * inv[nt];
+          }
+        }
+        const float sum = sums_of_rows(w, lane);
+        if (key < len) a.weight_out[weights + key] = old + sum;
+        here = ahead;
       }
-    }
+      before = a.weight_out;
+      first_row += 16 * NT;
+    } while (first_row < rows);
     at += units - it.unit;
     it = next_pair(a, pair);
   }
@@ -716,7 +758,10 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
     else cache_attn_kernel<2, kWaves, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
     cache_join_kernel<<<dim3(a.c.n_seq * a.c.n_kv_heads * a.tiles, min(rows, most_rows)), kThreads, 0, stream>>>(a, rows);
   }
-  if (a.weight_out != nullptr) cache_weight_kernel<FMT><<<grid, kThreads, 0, stream>>>(a);
+  if (a.weight_out != nullptr) {
+    if (rows == 16) cache_weight_kernel<1, FMT><<<grid, kThreads, 0, stream>>>(a);
+    else cache_weight_kernel<4, FMT><<<grid, kThreads, 0, stream>>>(a);
+  }
   return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
 }
 

@@ -64,7 +64,8 @@ static_assert(kCacheSlotRows >= int64_t(2) * (kCacheMaxWorkers / 4) * 32, "those
 int32_t launch_cache_append(const CacheArgs& c, const StepArgs& t, const void* k, const void* v, hipStream_t stream);
 int32_t launch_cache_load(const CacheArgs& c, const StepArgs& t, void* k, void* v, hipStream_t stream);
 int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int32_t* keep, int32_t n_sink, int32_t n_recent,
-                           const CacheArgs& dst, float* weight_out, int32_t* kept, hipStream_t stream);
+                           const CacheArgs& dst, float* weight_out, int32_t* kept, void* workspace, hipStream_t stream);
+int64_t cache_evict_workspace(const CacheArgs& c);
 // Rows (query token, head of the group) of an item of the list that the work is divided from.
 int32_t cache_attn_rows(int64_t most_rows);
 int32_t launch_cache_attn(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
@@ -114,26 +115,54 @@ __device__ __forceinline__ uint32_t larger_scale(uint32_t a, uint32_t b) {
   return max(int32_t(a), int32_t(b));
 }
 
-// The largest magnitude (divided by the scale) that may be rounded: at the largest scale codes stay at those whose
-// values are finite.  (240 * 2^120 and 63 * 2^122; one step more is 2^128.)
+// The codes of four values times f, the inverse of their page's scale, to nearest, ties to even: the product is exact, the one rounding is
+// that of the conversion, in int8 that of adding 1.5 * 2^23.  `last`: the page has the largest scale there is, at which codes stay at those whose
+// values are finite (240 * 2^120 and 63 * 2^122; one step more is 2^128).
 template <int FMT>
-__device__ __forceinline__ float code_limit(uint32_t scale) {
-  if constexpr (FMT == SHPLB_CACHE_E4M3) return scale >= (247u << 23) ? 240.0f : 448.0f;
-  return scale >= (249u << 23) ? 63.0f : 127.0f;
-}
-
-// Four codes of values that are already divided by the scale, to nearest, ties to even.
+__device__ __forceinline__ bool last_scale(uint32_t scale) { return scale >= (FMT == SHPLB_CACHE_E4M3 ? 247u : 249u) << 23; }
 template <int FMT>
-__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d, float limit) {
-  a = __builtin_amdgcn_fmed3f(a, -limit, limit);
-  b = __builtin_amdgcn_fmed3f(b, -limit, limit);
-  c = __builtin_amdgcn_fmed3f(c, -limit, limit);
-  d = __builtin_amdgcn_fmed3f(d, -limit, limit);
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d, float f, bool last) {
+  if (last) {
+    const float limit = (FMT == SHPLB_CACHE_E4M3 ? 240.0f : 63.0f) / f;
+    a = __builtin_amdgcn_fmed3f(a, -limit, limit);
+    b = __builtin_amdgcn_fmed3f(b, -limit, limit);
+    c = __builtin_amdgcn_fmed3f(c, -limit, limit);
+    d = __builtin_amdgcn_fmed3f(d, -limit, limit);
+  }
   if constexpr (FMT == SHPLB_CACHE_E4M3) {
-    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c * f, d * f, __builtin_amdgcn_cvt_pk_fp8_f32(a * f, b * f, 0, false), true);
   } else {
-    const uint32_t x = int(__builtin_rintf(a)), y = int(__builtin_rintf(b)), z = int(__builtin_rintf(c)), w = int(__builtin_rintf(d));
-    return (x & 0xff) | (y & 0xff) << 8 | (z & 0xff) << 16 | w << 24;
+    constexpr float kMagic = 12582912.0f;
+    const uint32_t x = __float_as_uint(__builtin_fmaf(a, f, kMagic)), y = __float_as_uint(__builtin_fmaf(b, f, kMagic));
+    const uint32_t z = __float_as_uint(__builtin_fmaf(c, f, kMagic)), w = __float_as_uint(__builtin_fmaf(d, f, kMagic));
+    return __builtin_amdgcn_perm(y, x, 0x0c0c0400u) | __builtin_amdgcn_perm(w, z, 0x04000c0cu);
+  }
+}
+// The largest magnitude of sixteen codes, as a number.
+template <int FMT>
+__device__ __forceinline__ float largest_code(u32x4 w) {
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  if constexpr (FMT == SHPLB_CACHE_E4M3) {
+    // magnitudes are in the order of their bits
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+      const u16x2 even = __builtin_bit_cast(u16x2, w[e] & 0x007f007fu), odd = __builtin_bit_cast(u16x2, w[e] >> 8 & 0x007f007fu);
+      top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_elementwise_max(even, odd)));
+    }
+    const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8(max(top & 0xffff, top >> 16), false);
+    return x.x;
+  } else {
+    // every code in the upper byte of sixteen bits
+    i16x2 most = {0, 0}, least = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const i16x2 odd = __builtin_bit_cast(i16x2, w[e] & 0xff00ff00u), even = __builtin_bit_cast(i16x2, w[e] << 8 & 0xff00ff00u);
+      most = __builtin_elementwise_max(most, __builtin_elementwise_max(odd, even));
+      least = __builtin_elementwise_min(least, __builtin_elementwise_min(odd, even));
+    }
+    return float(max(max(int(most.x), int(most.y)), -min(int(least.x), int(least.y))) >> 8);
   }
 }
 // Four codes as numbers.
