@@ -30,8 +30,8 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kUnit = 64;
 // What beginning with an item costs, in units of the list of all units (where it is that many empty ones in front of the item's own):
 // the queries, the first keys, the results, all of them waited for.  For a batch of 128 sequences x 8 heads of lengths between 100 and
-// 16000, where a wave has one to five items, 121 us without, 112 with three.
-constexpr int kStart = 3;
+// 16000, where a wave has one to five items, 102 us without, 97 with two, 100 with five.
+constexpr int kStart = 2;
 constexpr float kLift = 7.0f;                  // log2 of what probabilities are multiplied by, beside their reference ...
 constexpr float kHeadroom = 8.0f;              // ... and how far, in the exponent, they may be above it: 2^15 in fp16
 constexpr int kLdsRow = kHeadDim + 4;          // floats of a row in LDS: rows four banks apart
@@ -254,6 +254,205 @@ __device__ __forceinline__ void load_values(const CacheAttnArgs& a, const Page& 
         x.code[kk][half][i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(v, lane_byte, (kk * 32 + half * 16 + i) * kHeadDim, kOnce ? 2 : 0));
 }
 
+// The rows of a wave: what products are multiplied by, the reference exponent, the denominator, the keys seen and the output of row
+// 16 nt + lane % 16, of which a lane has dims 8 (4 (lane / 16) + i) + t.
+template <int NT>
+struct Rows {
+  float to_log2[NT], m[NT], l[NT];
+  int seen[NT];
+  f32x4 acc[NT][8];
+};
+// What is on its way to a wave: the codes of a unit, where they come from, and the place of the next one in the page table.  Keys are
+// asked for as soon as those of the unit before are operands, values when those are: either come while the other half of the work
+// is done, and one set of registers is enough.  A place in the page table is read one unit more ahead.
+struct Flight {
+  Keys k;
+  Values v;
+  Page here;
+  int page_next;
+};
+
+// Units first, first + STEP .. below end; last: one that can be read in any case.
+template <int STEP, bool ONCE>
+__device__ __forceinline__ void start(const CacheAttnArgs& a, int pair, int first, int end, int last, int lane, bool values, Flight& f) {
+  const int n16 = lane & 15, g = lane >> 4;
+  f.here = page_at(a.c, page_number(a.c, pair, min(first, last)), min(first, last));
+  f.page_next = page_number(a.c, pair, min(first + STEP, last));
+  load_keys<ONCE>(a, f.here, first < end, n16 * kHeadDim + g * 16, f.k);
+  if (values) load_values<ONCE>(a, f.here, first < end, g * 4 * kHeadDim + n16 * 8, f.v);
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Queries of the rows from first_row on into LDS, as each lane needs them: what it reads it wrote itself, and they cost no registers.
+template <int NT>
+__device__ __forceinline__ void take_rows(const CacheAttnArgs& a, int row0, int n, int h, int group, int first_row, int seen_before, int lane,
+                                          f16x8 (*lds_q)[4][64], Rows<NT>& r) {
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = first_row + nt * 16 + (lane & 15);
+    f16x8 q[4];
+    r.to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds_q[nt][e][lane] = q[e];
+    r.seen[nt] = row < n * group ? seen_before + row / group : 0;
+    r.m[nt] = -INFINITY;
+    r.l[nt] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) r.acc[nt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+}
+
+// Scores of a unit, S^T, of `groups` times sixteen rows.
+template <int NT, int FMT>
+__device__ __forceinline__ void scores(const Keys& keys, const f16x8 (*lds_q)[4][64], int lane, int groups, f32x4 (&sc)[NT][4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f16x8 k[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) k[t] = key_operand<FMT>(keys.code[t][e >> 1][2 * (e & 1)], keys.code[t][e >> 1][2 * (e & 1) + 1]);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (nt > 0 && nt >= groups) break;
+      const f16x8 q = lds_q[nt][e][lane];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[t], q, e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[nt][t], 0, 0, 0);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Goes through the units first, first + STEP ..; seen_first: the fewest keys that a row sees.
+template <int NT, int STEP, bool ONCE, int FMT>
+__device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first,
+                                       const f16x8 (*lds_q)[4][64], int lane, Flight& f, Rows<NT>& r) {
+  const int n16 = lane & 15, g = lane >> 4, k_byte = n16 * kHeadDim + g * 16, v_byte = g * 4 * kHeadDim + n16 * 8;
+  for (int u = first; u < end; u += STEP) {
+    const float k_scale = f.here.bad ? __uint_as_float(kNanBits) : f.here.k_scale, v_scale = f.here.bad ? k_scale : f.here.v_scale;
+    const bool more = u + STEP < end;
+    const Page ahead = page_at(a.c, f.page_next, min(u + STEP, last));
+    f.page_next = page_number(a.c, pair, min(u + 2 * STEP, last));
+    const int key0 = u * kUnit;
+    f32x4 sc[NT][4];
+    scores<NT, FMT>(f.k, lds_q, lane, NT, sc);
+    load_keys<ONCE>(a, ahead, more, k_byte, f.k);
+    __builtin_amdgcn_sched_barrier(0);
+    // the reference exponent, raised where a score is more than 2^kHeadroom above it
+    float to[NT], top[NT];
+    bool raise = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      to[nt] = r.to_log2[nt] * k_scale;
+      if (key0 + kUnit > seen_first) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[nt][t][i] = key0 + t * 16 + g * 4 + i < r.seen[nt] ? sc[nt][t][i] * to[nt] : -INFINITY;
+        to[nt] = 1.0f;
+      }
+      top[nt] = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[nt] = fmaxf(top[nt], sc[nt][t][i]);
+      top[nt] = quad_max(top[nt] * to[nt]);
+      raise |= top[nt] > r.m[nt] + kHeadroom;
+    }
+    if (__ballot(raise)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float m_new = top[nt] > r.m[nt] + kHeadroom ? top[nt] : r.m[nt];
+        const float alpha = m_new == r.m[nt] ? 1.0f : __builtin_amdgcn_exp2f(r.m[nt] - m_new);
+        r.m[nt] = m_new;
+        r.l[nt] *= alpha;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) r.acc[nt][t] *= alpha;
+      }
+    }
+    f16x8 p[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float off = kLift - (r.m[nt] == -INFINITY ? 0.0f : r.m[nt]);
+      f16x2 two[8];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        float e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(sc[nt][t][i] * to[nt] + off);
+          r.l[nt] += e[i];
+        }
+        two[2 * t] = f16x2{(_Float16)e[0], (_Float16)e[1]};
+        two[2 * t + 1] = f16x2{(_Float16)e[2], (_Float16)e[3]};
+      }
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, two[4 * kk + e]);
+        p[nt][kk] = __builtin_bit_cast(f16x8, w);
+      }
+    }
+    if (key0 + kUnit > len) {
+      // codes behind the last token may be anything, NaN among them
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (key0 + kk * 32 + half * 16 + g * 4 + i >= len) f.v.code[kk][half][i] = u32x2{0, 0};
+    }
+    // V^T: dim 8 n16 + t of key pairs; two bytes of a pair lie side by side after one permutation.  With a scale that leaves
+    // them fp16 numbers the values themselves are multiplied, and the sums go on where they are; else the codes, and the products
+    // are scaled (a scale of NaN does not reach rows that see none of the page).
+    const bool fp16 = fp16_scale<FMT>(v_scale);
+    const float factor = fp16 ? v_scale : 1.0f;
+#pragma unroll
+    for (int t2 = 0; t2 < 4; ++t2) {                           // dims 2 t2 and 2 t2 + 1
+      __builtin_amdgcn_sched_barrier(0);
+      f16x8 lo[2], hi[2];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        u32x4 wl, wh;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {                          // pairs of keys
+          const uint32_t x = f.v.code[kk][e >> 1][2 * (e & 1)][t2 >> 1], y = f.v.code[kk][e >> 1][2 * (e & 1) + 1][t2 >> 1];
+          const uint32_t w = turned<FMT>(__builtin_amdgcn_perm(y, x, t2 & 1 ? 0x07030602u : 0x05010400u));
+          wl[e] = half_codes<FMT, false>(w, factor);
+          wh[e] = half_codes<FMT, true>(w, factor);
+        }
+        lo[kk] = __builtin_bit_cast(f16x8, wl);
+        hi[kk] = __builtin_bit_cast(f16x8, wh);
+      }
+      if (fp16) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            r.acc[nt][2 * t2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[kk], p[nt][kk], r.acc[nt][2 * t2], 0, 0, 0);
+            r.acc[nt][2 * t2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[kk], p[nt][kk], r.acc[nt][2 * t2 + 1], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            x = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[kk], p[nt][kk], x, 0, 0, 0);
+            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[kk], p[nt][kk], y, 0, 0, 0);
+          }
+          const float scale = key0 < r.seen[nt] ? v_scale : 0.0f;
+          r.acc[nt][2 * t2] += x * scale;
+          r.acc[nt][2 * t2 + 1] += y * scale;
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_values<ONCE>(a, ahead, more, v_byte, f.v);
+    f.here = ahead;
+  }
+}
+
 // Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a workgroup, which
 // take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.  (For 128 rows x 8 heads x
 // 32768 int8 tokens 54 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.  A wave of 64 rows needs half of that but
@@ -264,7 +463,6 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
   constexpr bool kOwn = WAVES == 1;
   constexpr int kRows = 16 * NT;
   static_assert(kOwn || WAVES == kWaves, "one, or all of a workgroup");
-  // queries, as each lane needs them: what it reads it wrote itself, and they cost no registers
   __shared__ f16x8 lds_q[kOwn ? kWaves : 1][NT][4][64];
   __shared__ float lds_o[WAVES][16][kLdsRow];
   __shared__ float lds_m[WAVES][kRows], lds_l[WAVES][kRows];
@@ -280,7 +478,6 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     // takes no registers in between)
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
-    const int n16 = lane & 15, g = lane >> 4, k_byte = n16 * kHeadDim + g * 16, v_byte = g * 4 * kHeadDim + n16 * 8;
     const int pair = it.pair, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads;
     int row0, n, tiles, units;
     step_tokens<true>(a.t, s, row0, n);
@@ -293,175 +490,13 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     const bool good = good_length(a.c, len);
     const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
     if (u1 <= u0) break;                                         // the share ends before the item's first unit
-    // Keys are asked for as soon as those of the unit before are operands, values when those are: either come while the other
-    // half of the work is done, and one set of registers is enough.  A place in the page table is read one unit more ahead.
     const int first_row = it.tile * kRows, u_first = u0 + (kOwn ? 0 : wave), u_end = good && len > 0 ? u1 : 0;
-    Keys kc;
-    Values vc;
-    Page here = page_at(a.c, page_number(a.c, pair, min(u_first, u1 - 1)), min(u_first, u1 - 1));
-    int page_next = page_number(a.c, pair, min(u_first + WAVES, u1 - 1));
-    load_keys<kOwn>(a, here, u_first < u_end, k_byte, kc);
-    load_values<kOwn>(a, here, u_first < u_end, v_byte, vc);
-    __builtin_amdgcn_sched_barrier(0);
-
-    float to_log2[NT], m[NT], l[NT];
-    int seen[NT];                                                // keys that the lane's row sees
-    f32x4 acc[NT][8];
-    const int seen_first = len - n + 1 + first_row / group;      // by the tile's first row: the fewest
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = first_row + nt * 16 + n16;
-      f16x8 q[4];
-      to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
-      // (waves of one share write the same)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) lds_q[kOwn ? wave : 0][nt][e][lane] = q[e];
-      seen[nt] = row < n * group && good ? len - n + 1 + row / group : 0;
-      m[nt] = -INFINITY;
-      l[nt] = 0.0f;
-#pragma unroll
-      for (int t = 0; t < 8; ++t) acc[nt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-
-    for (int u = u_first; u < u_end; u += WAVES) {
-      const float k_scale = here.bad ? __uint_as_float(kNanBits) : here.k_scale, v_scale = here.bad ? k_scale : here.v_scale;
-      const bool more = u + WAVES < u_end;
-      const Page ahead = page_at(a.c, page_next, min(u + WAVES, u1 - 1));
-      page_next = page_number(a.c, pair, min(u + 2 * WAVES, u1 - 1));
-      const int key0 = u * kUnit;
-      f32x4 sc[NT][4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f16x8 q[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) q[nt] = lds_q[kOwn ? wave : 0][nt][e][lane];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const f16x8 k = key_operand<FMT>(kc.code[t][e >> 1][2 * (e & 1)], kc.code[t][e >> 1][2 * (e & 1) + 1]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[nt], e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[nt][t], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      load_keys<kOwn>(a, ahead, more, k_byte, kc);
-      __builtin_amdgcn_sched_barrier(0);
-      // the reference exponent, raised where a score is more than 2^kHeadroom above it
-      float to[NT], top[NT];
-      bool raise = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        to[nt] = to_log2[nt] * k_scale;
-        if (key0 + kUnit > seen_first) {
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sc[nt][t][i] = key0 + t * 16 + g * 4 + i < seen[nt] ? sc[nt][t][i] * to[nt] : -INFINITY;
-          to[nt] = 1.0f;
-        }
-        top[nt] = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) top[nt] = fmaxf(top[nt], sc[nt][t][i]);
-        top[nt] = quad_max(top[nt] * to[nt]);
-        raise |= top[nt] > m[nt] + kHeadroom;
-      }
-      if (__ballot(raise)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float m_new = top[nt] > m[nt] + kHeadroom ? top[nt] : m[nt];
-          const float alpha = m_new == m[nt] ? 1.0f : __builtin_amdgcn_exp2f(m[nt] - m_new);
-          m[nt] = m_new;
-          l[nt] *= alpha;
-#pragma unroll
-          for (int t = 0; t < 8; ++t) acc[nt][t] *= alpha;
-        }
-      }
-      f16x8 p[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float off = kLift - (m[nt] == -INFINITY ? 0.0f : m[nt]);
-        f16x2 two[8];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          float e[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(sc[nt][t][i] * to[nt] + off);
-            l[nt] += e[i];
-          }
-          two[2 * t] = f16x2{(_Float16)e[0], (_Float16)e[1]};
-          two[2 * t + 1] = f16x2{(_Float16)e[2], (_Float16)e[3]};
-        }
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          u32x4 w;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, two[4 * kk + e]);
-          p[nt][kk] = __builtin_bit_cast(f16x8, w);
-        }
-      }
-      if (key0 + kUnit > len) {
-        // codes behind the last token may be anything, NaN among them
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (key0 + kk * 32 + half * 16 + g * 4 + i >= len) vc.code[kk][half][i] = u32x2{0, 0};
-      }
-      // V^T: dim 8 n16 + t of key pairs; two bytes of a pair lie side by side after one permutation.  With a scale that leaves
-      // them fp16 numbers the values themselves are multiplied, and the sums go on where they are; else the codes, and the products
-      // are scaled (a scale of NaN does not reach rows that see none of the page).
-      const bool fp16 = fp16_scale<FMT>(v_scale);
-      const float factor = fp16 ? v_scale : 1.0f;
-#pragma unroll
-      for (int t2 = 0; t2 < 4; ++t2) {                           // dims 2 t2 and 2 t2 + 1
-        __builtin_amdgcn_sched_barrier(0);
-        f16x8 lo[2], hi[2];
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          u32x4 wl, wh;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {                          // pairs of keys
-            const uint32_t x = vc.code[kk][e >> 1][2 * (e & 1)][t2 >> 1], y = vc.code[kk][e >> 1][2 * (e & 1) + 1][t2 >> 1];
-            const uint32_t w = turned<FMT>(__builtin_amdgcn_perm(y, x, t2 & 1 ? 0x07030602u : 0x05010400u));
-            wl[e] = half_codes<FMT, false>(w, factor);
-            wh[e] = half_codes<FMT, true>(w, factor);
-          }
-          lo[kk] = __builtin_bit_cast(f16x8, wl);
-          hi[kk] = __builtin_bit_cast(f16x8, wh);
-        }
-        if (fp16) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-              acc[nt][2 * t2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[kk], p[nt][kk], acc[nt][2 * t2], 0, 0, 0);
-              acc[nt][2 * t2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[kk], p[nt][kk], acc[nt][2 * t2 + 1], 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-              x = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[kk], p[nt][kk], x, 0, 0, 0);
-              y = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[kk], p[nt][kk], y, 0, 0, 0);
-            }
-            const float scale = key0 < seen[nt] ? v_scale : 0.0f;
-            acc[nt][2 * t2] += x * scale;
-            acc[nt][2 * t2 + 1] += y * scale;
-          }
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      load_values<kOwn>(a, ahead, more, v_byte, vc);
-      here = ahead;
-    }
+    f16x8(*q)[4][64] = lds_q[kOwn ? wave : 0];                   // (waves of one share write the same)
+    Flight f;
+    Rows<NT> r;
+    start<WAVES, kOwn>(a, pair, u_first, u_end, u1 - 1, lane, true, f);
+    take_rows<NT>(a, row0, n, h, group, first_row, len - n + 1, lane, q, r);
+    attend<NT, WAVES, kOwn, FMT>(a, pair, len, u_first, u_end, u1 - 1, len - n + 1 + first_row / group, q, lane, f, r);
 
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
@@ -477,7 +512,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
         *reinterpret_cast<f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head)) = f32x2{(top == -INFINITY ? 0.0f : top) - kLift, inv};
     };
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) l[nt] = quad_sum(l[nt]);
+    for (int nt = 0; nt < NT; ++nt) r.l[nt] = quad_sum(r.l[nt]);
     if constexpr (kOwn) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -485,23 +520,23 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
         if (row >= n * group) continue;
         if (whole) {
           const int j = row / group, head = group_head(a.groups, h, row - j * group);
-          const float inv = !good ? __uint_as_float(kNanBits) : l[nt] == 0.0f ? 0.0f : 1.0f / l[nt];
+          const float inv = !good ? __uint_as_float(kNanBits) : r.l[nt] == 0.0f ? 0.0f : 1.0f / r.l[nt];
           uint16_t* dst = a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + quad * 32;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x4*>(dst + i * 8) = u32x4{pack_bf16(acc[nt][0][i] * inv, acc[nt][1][i] * inv), pack_bf16(acc[nt][2][i] * inv, acc[nt][3][i] * inv),
-                                                           pack_bf16(acc[nt][4][i] * inv, acc[nt][5][i] * inv), pack_bf16(acc[nt][6][i] * inv, acc[nt][7][i] * inv)};
-          if (quad == 0) row_done(j, head, m[nt], l[nt], inv);
+            *reinterpret_cast<u32x4*>(dst + i * 8) = u32x4{pack_bf16(r.acc[nt][0][i] * inv, r.acc[nt][1][i] * inv), pack_bf16(r.acc[nt][2][i] * inv, r.acc[nt][3][i] * inv),
+                                                           pack_bf16(r.acc[nt][4][i] * inv, r.acc[nt][5][i] * inv), pack_bf16(r.acc[nt][6][i] * inv, r.acc[nt][7][i] * inv)};
+          if (quad == 0) row_done(j, head, r.m[nt], r.l[nt], inv);
         } else {
           float* dst = a.part_o + (slot_row + in_tile) * kHeadDim + quad * 32;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<f32x4*>(dst + i * 8) = f32x4{acc[nt][0][i], acc[nt][1][i], acc[nt][2][i], acc[nt][3][i]};
-            *reinterpret_cast<f32x4*>(dst + i * 8 + 4) = f32x4{acc[nt][4][i], acc[nt][5][i], acc[nt][6][i], acc[nt][7][i]};
+            *reinterpret_cast<f32x4*>(dst + i * 8) = f32x4{r.acc[nt][0][i], r.acc[nt][1][i], r.acc[nt][2][i], r.acc[nt][3][i]};
+            *reinterpret_cast<f32x4*>(dst + i * 8 + 4) = f32x4{r.acc[nt][4][i], r.acc[nt][5][i], r.acc[nt][6][i], r.acc[nt][7][i]};
           }
           if (quad == 0) {
-            a.part_ml[slot_row * 2 + in_tile] = m[nt];
-            a.part_ml[slot_row * 2 + kRows + in_tile] = l[nt];
+            a.part_ml[slot_row * 2 + in_tile] = r.m[nt];
+            a.part_ml[slot_row * 2 + kRows + in_tile] = r.l[nt];
           }
         }
       }
@@ -509,8 +544,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         if (quad == 0) {
-          lds_m[wave][nt * 16 + col] = m[nt];
-          lds_l[wave][nt * 16 + col] = l[nt];
+          lds_m[wave][nt * 16 + col] = r.m[nt];
+          lds_l[wave][nt * 16 + col] = r.l[nt];
         }
       }
 #pragma unroll
@@ -519,11 +554,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float* dst = &lds_o[wave][col][(quad * 4 + i) * 8];
-          *reinterpret_cast<f32x4*>(dst) = f32x4{acc[nt][0][i], acc[nt][1][i], acc[nt][2][i], acc[nt][3][i]};
-          *reinterpret_cast<f32x4*>(dst + 4) = f32x4{acc[nt][4][i], acc[nt][5][i], acc[nt][6][i], acc[nt][7][i]};
+          *reinterpret_cast<f32x4*>(dst) = f32x4{r.acc[nt][0][i], r.acc[nt][1][i], r.acc[nt][2][i], r.acc[nt][3][i]};
+          *reinterpret_cast<f32x4*>(dst + 4) = f32x4{r.acc[nt][4][i], r.acc[nt][5][i], r.acc[nt][6][i], r.acc[nt][7][i]};
         }
         __syncthreads();
-        const int r = tid >> 4, d = (tid & 15) * 8, in_tile = nt * 16 + r, row = first_row + in_tile;
+        const int in_group = tid >> 4, d = (tid & 15) * 8, in_tile = nt * 16 + in_group, row = first_row + in_tile;
         if (row < n * group) {
           float top = -INFINITY, sum = 0.0f;
 #pragma unroll
@@ -534,8 +569,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
           for (int w = 0; w < WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f(lds_m[w][in_tile] - ref);
             sum += f * lds_l[w][in_tile];
-            o0 += f * *reinterpret_cast<const f32x4*>(&lds_o[w][r][d]);
-            o1 += f * *reinterpret_cast<const f32x4*>(&lds_o[w][r][d + 4]);
+            o0 += f * *reinterpret_cast<const f32x4*>(&lds_o[w][in_group][d]);
+            o1 += f * *reinterpret_cast<const f32x4*>(&lds_o[w][in_group][d + 4]);
           }
           if (whole) {
             const int j = row / group, head = group_head(a.groups, h, row - j * group);
@@ -642,15 +677,62 @@ __device__ __forceinline__ float sums_of_rows(float (&x)[16], int lane) {
   return x[0];
 }
 
-// weight_out = weight_in + the probabilities that the step's rows put on each key, taken again from the keys and the rows' statistics: every
-// key belongs to one wave, so nothing is added up between workgroups.  16 NT rows at a time; where there are more, the keys are gone
-// through again for them (of a wave's share, one time right after the other).
+// What rows need of their attention to say which weights they gave.
+template <int NT>
+struct Statistics {
+  float to_log2[NT], m[NT], inv[NT];           // inv: 1 / denominator
+  int seen[NT];
+};
+
+// weight_out = before + the probabilities that the rows put on each key of units first, first + STEP ..
+template <int NT, int STEP, int FMT>
+__device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first, int groups,
+                                      const f16x8 (*lds_q)[4][64], const float* before, int lane, Flight& f, const Statistics<NT>& r) {
+  const int n16 = lane & 15, g = lane >> 4;
+  const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
+  for (int u = first; u < end; u += STEP) {
+    const float k_scale = f.here.bad ? __uint_as_float(kNanBits) : f.here.k_scale;
+    const Page ahead = page_at(a.c, f.page_next, min(u + STEP, last));
+    f.page_next = page_number(a.c, pair, min(u + 2 * STEP, last));
+    const int key0 = u * kUnit, key = key0 + (n16 >> 2) * 16 + g * 4 + (n16 & 3);   // the key that is the lane's once sums over the rows are taken
+    float old = 0.0f;
+    if (before != nullptr && key < len) old = before[row_of_weights + key];
+    f32x4 sc[NT][4];
+    scores<NT, FMT>(f.k, lds_q, lane, groups, sc);
+    load_keys<false>(a, ahead, u + STEP < end, n16 * kHeadDim + g * 16, f.k);
+    __builtin_amdgcn_sched_barrier(0);
+    float w[16];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) w[x] = 0.0f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (nt >= groups) break;
+      const float c = r.to_log2[nt] * k_scale;
+      if (key0 + kUnit > seen_first) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const float p = __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - r.m[nt]) * r.inv[nt];
+          w[x] += key0 + (x >> 2) * 16 + g * 4 + (x & 3) < r.seen[nt] ? p : 0.0f;
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) w[x] += __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - r.m[nt]) * r.inv[nt];
+      }
+    }
+    const float sum = sums_of_rows(w, lane);
+    if (key < len) a.weight_out[row_of_weights + key] = old + sum;
+    f.here = ahead;
+  }
+}
+
+// The weights of the step by themselves, taken again from the keys and the rows' statistics: every key belongs to one wave, so nothing is added up
+// between workgroups.  16 NT rows at a time; where there are more, the keys are gone through again for them (of a wave's share, one time right
+// after the other).
 template <int NT, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs a) {
   __shared__ f16x8 lds_q[kWaves][NT][4][64];
   __shared__ int lds_i[kWaves + kThreads];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-  const int k_byte = n16 * kHeadDim + g * 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int at, end;
   Shares shares;
   Item it = locate<true, 1>(a, int(blockIdx.x) + wave * int(gridDim.x), int(gridDim.x) * kWaves, 1, lds_i, at, end, shares);
@@ -660,89 +742,33 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
     step_tokens<true>(a.t, s, row0, n);
     const int len = it.len, group = group_size(a.groups, h), rows = n * group;
     pair_units<true, 1>(a, rows, len, tiles, units);
-    const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
-    const int64_t weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
-    const float* before = a.weight_in;
+    const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at)), last = max(min(units, u1) - 1, 0);
     int first_row = 0;
     do {
-      const int groups = min(NT, (rows - first_row + 15) >> 4);   // of sixteen rows
-      Keys kc;
-      Page here = page_at(a.c, page_number(a.c, pair, max(min(u0, u1 - 1), 0)), max(min(u0, u1 - 1), 0));
-      int page_next = page_number(a.c, pair, max(min(u0 + 1, u1 - 1), 0));
-      load_keys<false>(a, here, u0 < u1, k_byte, kc);
-      __builtin_amdgcn_sched_barrier(0);
-      float to_log2[NT], m[NT], inv[NT];
-      int seen[NT];
+      const int groups = min(NT, (rows - first_row + 15) >> 4);  // of sixteen rows
+      Flight f;
+      start<1, false>(a, pair, u0, u1, last, lane, false, f);
+      Statistics<NT> r;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int row = first_row + nt * 16 + n16;
+        const int row = first_row + nt * 16 + (lane & 15);
+        r.to_log2[nt] = r.m[nt] = r.inv[nt] = 0.0f;
+        r.seen[nt] = 0;
+        if (nt >= groups) continue;
         f16x8 q[4];
-        to_log2[nt] = m[nt] = inv[nt] = 0.0f;
-        seen[nt] = 0;
-        if (nt < groups) {
-          to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
+        r.to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) lds_q[wave][nt][e][lane] = q[e];
-          if (row < rows) {
-            const int j = row / group, head = group_head(a.groups, h, row - j * group);
-            const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head));
-            seen[nt] = len - n + 1 + j;
-            m[nt] = st.x;
-            inv[nt] = st.y;
-          }
+        for (int e = 0; e < 4; ++e) lds_q[wave][nt][e][lane] = q[e];
+        if (row < rows) {
+          const int j = row / group, head = group_head(a.groups, h, row - j * group);
+          const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head));
+          r.seen[nt] = len - n + 1 + j;
+          r.m[nt] = st.x;
+          r.inv[nt] = st.y;
         }
       }
-      const int seen_first = len - n + 1 + first_row / max(group, 1);
-      for (int u = u0; u < u1; ++u) {
-        const float k_scale = here.bad ? __uint_as_float(kNanBits) : here.k_scale;
-        const Page ahead = page_at(a.c, page_next, min(u + 1, u1 - 1));
-        page_next = page_number(a.c, pair, min(u + 2, u1 - 1));
-        const int key0 = u * kUnit;
-        // this lane's key, once the sums over the rows are taken
-        const int key = key0 + (n16 >> 2) * 16 + g * 4 + (n16 & 3);
-        float old = 0.0f;
-        if (before != nullptr && key < len) old = before[weights + key];
-        f32x4 sc[NT][4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f16x8 k[4];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) k[t] = key_operand<FMT>(kc.code[t][e >> 1][2 * (e & 1)], kc.code[t][e >> 1][2 * (e & 1) + 1]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (nt > 0 && nt >= groups) break;
-            const f16x8 q = lds_q[wave][nt][e][lane];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-              sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[t], q, e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[nt][t], 0, 0, 0);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        load_keys<false>(a, ahead, u + 1 < u1, k_byte, kc);
-        __builtin_amdgcn_sched_barrier(0);
-        float w[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) w[x] = 0.0f;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (nt >= groups) break;
-          const float c = to_log2[nt] * k_scale;
-          if (key0 + kUnit > seen_first) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              const float p = __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - m[nt]) * inv[nt];
-              w[x] += key0 + (x >> 2) * 16 + g * 4 + (x & 3) < seen[nt] ? p : 0.0f;
-            }
-          } else {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) w[x] += __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - m[nt]) * inv[nt];
-          }
-        }
-        const float sum = sums_of_rows(w, lane);
-        if (key < len) a.weight_out[weights + key] = old + sum;
-        here = ahead;
-      }
-      before = a.weight_out;
+      weigh<NT, 1, FMT>(a, pair, len, u0, u1, last, len - n + 1 + first_row / max(group, 1), groups, lds_q[wave],
+                        first_row == 0 ? a.weight_in : a.weight_out, lane, f, r);
       first_row += 16 * NT;
     } while (first_row < rows);
     at += units - it.unit;
@@ -750,13 +776,86 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
   }
 }
 
+// A head a workgroup, eight waves taking turns at its units: output, denominators and weights in one launch, without partial results.  For
+// up to 16 rows and as many heads as there are compute units, in caches that leave a wave no more than kWholeUnits units.
+constexpr int kWholeWaves = 8, kWholeUnits = 4;
+
+template <int FMT>
+__global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheAttnArgs a) {
+  __shared__ f16x8 lds_q[1][4][64];
+  __shared__ float lds_o[kWholeWaves][16][kLdsRow];
+  __shared__ float lds_m[kWholeWaves][16], lds_l[kWholeWaves][16], lds_ref[16], lds_inv[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, quad = lane >> 4;
+  const int pair = blockIdx.x, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads, len = scalar_load(a.c.lens + pair);
+  const int group = group_size(a.groups, h);
+  int row0, n;
+  step_tokens<true>(a.t, s, row0, n);
+  const bool good = good_length(a.c, len);
+  const int rows = n * group, units = good ? (len + kUnit - 1) / kUnit : 0, last = max(units - 1, 0), seen_before = len - n + 1;
+  if (rows == 0 && a.weight_out == nullptr) return;
+  Flight f;
+  Rows<1> r;
+  start<kWholeWaves, false>(a, pair, wave, units, last, lane, true, f);
+  take_rows<1>(a, row0, n, h, max(group, 1), 0, seen_before, lane, lds_q, r);
+  if (rows > 0) {
+    attend<1, kWholeWaves, false, FMT>(a, pair, len, wave, units, last, seen_before, lds_q, lane, f, r);
+    r.l[0] = quad_sum(r.l[0]);
+    if (quad == 0) {
+      lds_m[wave][n16] = r.m[0];
+      lds_l[wave][n16] = r.l[0];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float* dst = &lds_o[wave][n16][(quad * 4 + i) * 8];
+      *reinterpret_cast<f32x4*>(dst) = f32x4{r.acc[0][0][i], r.acc[0][1][i], r.acc[0][2][i], r.acc[0][3][i]};
+      *reinterpret_cast<f32x4*>(dst + 4) = f32x4{r.acc[0][4][i], r.acc[0][5][i], r.acc[0][6][i], r.acc[0][7][i]};
+    }
+  }
+  if (a.weight_out != nullptr) start<kWholeWaves, false>(a, pair, wave, units, last, lane, false, f);   // the keys again
+  __syncthreads();
+  const int row = tid >> 5, d = (tid & 31) * 4;
+  if (row < rows) {
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWholeWaves; ++w) top = fmaxf(top, lds_m[w][row]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kWholeWaves; ++w) {
+      const float x = __builtin_amdgcn_exp2f(lds_m[w][row] - ref);
+      sum += x * lds_l[w][row];
+      o += x * *reinterpret_cast<const f32x4*>(&lds_o[w][row][d]);
+    }
+    const int j = row / group, head = group_head(a.groups, h, row - j * group);
+    const float inv = !good ? __uint_as_float(kNanBits) : sum == 0.0f ? 0.0f : 1.0f / sum;
+    *reinterpret_cast<u32x2*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d) =
+        u32x2{pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)};
+    if (d == 0) {
+      if (a.lse != nullptr)
+        a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = good ? (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f : inv;
+      lds_ref[row] = ref - kLift;
+      lds_inv[row] = inv;
+    }
+  }
+  if (a.weight_out == nullptr) return;
+  __syncthreads();
+  const bool there = n16 < rows;
+  const Statistics<1> st = {{r.to_log2[0]}, {there ? lds_ref[n16] : 0.0f}, {there ? lds_inv[n16] : 0.0f}, {r.seen[0]}};
+  weigh<1, kWholeWaves, FMT>(a, pair, len, wave, units, last, seen_before, rows > 0 ? 1 : 0, lds_q, a.weight_in, lane, f, st);
+}
+
 template <int FMT>
 int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compute_units, hipStream_t stream) {
-  const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2);
+  const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2), pairs = a.c.n_seq * a.c.n_kv_heads;
+  const int64_t capacity = int64_t(a.c.max_pages) << a.c.block_log2;
+  if (rows == 16 && pairs <= compute_units && capacity <= kWholeWaves * kWholeUnits * kUnit) {
+    cache_whole_kernel<FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
+    return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
+  }
   if (a.t.n_tokens > 0) {
     if (rows == 16) cache_attn_kernel<1, 1, FMT><<<grid, kThreads, 0, stream>>>(a, 1);
     else cache_attn_kernel<2, kWaves, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
-    cache_join_kernel<<<dim3(a.c.n_seq * a.c.n_kv_heads * a.tiles, min(rows, most_rows)), kThreads, 0, stream>>>(a, rows);
+    cache_join_kernel<<<dim3(pairs * a.tiles, min(rows, most_rows)), kThreads, 0, stream>>>(a, rows);
   }
   if (a.weight_out != nullptr) {
     if (rows == 16) cache_weight_kernel<1, FMT><<<grid, kThreads, 0, stream>>>(a);

@@ -172,15 +172,17 @@ def run_attn(c, q, cu, dev, step, weight_in=None, packed=0):
 
 @FORMATS
 @BLOCKS
+@pytest.mark.parametrize("room", [0, 4096], ids=["short", "long"])
 @pytest.mark.parametrize("name", ATTNS)
-def test_attn(name, block, fmt):
+def test_attn(name, room, block, fmt):
+    # room: tokens that the page table has places for; a cache of many is worked on by shares of all heads' keys, one of few head by head
     lens, new, hq, hkv = ATTNS[name]
-    print("case", name, block, fmt, flush=True)
+    print("case", name, room, block, fmt, flush=True)
     rng = np.random.default_rng([block, fmt, len(name)])
     lens = np.repeat(np.array(lens)[:, None], hkv, 1)
     if name in ("ragged", "rows_60"):                    # heads of lengths of their own
         lens = np.maximum(np.minimum(lens, 1), (lens * rng.uniform(0.3, 1, size=lens.shape)).astype(int))
-    c = filled(rng, lens, block, fmt)
+    c = filled(rng, lens, block, fmt, max_pages=room // block or None)
     ragged = len(set(new)) > 1
     behind = 2 if ragged else 0
     q, q64 = bf16(2 * rng.standard_normal((sum(new) + behind, hq, D)))
@@ -228,10 +230,11 @@ def test_attn_many_short_sequences():
     check_attn(c, out, lse, q64, cu, [h // 2 for h in range(12)], got_weight=w_out, weight_in=w)
 
 
-def test_attn_mapped_heads_and_scale():
+@pytest.mark.parametrize("room", [None, 64])
+def test_attn_mapped_heads_and_scale(room):
     rng = np.random.default_rng(7)
     kv_of = [2, 0, 2, 2, 0, 2]                           # the second KV head has no query head
-    c = filled(rng, [[200, 150, 330], [64, 1, 0]], 64, orc.INT8)
+    c = filled(rng, [[200, 150, 330], [64, 1, 0]], 64, orc.INT8, max_pages=room)
     q, q64 = bf16(rng.standard_normal((4, 6, D)))
     dev = Device(c)
     step, cu = step_of(dev, [2, 2], 6, False, kv_head_of=kv_of, softmax_scale=0.03)
@@ -241,10 +244,11 @@ def test_attn_mapped_heads_and_scale():
 
 
 @FORMATS
-def test_attn_of_extreme_sizes(fmt):
+@pytest.mark.parametrize("room", [None, 64])
+def test_attn_of_extreme_sizes(room, fmt):
     # queries and keys of very different size: scales far apart, scores near 0 and in the hundreds, values of 1e30 beside 1e-30
     rng = np.random.default_rng(8)
-    c = state(rng, [[200]] * 4, 64, fmt)
+    c = state(rng, [[200]] * 4, 64, fmt, max_pages=room)
     sizes = np.array([1e-30, 1e-3, 1.0, 1e3])
     k, k64 = bf16((sizes[:, None, None, None] * rng.standard_normal((4, 200, 1, D))).reshape(-1, 1, D))
     per_page = np.exp(rng.uniform(-60, 60, size=(4, 4)))[:, np.arange(200) // 64]
@@ -257,10 +261,11 @@ def test_attn_of_extreme_sizes(fmt):
     check_attn(c, out, lse, q64, cu, [0] * 4)
 
 
-def test_attn_nothing_to_do():
+@pytest.mark.parametrize("room", [None, 64])
+def test_attn_nothing_to_do(room):
     # a step without a token: nothing but the weights, which are copied
     rng = np.random.default_rng(9)
-    c = filled(rng, [[100, 64], [0, 3]], 64, orc.E4M3)
+    c = filled(rng, [[100, 64], [0, 3]], 64, orc.E4M3, max_pages=room)
     dev = Device(c)
     step = S.Step(2, 4, 2, 0, 0)
     w = torch.rand((2, 2, c.capacity), device=DEV)
@@ -358,10 +363,11 @@ def test_evict_inside_one_pool():
 # ---- what should not happen, and what else a program does ---------------------------------------------------------------
 
 
-def test_damaged_pages_lengths_and_offsets():
+@pytest.mark.parametrize("room", [None, 64])
+def test_damaged_pages_lengths_and_offsets(room):
     # pages outside the pool, lengths outside the table, offsets outside the rows: nothing is touched outside, results say NaN
     rng = np.random.default_rng(21)
-    c = filled(rng, [[200, 200], [200, 200], [90, 90]], 64, orc.E4M3)
+    c = filled(rng, [[200, 200], [200, 200], [90, 90]], 64, orc.E4M3, max_pages=room)
     c.table[0, 0, 1], c.table[0, 1, 0], c.table[1, 0, 3] = -7, c.n_pages, 2 ** 31 - 1
     c.lens[1, 1], c.lens[2, 0] = c.capacity + 1, -1
     dev = Device(c)
@@ -430,10 +436,11 @@ def test_pages_far_into_a_pool():
     np.testing.assert_array_equal(back2.double().cpu().numpy(), want[1])
 
 
-def test_shared_pages_and_another_stream():
+@pytest.mark.parametrize("room", [None, 40])
+def test_shared_pages_and_another_stream(room):
     # three sequences read one prefix; on a stream that is not the current one
     rng = np.random.default_rng(23)
-    c = filled(rng, [[256 + 10, 256 + 10]] * 3, 128, orc.INT8)
+    c = filled(rng, [[256 + 10, 256 + 10]] * 3, 128, orc.INT8, max_pages=room)
     c.table[1:, :, :2] = c.table[0, :, :2]
     q, q64 = bf16(rng.standard_normal((3, 8, D)))
     dev = Device(c)
@@ -448,11 +455,12 @@ def test_shared_pages_and_another_stream():
                weight_in=np.zeros(w.shape, np.float32))
 
 
-def test_decoding_step_in_a_hip_graph():
+@pytest.mark.parametrize("room", [None, 40])
+def test_decoding_step_in_a_hip_graph(room):
     # one token of three sequences appended and attended to, captured once and replayed while lengths and inputs change; with eager
     # calls and other use of the workspace in between
     rng = np.random.default_rng(24)
-    c = filled(rng, [[60, 60], [130, 90], [1, 2]], 64, orc.E4M3, spare=2)
+    c = filled(rng, [[60, 60], [130, 90], [1, 2]], 64, orc.E4M3, **(dict(spare=2) if room is None else dict(max_pages=room, spare=2)))
     dev = Device(c)
     hq = 8
     step, cu = step_of(dev, [1] * 3, hq, False)
