@@ -155,25 +155,28 @@ __device__ __forceinline__ Item next_pair(const CacheAttnArgs& a, int pair) {
   return {pair + 1, scalar_load(a.c.lens + min(pair + 1, a.c.n_seq * a.c.n_kv_heads - 1)), 0, -kStart};
 }
 
-// Sixteen query rows as operand: lane n + 16 g holds of row n dims 64 x + 16 g .. + 15, x = 0, 1, eight to a product.  Returns what the products
-// are to be multiplied by (softmax scale * log2(e), less the power of two), and 0 for rows that are not there.
-__device__ __forceinline__ float load_queries(const CacheAttnArgs& a, int row0, int n, int h, int group, int row, f16x8 (&q)[4]) {
-  const int g = (threadIdx.x & 63) >> 4;
-  u32x4 in[4];
+// A query row as a lane has it on the way: lane n + 16 g of row n dims 64 x + 16 g .. + 15, x = 0, 1.
+struct Query {
+  u32x4 part[4];
+};
+// Asks for it; of rows that are not there it is zeros.
+__device__ __forceinline__ void ask_query(const CacheAttnArgs& a, int row0, int n, int h, int group, int row, int lane, Query& q) {
 #pragma unroll
-  for (int x = 0; x < 4; ++x) in[x] = u32x4{0, 0, 0, 0};
-  const bool there = row < n * group;
-  if (there) {
-    const int j = row / group, head = group_head(a.groups, h, row - j * group);
-    const uint16_t* src = a.q + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h;
+  for (int x = 0; x < 4; ++x) q.part[x] = u32x4{0, 0, 0, 0};
+  if (row >= n * group) return;
+  const int j = row / group, head = group_head(a.groups, h, row - j * group);
+  const uint16_t* src = a.q + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + (lane >> 4) * 16;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) in[x] = *reinterpret_cast<const u32x4*>(src + (x >> 1) * 64 + g * 16 + (x & 1) * 8);
-  }
+  for (int x = 0; x < 4; ++x) q.part[x] = *reinterpret_cast<const u32x4*>(src + (x >> 1) * 64 + (x & 1) * 8);
+}
+// ... and makes it four operands, eight dims to a product each.  Returns what the products are to be multiplied by: softmax scale *
+// log2(e), less the power of two that brings the row to fp16.
+__device__ __forceinline__ float query_operands(const CacheAttnArgs& a, const Query& in, f16x8 (&q)[4]) {
   uint32_t top = 0;
 #pragma unroll
   for (int x = 0; x < 4; ++x)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) top = max(top, max(in[x][e] << 16 & 0x7fff0000u, in[x][e] & 0x7fff0000u));
+    for (int e = 0; e < 4; ++e) top = max(top, max(in.part[x][e] << 16 & 0x7fff0000u, in.part[x][e] & 0x7fff0000u));
   top = max(top, uint32_t(__shfl_xor(int(top), 16)));
   top = max(top, uint32_t(__shfl_xor(int(top), 32)));
   const int up = top == 0 ? 0 : min(max(13 - (int(top >> 23) - 127), -120), 100);
@@ -183,12 +186,12 @@ __device__ __forceinline__ float load_queries(const CacheAttnArgs& a, int row0, 
     u32x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const f16x2 two = {(_Float16)(__uint_as_float(in[x][e] << 16) * f), (_Float16)(__uint_as_float(in[x][e] & 0xffff0000u) * f)};
+      const f16x2 two = {(_Float16)(__uint_as_float(in.part[x][e] << 16) * f), (_Float16)(__uint_as_float(in.part[x][e] & 0xffff0000u) * f)};
       o[e] = __builtin_bit_cast(uint32_t, two);
     }
     q[x] = __builtin_bit_cast(f16x8, o);
   }
-  return there ? a.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23) : 0.0f;
+  return a.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
 }
 
 // Eight bytes of a K row as operand.
@@ -272,29 +275,39 @@ struct Flight {
   int page_next;
 };
 
-// Units first, first + STEP .. below end; last: one that can be read in any case.
-template <int STEP, bool ONCE>
-__device__ __forceinline__ void start(const CacheAttnArgs& a, int pair, int first, int end, int last, int lane, bool values, Flight& f) {
+// Asks for unit `first`, if it is below end, whose page's number is `page`.
+template <bool ONCE>
+__device__ __forceinline__ void ask_unit(const CacheAttnArgs& a, int page, int first, int end, int lane, bool values, Flight& f) {
   const int n16 = lane & 15, g = lane >> 4;
-  f.here = page_at(a.c, page_number(a.c, pair, min(first, last)), min(first, last));
-  f.page_next = page_number(a.c, pair, min(first + STEP, last));
+  f.here = page_at(a.c, page, first);
   load_keys<ONCE>(a, f.here, first < end, n16 * kHeadDim + g * 16, f.k);
   if (values) load_values<ONCE>(a, f.here, first < end, g * 4 * kHeadDim + n16 * 8, f.v);
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Queries of the rows from first_row on into LDS, as each lane needs them: what it reads it wrote itself, and they cost no registers.
-template <int NT>
-__device__ __forceinline__ void take_rows(const CacheAttnArgs& a, int row0, int n, int h, int group, int first_row, int seen_before, int lane,
-                                          f16x8 (*lds_q)[4][64], Rows<NT>& r) {
+// What a wave begins with: the rows from first_row on and the first unit of first, first + STEP .. below end (last: a unit whose place in the page
+// table can be read in any case).  Queries are on their way while the page is looked up, and are worked on while its codes are.  They go
+// into LDS, as each lane needs them: what it reads it wrote itself, and they cost no registers.
+template <int NT, int STEP, bool ONCE>
+__device__ __forceinline__ void begin_rows(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int seen_before, int first,
+                                           int end, int last, int lane, f16x8 (*lds_q)[4][64], Flight& f, Rows<NT>& r) {
+  const int page = page_number(a.c, pair, min(first, last));
+  f.page_next = page_number(a.c, pair, min(first + STEP, last));
+  Query q[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) ask_query(a, row0, n, h, group, first_row + nt * 16 + (lane & 15), lane, q[nt]);
+  __builtin_amdgcn_sched_barrier(0);
+  ask_unit<ONCE>(a, page, min(first, last), first < end ? end : 0, lane, true, f);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = first_row + nt * 16 + (lane & 15);
-    f16x8 q[4];
-    r.to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
+    f16x8 operand[4];
+    const float to_log2 = query_operands(a, q[nt], operand);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) lds_q[nt][e][lane] = q[e];
-    r.seen[nt] = row < n * group ? seen_before + row / group : 0;
+    for (int e = 0; e < 4; ++e) lds_q[nt][e][lane] = operand[e];
+    const bool there = row < n * group;
+    r.to_log2[nt] = there ? to_log2 : 0.0f;
+    r.seen[nt] = there ? seen_before + row / group : 0;
     r.m[nt] = -INFINITY;
     r.l[nt] = 0.0f;
 #pragma unroll
@@ -494,8 +507,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     f16x8(*q)[4][64] = lds_q[kOwn ? wave : 0];                   // (waves of one share write the same)
     Flight f;
     Rows<NT> r;
-    start<WAVES, kOwn>(a, pair, u_first, u_end, u1 - 1, lane, true, f);
-    take_rows<NT>(a, row0, n, h, group, first_row, len - n + 1, lane, q, r);
+    begin_rows<NT, WAVES, kOwn>(a, pair, h, group, row0, n, first_row, len - n + 1, u_first, u_end, u1 - 1, lane, q, f, r);
     attend<NT, WAVES, kOwn, FMT>(a, pair, len, u_first, u_end, u1 - 1, len - n + 1 + first_row / group, q, lane, f, r);
 
     int tid = threadIdx.x;
@@ -747,18 +759,16 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
     do {
       const int groups = min(NT, (rows - first_row + 15) >> 4);  // of sixteen rows
       Flight f;
-      start<1, false>(a, pair, u0, u1, last, lane, false, f);
+      const int page = page_number(a.c, pair, min(u0, last));
+      f.page_next = page_number(a.c, pair, min(u0 + 1, last));
       Statistics<NT> r;
+      Query q[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int row = first_row + nt * 16 + (lane & 15);
-        r.to_log2[nt] = r.m[nt] = r.inv[nt] = 0.0f;
+        r.m[nt] = r.inv[nt] = 0.0f;
         r.seen[nt] = 0;
-        if (nt >= groups) continue;
-        f16x8 q[4];
-        r.to_log2[nt] = load_queries(a, row0, n, h, group, row, q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lds_q[wave][nt][e][lane] = q[e];
+        ask_query(a, row0, n, h, group, row, lane, q[nt]);
         if (row < rows) {
           const int j = row / group, head = group_head(a.groups, h, row - j * group);
           const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head));
@@ -766,6 +776,16 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
           r.m[nt] = st.x;
           r.inv[nt] = st.y;
         }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      ask_unit<false>(a, page, min(u0, last), u0 < u1 ? u1 : 0, lane, false, f);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        f16x8 operand[4];
+        const float to_log2 = query_operands(a, q[nt], operand);
+        r.to_log2[nt] = first_row + nt * 16 + (lane & 15) < rows ? to_log2 : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds_q[wave][nt][e][lane] = operand[e];
       }
       weigh<NT, 1, FMT>(a, pair, len, u0, u1, last, len - n + 1 + first_row / max(group, 1), groups, lds_q[wave],
                         first_row == 0 ? a.weight_in : a.weight_out, lane, f, r);
@@ -791,12 +811,13 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
   int row0, n;
   step_tokens<true>(a.t, s, row0, n);
   const bool good = good_length(a.c, len);
-  const int rows = n * group, units = good ? (len + kUnit - 1) / kUnit : 0, last = max(units - 1, 0), seen_before = len - n + 1;
+  // (the page table is read up to its end: what is looked up does not wait for the length)
+  const int rows = n * group, units = good ? (len + kUnit - 1) / kUnit : 0, last = ((a.c.max_pages << a.c.block_log2) / kUnit) - 1, seen_before = len - n + 1;
   if (rows == 0 && a.weight_out == nullptr) return;
   Flight f;
   Rows<1> r;
-  start<kWholeWaves, false>(a, pair, wave, units, last, lane, true, f);
-  take_rows<1>(a, row0, n, h, max(group, 1), 0, seen_before, lane, lds_q, r);
+  const int page = page_number(a.c, pair, min(wave, last)), page_next = page_number(a.c, pair, min(wave + kWholeWaves, last));
+  begin_rows<1, kWholeWaves, false>(a, pair, h, max(group, 1), row0, n, 0, seen_before, wave, units, last, lane, lds_q, f, r);
   if (rows > 0) {
     attend<1, kWholeWaves, false, FMT>(a, pair, len, wave, units, last, seen_before, lds_q, lane, f, r);
     r.l[0] = quad_sum(r.l[0]);
@@ -811,7 +832,10 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
       *reinterpret_cast<f32x4*>(dst + 4) = f32x4{r.acc[0][4][i], r.acc[0][5][i], r.acc[0][6][i], r.acc[0][7][i]};
     }
   }
-  if (a.weight_out != nullptr) start<kWholeWaves, false>(a, pair, wave, units, last, lane, false, f);   // the keys again
+  if (a.weight_out != nullptr) {                                 // the keys again
+    f.page_next = page_next;
+    ask_unit<false>(a, page, min(wave, last), wave < units ? units : 0, lane, false, f);
+  }
   __syncthreads();
   const int row = tid >> 5, d = (tid & 31) * 4;
   if (row < rows) {
