@@ -546,10 +546,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
             *reinterpret_cast<f32x4*>(dst + i * 8) = f32x4{r.acc[nt][0][i], r.acc[nt][1][i], r.acc[nt][2][i], r.acc[nt][3][i]};
             *reinterpret_cast<f32x4*>(dst + i * 8 + 4) = f32x4{r.acc[nt][4][i], r.acc[nt][5][i], r.acc[nt][6][i], r.acc[nt][7][i]};
           }
-          if (quad == 0) {
-            a.part_ml[slot_row * 2 + in_tile] = r.m[nt];
-            a.part_ml[slot_row * 2 + kRows + in_tile] = r.l[nt];
-          }
+          if (quad == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * (slot_row + in_tile)) = f32x2{r.m[nt], r.l[nt]};
         }
       }
     } else {
@@ -594,10 +591,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
             float* dst = a.part_o + (slot_row + in_tile) * kHeadDim + d;
             *reinterpret_cast<f32x4*>(dst) = o0;
             *reinterpret_cast<f32x4*>(dst + 4) = o1;
-            if (d == 0) {
-              a.part_ml[slot_row * 2 + in_tile] = top;
-              a.part_ml[slot_row * 2 + kRows + in_tile] = sum;
-            }
+            if (d == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * (slot_row + in_tile)) = f32x2{top, sum};
           }
         }
       }
@@ -612,11 +606,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
 }
 
 // Joins the pieces of one row of an item: with M the largest m, out = sum 2^(m - M) O / sum 2^(m - M) l.  A workgroup a row (y) of an
-// item (x).  The first piece lies in slot 2 w + 1 of the share w it begins in, the others in 2 (w + 1), 2 (w + 2) ...; eight groups of
-// 32 lanes take every eighth piece, a lane four dims, and what they have is added up in order.  What the first pieces hold is asked for
+// item (x).  The first piece lies in slot 2 w + 1 of the share w it begins in, the others in 2 (w + 1), 2 (w + 2) ...; groups of
+// 32 lanes take turns at the pieces, a lane four dims, and what they have is added up in order.  What the first pieces hold is asked for
 // together with the statistics.
-__global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a, int rows_per_tile) {
-  __shared__ f32x4 lds_o[8][32];
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void cache_join_kernel(CacheAttnArgs a, int rows_per_tile) {
+  constexpr int kGroups = THREADS / 32;
+  constexpr bool kShared = THREADS > 64;       // each piece's statistics are read by one thread and shared
+  __shared__ float lds_m[kShared ? kCacheMaxWorkers : 1], lds_l[kShared ? kCacheMaxWorkers : 1];
+  __shared__ f32x4 lds_o[kGroups][32];
   const int tid = threadIdx.x, lane = tid & 63, d4 = tid & 31, part = tid >> 5;
   const int pair = blockIdx.x / uint32_t(a.tiles), tile = blockIdx.x - pair * a.tiles, in_tile = blockIdx.y, row = tile * rows_per_tile + in_tile;
   const int2 begun = *reinterpret_cast<const int2*>(a.begun + 2 * int64_t(blockIdx.x));
@@ -627,41 +625,58 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(CacheAttnArgs a, i
   const int w = begun.x, pieces = begun.y;
   if (pieces == 0) return;                                       // it was whole
   const auto slot = [&](int x) { return 2 * int64_t(w + x) + (x == 0); };
-  const auto stats = [&](int x) { return a.part_ml + slot(x) * 2 * rows_per_tile + in_tile; };
+  const auto stats = [&](int x) { return *reinterpret_cast<const f32x2*>(a.part_ml + 2 * (slot(x) * rows_per_tile + in_tile)); };
   const auto values = [&](int x) { return *reinterpret_cast<const f32x4*>(a.part_o + (slot(x) * rows_per_tile + in_tile) * kHeadDim + d4 * 4); };
   constexpr int kEarly = 4;
   f32x4 early[kEarly];
-  float early_m[kEarly];
 #pragma unroll
-  for (int x = 0; x < kEarly; ++x) {
-    early[x] = part + 8 * x < pieces ? values(part + 8 * x) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    early_m[x] = part + 8 * x < pieces ? *stats(part + 8 * x) : -INFINITY;
+  for (int x = 0; x < kEarly; ++x) early[x] = part + kGroups * x < pieces ? values(part + kGroups * x) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float early_m[kEarly];
+  f32x2 mine = {-INFINITY, 0.0f};
+  if (!kShared) {
+#pragma unroll
+    for (int x = 0; x < kEarly; ++x) early_m[x] = part + kGroups * x < pieces ? stats(part + kGroups * x).x : -INFINITY;
+    if (lane < pieces) mine = stats(lane);
+  } else {
+    for (int x = tid; x < pieces; x += THREADS) {
+      const f32x2 ml = stats(x);
+      lds_m[x] = ml.x;
+      lds_l[x] = ml.y;
+    }
+    __syncthreads();
   }
+  const auto m = [&](int x) { return kShared ? lds_m[x] : stats(x).x; };
   // every wave by itself, in the same order
-  float m = -INFINITY, l = 0.0f;
-  if (lane < pieces) {
-    m = stats(lane)[0];
-    l = stats(lane)[rows_per_tile];
-  }
-  float top = m;
-  for (int x = lane + 64; x < pieces; x += 64) top = fmaxf(top, *stats(x));
+  if (kShared && lane < pieces) mine = f32x2{lds_m[lane], lds_l[lane]};
+  float top = mine.x;
+  for (int x = lane + 64; x < pieces; x += 64) top = fmaxf(top, m(x));
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float ref = top == -INFINITY ? 0.0f : top;
-  float sum = __builtin_amdgcn_exp2f(m - ref) * l;
-  for (int x = lane + 64; x < pieces; x += 64) sum += __builtin_amdgcn_exp2f(*stats(x) - ref) * stats(x)[rows_per_tile];
+  float sum = __builtin_amdgcn_exp2f(mine.x - ref) * mine.y;
+  for (int x = lane + 64; x < pieces; x += 64) sum += __builtin_amdgcn_exp2f(m(x) - ref) * (kShared ? lds_l[x] : stats(x).y);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int x = 0; x < kEarly; ++x) o += __builtin_amdgcn_exp2f(early_m[x] - ref) * early[x];
+  for (int x = 0; x < kEarly; ++x)
+    if (part + kGroups * x < pieces) o += __builtin_amdgcn_exp2f((kShared ? lds_m[part + kGroups * x] : early_m[x]) - ref) * early[x];
 #pragma unroll 8
-  for (int x = part + 8 * kEarly; x < pieces; x += 8) o += __builtin_amdgcn_exp2f(*stats(x) - ref) * values(x);
+  for (int x = part + kGroups * kEarly; x < pieces; x += kGroups) o += __builtin_amdgcn_exp2f(m(x) - ref) * values(x);
   lds_o[part][d4] = o;
   __syncthreads();
+  if constexpr (kGroups > 8) {
+    if (part < 4) {
+#pragma unroll
+      for (int x = 1; x < kGroups / 4; ++x) o += lds_o[part + 4 * x][d4];
+    }
+    __syncthreads();
+    if (part < 4) lds_o[part][d4] = o;
+    __syncthreads();
+  }
   if (tid >= 32) return;
 #pragma unroll
-  for (int x = 1; x < 8; ++x) o += lds_o[x][d4];
+  for (int x = 1; x < min(kGroups, kGroups > 8 ? 4 : 8); ++x) o += lds_o[x][d4];
   const int j = row / group, head = group_head(a.groups, h, row - j * group);
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   *reinterpret_cast<u32x2*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d4 * 4) =
@@ -879,7 +894,12 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
   if (a.t.n_tokens > 0) {
     if (rows == 16) cache_attn_kernel<1, 1, FMT><<<grid, kThreads, 0, stream>>>(a, 1);
     else cache_attn_kernel<2, kWaves, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
-    cache_join_kernel<<<dim3(pairs * a.tiles, min(rows, most_rows)), kThreads, 0, stream>>>(a, rows);
+    // few rows are of many pieces, many of few: 32 rows of 256 pieces (131072 tokens x 8 heads) take 6.6 us with 1024 threads each, 9 with 256; 4096 rows
+    // of one to four 5.4 with 64, 7 with 256
+    const dim3 all(pairs * a.tiles, min(rows, most_rows));
+    if (int64_t(all.x) * all.y <= 256) cache_join_kernel<1024><<<all, 1024, 0, stream>>>(a, rows);
+    else if (int64_t(all.x) * all.y < 2048) cache_join_kernel<256><<<all, 256, 0, stream>>>(a, rows);
+    else cache_join_kernel<64><<<all, 64, 0, stream>>>(a, rows);
   }
   if (a.weight_out != nullptr) {
     if (rows == 16) cache_weight_kernel<1, FMT><<<grid, kThreads, 0, stream>>>(a);

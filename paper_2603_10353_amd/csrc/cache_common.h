@@ -51,7 +51,7 @@ struct CacheAttnArgs {
   const float* weight_in;          // or null
   float* weight_out;               // or null
   // workspace
-  float *part_o, *part_ml;         // partial results: [2 shares][rows][128], [2 shares][2][rows]
+  float *part_o, *part_ml;         // partial results: [2 shares][rows][128], [2 shares][rows][2]
   int32_t* begun;                  // [sequences x KV heads][tiles][2]: the share that a tile of rows begins in, its pieces (0: it is whole)
   float* stats;                    // [n_tokens][n_q_heads][2]: reference exponent and 1 / denominator, for the weights
 };
