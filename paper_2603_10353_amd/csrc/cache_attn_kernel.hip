@@ -29,22 +29,35 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kUnit = 64;
 // What beginning with an item costs, in units of the list of all units (where it is that many empty ones in front of the item's own):
-// the queries, the first keys, the results, all of them waited for.  For a batch of 128 sequences x 8 heads of lengths between 100 and
-// 16000, where a wave has one to five items, 102 us without, 97 with two, 100 with five.
-constexpr int kStart = 2;
+// the queries, the first keys, the results, all of them waited for.  A wave by itself: for a batch of 128 sequences x 8 heads of lengths
+// between 100 and 16000, where it has one to five items, 102 us without, 97 with two, 100 with five.  Four waves together, which
+// have a unit's work done in a quarter of the time: for 100 sequences x 2 heads of 128 rows and up to a few hundred tokens 44 us with
+// two, 34 with eight, 42 with sixteen; for 128 rows x 8 heads x 32768 tokens 53 with two, 51 from four on.
+constexpr int start_units(int waves) { return waves == 1 ? 2 : 8; }
 constexpr float kLift = 7.0f;                  // log2 of what probabilities are multiplied by, beside their reference ...
 constexpr float kHeadroom = 8.0f;              // ... and how far, in the exponent, they may be above it: 2^15 in fp16
 constexpr int kLdsRow = kHeadDim + 4;          // floats of a row in LDS: rows four banks apart
 
 struct Item {                                  // a place in the list of units
   int pair, len;                               // the head, and its length
-  int tile, unit;                              // tile of rows, unit inside it; from -kStart on, where there are none yet
+  int tile, unit;                              // tile of rows, unit inside it; below 0 the beginning
 };
-// How the list is divided: the first `more` shares have one unit more than the others.
+// How the list is divided: `each` units a share, and `more` of the shares one more.  Those of waves by themselves: the first ones.  Those of
+// workgroups: evenly among the others, or shares and items of equal lengths drift apart, and more shares have the end of one item and the
+// beginning of another (128 rows x 8 heads x 32768 tokens, eight units a beginning: 51 us, 56 with the first ones; the larger number of shares of
+// waves has less of it, and some power of two apart the longer ones meet on one compute unit: weights of those rows 31 us, 33 evenly).
+template <bool EVENLY>
 struct Shares {
-  int each, more;
-  __device__ int begin(int w) const { return w * each + min(w, more); }
-  __device__ int of(int at) const { return at < more * (each + 1) ? at / (each + 1) : more + (at - more * (each + 1)) / each; }
+  int each, more, n;                           // n: of shares, at most kCacheMaxWorkers; more is less
+  __device__ int begin(int w) const { return w * each + (EVENLY ? int(uint32_t(w * more) / uint32_t(n)) : min(w, more)); }
+  // the share that unit `at` of the list is in
+  __device__ int of(int at) const {
+    if (!EVENLY) return at < more * (each + 1) ? at / (each + 1) : more + (at - more * (each + 1)) / each;
+    int w = min(int(float(at) / (float(each) + float(more) / float(n))), n - 1);       // a near guess: less than one off
+    while (begin(w) > at) --w;
+    while (begin(w + 1) <= at) ++w;
+    return w;
+  }
 };
 
 __device__ __forceinline__ int group_size(const HeadGroups& g, int h) { return g.mapped ? g.begin[h + 1] - g.begin[h] : g.group; }
@@ -85,8 +98,8 @@ __device__ __forceinline__ int lane_sums(int x) {
 // The place where a worker's share [begin, end) of all units begins.  Up to 512 pairs every wave adds them up by itself, a lane a run of
 // them; beyond, the four waves do it together, and each looks for its place in the run where it lies, 64 pairs at a time.  (All
 // units are below 2^30: the entry point sees to that.)
-template <bool WEIGHTS, int ROWS>
-__device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int* lds, int& begin, int& end, Shares& shares) {
+template <bool WEIGHTS, int ROWS, int START, class SHARES>
+__device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int* lds, int& begin, int& end, SHARES& shares) {
   const int pairs = a.c.n_seq * a.c.n_kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool together = pairs > 512;
   const int me = together ? threadIdx.x : lane, each = together ? (pairs + kThreads - 1) / kThreads : (pairs + 63) / 64;
@@ -96,7 +109,7 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
   for (int p = first; p < last; ++p) {
     len = a.c.lens[p];
     pair_units<WEIGHTS, ROWS>(a, pair_rows<false>(a, p), len, tiles, units);
-    mine += tiles * (units + kStart);
+    mine += tiles * (units + START);
   }
   int sum = lane_sums(mine);
   int total = __builtin_amdgcn_readlane(sum, 63);
@@ -114,6 +127,7 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
   if (total < workers * least) workers = max((total + least - 1) / least, 1);
   shares.each = total / workers;
   shares.more = total - shares.each * workers;
+  shares.n = workers;
   begin = worker < workers ? shares.begin(worker) : total;
   end = worker < workers ? shares.begin(worker + 1) : total;
   if (begin >= end) return {0, 0, 0, 0};
@@ -124,8 +138,8 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
       for (;; ++p) {
         len = a.c.lens[p];
         pair_units<WEIGHTS, ROWS>(a, pair_rows<false>(a, p), len, tiles, units);
-        if (left < tiles * (units + kStart)) break;
-        left -= tiles * (units + kStart);
+        if (left < tiles * (units + START)) break;
+        left -= tiles * (units + START);
       }
   } else {
     int run = 0;                                                 // runs that end before the share begins
@@ -136,7 +150,7 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
       len = p < pairs ? a.c.lens[p] : 0;
       tiles = units = 0;
       if (p < pairs) pair_units<WEIGHTS, ROWS>(a, pair_rows<false>(a, p), len, tiles, units);
-      mine = tiles * (units + kStart);
+      mine = tiles * (units + START);
       sum = before + lane_sums(mine);
       left = begin - (sum - mine);
       here = left >= 0 && left < mine;
@@ -144,15 +158,31 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
       before = __builtin_amdgcn_readlane(sum, 63);
     }
   }
-  const int tile = tiles <= 1 ? 0 : left / (units + kStart), unit = left - tile * (units + kStart) - kStart;
+  const int tile = tiles <= 1 ? 0 : left / (units + START), unit = left - tile * (units + START) - START;
   const uint64_t who = __ballot(here);
   const int from = who ? __builtin_ctzll(who) : 0;
   return {__builtin_amdgcn_readlane(p, from), __builtin_amdgcn_readlane(len, from), __builtin_amdgcn_readlane(tile, from),
           __builtin_amdgcn_readlane(unit, from)};
 }
-// The beginning of the next pair (which may be none: the caller's share has ended then).
+// The beginning of the next pair (the last one's again where there is none: the caller's share has ended then).
+template <int START>
 __device__ __forceinline__ Item next_pair(const CacheAttnArgs& a, int pair) {
-  return {pair + 1, scalar_load(a.c.lens + min(pair + 1, a.c.n_seq * a.c.n_kv_heads - 1)), 0, -kStart};
+  const int next = min(pair + 1, a.c.n_seq * a.c.n_kv_heads - 1);
+  return {next, scalar_load(a.c.lens + next), 0, -START};
+}
+// The beginning of the next sequence after s that has tokens in this step, 64 looked at together: a batch may have many that have none.
+template <int START>
+__device__ __forceinline__ bool next_sequence(const CacheAttnArgs& a, int s, int lane, Item& it) {
+  for (int s0 = s + 1; s0 < a.c.n_seq; s0 += 64) {
+    int row0, n;
+    step_tokens<false>(a.t, min(s0 + lane, a.c.n_seq - 1), row0, n);
+    const uint64_t found = __ballot(n > 0);
+    if (found == 0) continue;
+    const int pair = min(s0 + int(__builtin_ctzll(found)), a.c.n_seq - 1) * a.c.n_kv_heads;
+    it = {pair, scalar_load(a.c.lens + pair), 0, -START};
+    return true;
+  }
+  return false;
 }
 
 // A query row as a lane has it on the way: lane n + 16 g of row n dims 64 x + 16 g .. + 15, x = 0, 1.
@@ -474,7 +504,7 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
 template <int NT, int WAVES, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a, int least) {
   constexpr bool kOwn = WAVES == 1;
-  constexpr int kRows = 16 * NT;
+  constexpr int kRows = 16 * NT, kStart = start_units(WAVES);
   static_assert(kOwn || WAVES == kWaves, "one, or all of a workgroup");
   __shared__ f16x8 lds_q[kOwn ? kWaves : 1][NT][4][64];
   __shared__ float lds_o[WAVES][16][kLdsRow];
@@ -482,10 +512,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
   __shared__ int lds_i[kWaves + kThreads];
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   int at, end;
-  Shares shares;
+  Shares<!kOwn> shares;
   // neighbouring shares in different workgroups, on different compute units
   const int worker = kOwn ? int(blockIdx.x) + wave * int(gridDim.x) : int(blockIdx.x);
-  Item it = locate<false, kRows>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, lds_i, at, end, shares);
+  Item it = locate<false, kRows, kStart>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, lds_i, at, end, shares);
   while (at < end) {
     // (the lane as a number of which the compiler knows nothing: what follows from it is worked out here and again at the item's end, and
     // takes no registers in between)
@@ -497,7 +527,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     const int len = it.len, group = group_size(a.groups, h);
     pair_units<false, kRows>(a, n * group, len, tiles, units);
     if (tiles == 0) {
-      it = next_pair(a, pair);
+      if (n > 0) it = next_pair<kStart>(a, pair);               // no query heads of this KV head
+      else if (!next_sequence<kStart>(a, s, lane, it)) break;
       continue;
     }
     const bool good = good_length(a.c, len);
@@ -601,7 +632,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
       *reinterpret_cast<int2*>(a.begun + 2 * (int64_t(pair) * a.tiles + it.tile)) = int2{worker, whole ? 0 : shares.of(at - it.unit + units - 1) - worker + 1};
     at += u1 - it.unit;
     it.unit = -kStart;
-    if (++it.tile == tiles) it = next_pair(a, pair);
+    if (++it.tile == tiles) it = next_pair<kStart>(a, pair);
   }
 }
 
@@ -757,12 +788,13 @@ __device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len,
 // after the other).
 template <int NT, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs a) {
+  constexpr int kStart = start_units(1);
   __shared__ f16x8 lds_q[kWaves][NT][4][64];
   __shared__ int lds_i[kWaves + kThreads];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int at, end;
-  Shares shares;
-  Item it = locate<true, 1>(a, int(blockIdx.x) + wave * int(gridDim.x), int(gridDim.x) * kWaves, 1, lds_i, at, end, shares);
+  Shares<false> shares;
+  Item it = locate<true, 1, kStart>(a, int(blockIdx.x) + wave * int(gridDim.x), int(gridDim.x) * kWaves, 1, lds_i, at, end, shares);
   while (at < end) {
     const int pair = it.pair, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads;
     int row0, n, tiles, units;
@@ -807,7 +839,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
       first_row += 16 * NT;
     } while (first_row < rows);
     at += units - it.unit;
-    it = next_pair(a, pair);
+    it = next_pair<kStart>(a, pair);
   }
 }
 

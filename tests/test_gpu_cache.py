@@ -230,6 +230,47 @@ def test_attn_many_short_sequences():
     check_attn(c, out, lse, q64, cu, [h // 2 for h in range(12)], got_weight=w_out, weight_in=w)
 
 
+@FORMATS
+@pytest.mark.parametrize("tokens", [2, 11])
+def test_attn_few_of_many_sequences(tokens, fmt):
+    # 700 sequences of which seven have tokens in this step, the first and the last among them, and a KV head without query heads
+    rng = np.random.default_rng([tokens, fmt])
+    new = np.zeros(700, int)
+    new[[0, 1, 63, 64, 65, 400, 699]] = tokens
+    lens = rng.integers(0, 150, size=(700, 3))
+    c = filled(rng, lens, 64, fmt)
+    kv_of = [2, 0, 2]
+    q, q64 = bf16(rng.standard_normal((int(new.sum()), 3, D)))
+    dev = Device(c)
+    step, cu = step_of(dev, new, 3, True, kv_head_of=kv_of)
+    w = rng.random((700, 3, c.capacity)).astype(np.float32)
+    out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+    check_attn(c, out, lse, q64, cu, kv_of, got_weight=w_out, weight_in=w)
+
+
+@FORMATS
+@pytest.mark.parametrize("room", [1, 64], ids=["short", "long"])
+def test_attn_one_token_of_every_scale(room, fmt):
+    # a head of one token: its output is that token's value, whatever the page's scale is.  (The probability is within 2^-20 of one, and the value a bf16
+    # number: half a step, 2^-9 of it, away from rounding to another.)
+    rng = np.random.default_rng(fmt)
+    scales = 2.0 ** np.arange(-110, 101)
+    c = state(rng, np.ones((scales.size, 1), int), 64, fmt, spare=0, max_pages=room)
+    c.k_scale[:] = 2.0 ** -6
+    c.k_pages[:] = orc.encode(rng.standard_normal(c.k_pages.shape), fmt)
+    most = orc.LARGEST[fmt]
+    c.v_pages[c.table[:, 0, 0], 0] = orc.encode(rng.uniform(-most, most, size=(scales.size, D)), fmt)
+    c.v_scale[c.table[:, 0, 0]] = scales
+    q, _ = bf16(rng.standard_normal((scales.size, 2, D)))
+    dev = Device(c)
+    step, cu = step_of(dev, np.ones(scales.size, int), 2, False)
+    w = np.zeros((scales.size, 1, c.capacity), np.float32)
+    out, _, w_out = run_attn(c, q, cu, dev, step, w)
+    want = np.stack([c.values("v", s, 0, 1)[0] for s in range(scales.size)])
+    np.testing.assert_array_equal(out, np.stack([want, want], 1))
+    assert (np.abs(w_out[:, 0, 0] - 2) <= 2 * 2.0 ** -20).all()
+
+
 @pytest.mark.parametrize("room", [None, 64])
 def test_attn_mapped_heads_and_scale(room):
     rng = np.random.default_rng(7)
@@ -336,6 +377,18 @@ def test_evict_long_head():
     rng = np.random.default_rng(4)
     evict_case(rng, [[70001, 2000, 64]], [[9000, 1999, 1]], 128, 128, 128, 128, orc.INT8, 80)
     evict_case(rng, [[70001, 2000, 64]], [[9000, 1999, 1]], 128, 128, 128, 128, orc.E4M3, 80, "ties")
+
+
+# tokens of three heads: where one workgroup still sees all of a head's weights, and where parts of 8192 are counted by themselves
+EVICTS = {"one_part": [5000, 8000, 2049], "whole_part": [8064, 3, 8000], "parts": [16385, 8193, 8192], "last_of_a_part": [24448, 16384, 0]}
+
+
+@pytest.mark.parametrize("kind", ["heavy", "ties", "zeros"])
+@pytest.mark.parametrize("sink,recent", [(3, 40), (8200, 150), (100, 8200)])
+@pytest.mark.parametrize("name", EVICTS)
+def test_evict_parts(name, sink, recent, kind):
+    rng = np.random.default_rng([len(name), sink, len(kind)])
+    evict_case(rng, [EVICTS[name]], [[1500, 8300, 8192]], sink, recent, 128, 64, orc.E4M3, 150, kind)
 
 
 def test_evict_inside_one_pool():
@@ -501,6 +554,69 @@ def test_decoding_step_in_a_hip_graph(room):
         check_attn(c, out.double().cpu().numpy(), lse.double().cpu().numpy(), q64, cu, kv_of, got_weight=w.double().cpu().numpy(),
                    weight_in=w64)
         w64 = w.double().cpu().numpy()
+
+
+@FORMATS
+def test_two_graphs_of_one_workspace(fmt):
+    # a decoding step and a prompt's window with the eviction behind it, captured each, share one workspace and take turns, with the
+    # program's own calls in between; every replay leaves what the same calls leave outside of a graph
+    rng = np.random.default_rng([25, fmt])
+    hq, hkv, n = 8, 2, 9
+    c = filled(rng, [[3000, 2500], [400, 900], [64, 1]], 64, fmt, spare=2)
+    to = state(rng, np.full((3, hkv), 640), 64, fmt, spare=0)
+    dev, dto = Device(c), Device(to)
+    one, _ = step_of(dev, [1] * 3, hq, False)
+    many, _ = step_of(dev, [n] * 3, hq, False)
+    new = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16, device=DEV)
+    k, v, q1, o1 = new(3, hkv, D), new(3, hkv, D), new(3, hq, D), new(3, hq, D)
+    q2, o2, back_k, back_v = new(3 * n, hq, D), new(3 * n, hq, D), new(3 * n, hkv, D), new(3 * n, hkv, D)
+    w1, w2 = (torch.zeros((3, hkv, c.capacity), device=DEV) for _ in "12")
+    lse = torch.zeros((hq, 3 * n), device=DEV)
+    keep = torch.full((3, hkv), 500, dtype=torch.int32, device=DEV)
+    w_kept = torch.zeros((3, hkv, to.capacity), device=DEV)
+    kept = torch.zeros((3, hkv, to.capacity), dtype=torch.int32, device=DEV)
+    ws = torch.empty(max(S.shplb_cache_attn_workspace_bytes(dev.cache, one), S.shplb_cache_attn_workspace_bytes(dev.cache, many),
+                         S.shplb_cache_evict_workspace_bytes(dev.cache)), dtype=torch.uint8, device=DEV)
+
+    def decode(st):
+        S.shplb_cache_append(dev.cache, one, k, v, st)
+        S.shplb_cache_attn(dev.cache, one, q1, o1, None, None, w1, ws, st)
+
+    def window(st):
+        S.shplb_cache_attn(dev.cache, many, q2, o2, lse, None, w2, ws, st)
+        S.shplb_cache_evict(dev.cache, w2, keep, 4, n, dto.cache, w_kept, kept, ws, st)
+        S.shplb_cache_load(dev.cache, many, back_k, back_v, st)
+
+    results = [dev.k_pages, dev.v_pages, dev.k_scale, dev.v_scale, o1, w1, o2, lse, w2, dto.k_pages, dto.v_pages, dto.k_scale, dto.v_scale,
+               dto.lens, w_kept, kept, back_k, back_v]
+    side = torch.cuda.Stream()
+    side.wait_stream(stream())
+    graphs = []
+    for f in (decode, window):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.stream(side):
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graphs[-1], stream=side):
+                f(side)
+    torch.cuda.synchronize()
+    for t in range(5):
+        for x in (k, v, q1, q2):
+            x.copy_(torch.from_numpy(rng.standard_normal(tuple(x.shape))))
+        dev.lens += 1
+        ws.random_(0, 255)
+        before = [x.clone() for x in results]
+        torch.cuda.synchronize()
+        for g in graphs if t % 2 == 0 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in results]
+        for x, y in zip(results, before):                # (the window may have looked at a token that is not there yet)
+            x.copy_(y)
+        for f in (decode, window) if t % 2 == 0 else (window, decode):
+            f(stream())
+        torch.cuda.synchronize()
+        for x, y in zip(got, results):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
 def test_prompt_window_eviction_and_steps():
