@@ -296,7 +296,11 @@ SHPLB_API int32_t shplb_token_recovery_heads(const shplb_problem* p, const float
  *     read or written there, what is computed from it is NaN.  A length below 0 or above
  *     max_pages * block: the head's outputs are NaN, nothing is written into it, read out of
  *     it or counted for it, and eviction hands it on as length -1.
- *   - Pages may be shared (a common prefix) by heads that only read them. */
+ *   - Pages may be shared (a common prefix) by heads that only read them.
+ * Errors of all calls: SHPLB_E_NULL, SHPLB_E_SHAPE (sizes below those below, strides that are no multiple of 8 or smaller than what they
+ * hold, pointers not aligned to their elements, of tensors and pages to 16 bytes), SHPLB_E_UNSUPPORTED (more than stands below, element strides
+ * from 2^24 on, 2^23 pages or more that a call may touch, in attention 2^24 rows of a KV head, 2^26 tiles of 32 rows or
+ * 2^30 - 8 tiles units of 64 tokens, of page tables' capacity, for all tiles). */
 #define SHPLB_CACHE_E4M3 0
 #define SHPLB_CACHE_INT8 1
 
@@ -350,8 +354,9 @@ SHPLB_API int32_t shplb_cache_load(const shplb_cache* cache, const shplb_step* s
  * the j-th of a sequence's n queries sees the head's first lens - n + 1 + j tokens, the
  * last one all of them.  Products of bf16 queries and 8-bit codes are exact, sums,
  * softmax and its statistics fp32, probabilities are rounded to fp16 before they meet the
- * values.  A query that sees no token has the output 0 and the denominator's logarithm -inf.
- *   q: device bf16 [n_tokens, n_q_heads, 128]; out: likewise, strides as Q.
+ * values.  (Sums are taken at 2^7 times their size or more: values whose magnitude times the head's tokens is beyond 2^112 may
+ * come out as infinity.)  A query that sees no token has the output 0 and the denominator's logarithm -inf.
+ *   q: device bf16 [n_tokens, n_q_heads, 128]; out: likewise, strides as Q, in other memory.
  *   lse_out: device fp32 [n_q_heads, n_tokens], natural logarithm of the softmax denominators, or NULL.
  *   weight_in, weight_out: device fp32 [n_seq][n_kv_heads][max_pages * block]:
  *     weight_out[s][h][t] = weight_in[s][h][t] + the attention weights that all rows of the

@@ -29,7 +29,7 @@ int32_t check_step(const shplb_cache* c, const shplb_step* t, int32_t n_heads, i
   if (!t) return SHPLB_E_NULL;
   if (t->n_tokens < 0 || t->max_tokens < 0 || misaligned(t->cu_tokens, 4)) return SHPLB_E_SHAPE;
   if (!t->cu_tokens && int64_t(c->n_seq) * t->max_tokens != t->n_tokens) return SHPLB_E_SHAPE;
-  if (stride_h < kHeadDim || stride_t < stride_h * n_heads || (stride_t | stride_h) & 7) return SHPLB_E_SHAPE;
+  if (stride_h < kHeadDim || stride_t < stride_h || stride_t / n_heads < stride_h || (stride_t | stride_h) & 7) return SHPLB_E_SHAPE;
   if (stride_t >= int64_t(1) << 24) return SHPLB_E_UNSUPPORTED;
   *a = StepArgs{t->n_tokens, t->max_tokens, t->cu_tokens, stride_t, stride_h};
   return SHPLB_OK;
@@ -61,10 +61,10 @@ int32_t check_queries(const shplb_cache* c, const shplb_step* t, HeadGroups* g, 
   }
   *most_rows = int64_t(most) * t->max_tokens;
   if (t->n_q_heads > SHPLB_MAX_SEQ_HEADS || *most_rows > (1 << 24)) return SHPLB_E_UNSUPPORTED;
-  // places in the list of all units of 64 keys are 32-bit numbers
+  // places in the list of all units are 32-bit numbers, and a grid has one workgroup of 64 threads for every row of a tile
   const int rows = cache_attn_rows(*most_rows);
-  const int64_t tiles = *most_rows > rows ? (*most_rows + rows - 1) / rows : 1;
-  if (int64_t(c->n_seq) * c->n_kv_heads * (int64_t(c->max_pages) * c->block / 64) * tiles >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
+  const int64_t tiles = *most_rows > rows ? (*most_rows + rows - 1) / rows : 1, items = int64_t(c->n_seq) * c->n_kv_heads * tiles;
+  if (items >= int64_t(1) << 26 || items * (int64_t(c->max_pages) * c->block / 64 + kCacheMostStart) >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
   return SHPLB_OK;
 }
 
@@ -139,7 +139,7 @@ int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const
   if (weight_in && !weight_out) return SHPLB_E_NULL;
   if (a.t.n_tokens == 0 && !weight_out) return SHPLB_OK;
   if ((a.t.n_tokens > 0 && (!q || !out)) || !workspace) return SHPLB_E_NULL;
-  if (misaligned(q, 16) || misaligned(out, 16) || misaligned(workspace, 256) || misaligned(lse_out, 4) || misaligned(weight_in, 4) ||
+  if ((q && q == out) || misaligned(q, 16) || misaligned(out, 16) || misaligned(workspace, 256) || misaligned(lse_out, 4) || misaligned(weight_in, 4) ||
       misaligned(weight_out, 4))
     return SHPLB_E_SHAPE;
   const int32_t n_wg = persistent_workgroups();   // two per compute unit

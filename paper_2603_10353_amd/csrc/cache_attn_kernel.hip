@@ -33,7 +33,7 @@ constexpr int kThreads = 256, kWaves = 4, kUnit = 64;
 // between 100 and 16000, where it has one to five items, 102 us without, 97 with two, 100 with five.  Four waves together, which
 // have a unit's work done in a quarter of the time: for 100 sequences x 2 heads of 128 rows and up to a few hundred tokens 44 us with
 // two, 34 with eight, 42 with sixteen; for 128 rows x 8 heads x 32768 tokens 53 with two, 51 from four on.
-constexpr int start_units(int waves) { return waves == 1 ? 2 : 8; }
+constexpr int start_units(int waves) { return waves == 1 ? 2 : kCacheMostStart; }
 constexpr float kLift = 7.0f;                  // log2 of what probabilities are multiplied by, beside their reference ...
 constexpr float kHeadroom = 8.0f;              // ... and how far, in the exponent, they may be above it: 2^15 in fp16
 constexpr int kLdsRow = kHeadDim + 4;          // floats of a row in LDS: rows four banks apart
@@ -97,7 +97,7 @@ __device__ __forceinline__ int lane_sums(int x) {
 
 // The place where a worker's share [begin, end) of all units begins.  Up to 512 pairs every wave adds them up by itself, a lane a run of
 // them; beyond, the four waves do it together, and each looks for its place in the run where it lies, 64 pairs at a time.  (All
-// units are below 2^30: the entry point sees to that.)
+// units, beginnings and all, are below 2^30: the entry point sees to that.)
 template <bool WEIGHTS, int ROWS, int START, class SHARES>
 __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int* lds, int& begin, int& end, SHARES& shares) {
   const int pairs = a.c.n_seq * a.c.n_kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -61,6 +61,9 @@ constexpr int kCacheMaxWorkers = 2048;
 constexpr int64_t kCacheSlotRows = int64_t(2) * kCacheMaxWorkers * 16;
 static_assert(kCacheSlotRows >= int64_t(2) * (kCacheMaxWorkers / 4) * 32, "those of 32 rows, too");
 
+// Units that the beginning of an item counts as at most, beside its own.
+constexpr int kCacheMostStart = 8;
+
 int32_t launch_cache_append(const CacheArgs& c, const StepArgs& t, const void* k, const void* v, hipStream_t stream);
 int32_t launch_cache_load(const CacheArgs& c, const StepArgs& t, void* k, void* v, hipStream_t stream);
 int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int32_t* keep, int32_t n_sink, int32_t n_recent,

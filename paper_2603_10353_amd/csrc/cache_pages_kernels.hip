@@ -164,6 +164,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // up what the parts of its head counted in the launch before.  (One workgroup for a head of 131072 tokens took 195 us.)
 constexpr int kBins = 2048, kEach = 8;                           // bins of a count, weights that a thread holds
 constexpr int kSelectThreads = 1024, kFewThreads = 256, kRun = kSelectThreads * kEach;
+static_assert((int64_t(SHPLB_MAX_BLOCKS) * 128 + kRun - 1) / kRun * SHPLB_MAX_SEQ_HEADS * kSelectThreads <= int64_t(UINT32_MAX), "a grid for all parts");
 
 struct SelectArgs {
   CacheArgs src, dst;
@@ -435,7 +436,11 @@ __global__ __launch_bounds__(kThreads) void evict_gather_kernel(CacheArgs src, C
 
 static int32_t launched() { return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP; }
 
-// Pages of a row that a step can touch at most, and the workgroups for all of them (0: more than a grid holds).
+// Whether a grid holds so many workgroups: its threads are counted in 32 bits.  (Those of 1024 that select are at most 65535 heads
+// x 64 parts.)
+static bool grid_holds(int64_t workgroups) { return workgroups * kThreads <= int64_t(UINT32_MAX); }
+
+// Pages of a row that a step can touch at most.
 static int pages_touched(const CacheArgs& c, const StepArgs& t) {
   const int64_t block = int64_t(1) << c.block_log2, most = (int64_t(t.max_tokens) + block - 2) / block + 1;
   return int(most < c.max_pages ? most : c.max_pages);
@@ -444,7 +449,7 @@ static int pages_touched(const CacheArgs& c, const StepArgs& t) {
 int32_t launch_cache_append(const CacheArgs& c, const StepArgs& t, const void* k, const void* v, hipStream_t stream) {
   const int each = pages_touched(c, t);
   const int64_t grid = int64_t(c.n_seq) * c.n_kv_heads * each * 2;
-  if (grid > INT32_MAX) return SHPLB_E_UNSUPPORTED;
+  if (!grid_holds(grid)) return SHPLB_E_UNSUPPORTED;
   const auto run = c.block_log2 == 7 ? c.format == SHPLB_CACHE_E4M3 ? append_kernel<128, SHPLB_CACHE_E4M3> : append_kernel<128, SHPLB_CACHE_INT8>
                                      : c.format == SHPLB_CACHE_E4M3 ? append_kernel<64, SHPLB_CACHE_E4M3> : append_kernel<64, SHPLB_CACHE_INT8>;
   run<<<dim3(uint32_t(grid)), kThreads, 0, stream>>>(c, t, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), each);
@@ -454,7 +459,7 @@ int32_t launch_cache_append(const CacheArgs& c, const StepArgs& t, const void* k
 int32_t launch_cache_load(const CacheArgs& c, const StepArgs& t, void* k, void* v, hipStream_t stream) {
   const int each = pages_touched(c, t);
   const int64_t grid = int64_t(c.n_seq) * c.n_kv_heads * each * 2;
-  if (grid > INT32_MAX) return SHPLB_E_UNSUPPORTED;
+  if (!grid_holds(grid)) return SHPLB_E_UNSUPPORTED;
   const auto run = c.block_log2 == 7 ? c.format == SHPLB_CACHE_E4M3 ? load_kernel<128, SHPLB_CACHE_E4M3> : load_kernel<128, SHPLB_CACHE_INT8>
                                      : c.format == SHPLB_CACHE_E4M3 ? load_kernel<64, SHPLB_CACHE_E4M3> : load_kernel<64, SHPLB_CACHE_INT8>;
   run<<<dim3(uint32_t(grid)), kThreads, 0, stream>>>(c, t, static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), each);
@@ -474,7 +479,7 @@ int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int3
                            const CacheArgs& dst, float* weight_out, int32_t* kept, void* workspace, hipStream_t stream) {
   const int parts = evict_parts(src);
   const int64_t pairs = int64_t(src.n_seq) * src.n_kv_heads, grid = pairs * dst.max_pages * 2;
-  if (grid > INT32_MAX) return SHPLB_E_UNSUPPORTED;
+  if (!grid_holds(grid)) return SHPLB_E_UNSUPPORTED;
   uint32_t* bins = static_cast<uint32_t*>(workspace);
   const SelectArgs a{src, dst, weight, keep, n_sink, n_recent, parts, weight_out, kept, bins, bins + pairs * parts * 3 * kBins};
   const dim3 all(uint32_t(pairs * parts));

@@ -122,6 +122,44 @@ def test_pointers_of_the_calls():
         assert status(S.shplb_cache_evict, c, *args) == code, (at, value)
 
 
+def test_output_in_place():
+    # queries are read again after the first outputs are written
+    assert status(S.shplb_cache_attn, cache(), step(), FAKE, FAKE, None, None, None, FAKE) == -2
+
+
+def test_strides_whose_product_is_past_64_bits():
+    s = step(n_tokens=2)
+    s.c.kv_stride_h = s.c.q_stride_h = 1 << 62
+    assert status(S.shplb_cache_append, cache(), s, FAKE, FAKE) == -2
+    assert status(S.shplb_cache_load, cache(), s, FAKE, FAKE) == -2
+    assert status(S.shplb_cache_attn_workspace_bytes, cache(), s) == -2
+
+
+@pytest.mark.parametrize("n_seq,max_pages,max_tokens,fits", [
+    (2048, 4096, 1, True), (8192, 4096, 32, True), (8192, 4096, 224, True), (8192, 4096, 256, False),       # units of 64 keys: below 2^30
+    (16000, 1, 34000, False), (8000, 1, 34000, True),                                                    # tiles of 32 rows: below 2^26
+    (16000, 1, 20000, True), (16000, 20, 20000, False),                                                  # ... and eight units more for each
+])
+def test_most_that_attention_takes(n_seq, max_pages, max_tokens, fits):
+    c = cache(n_seq=n_seq, n_kv_heads=4, max_pages=max_pages, block=64)
+    s = step(n_seq=n_seq, n_q_heads=4, n_tokens=5, max_tokens=max_tokens, cu_tokens=FAKE)
+    if fits:
+        assert S.shplb_cache_attn_workspace_bytes(c, s) > 0
+    else:
+        assert status(S.shplb_cache_attn_workspace_bytes, c, s) == -5
+        assert status(S.shplb_cache_attn, c, s, FAKE, 2 * FAKE, None, None, None, FAKE) == -5
+
+
+def test_most_pages_of_a_call():
+    # 2^23 pages that a call may touch
+    c = cache(n_seq=2048, n_kv_heads=4, max_pages=1024, block=64)
+    s = step(n_seq=2048, n_tokens=5, max_tokens=1024 * 64, cu_tokens=FAKE)
+    assert status(S.shplb_cache_append, c, s, FAKE, FAKE) == -5
+    assert status(S.shplb_cache_load, c, s, FAKE, FAKE) == -5
+    small = cache(n_seq=2048, n_kv_heads=4, max_pages=4, page_table=2 * FAKE, lens=2 * FAKE)
+    assert status(S.shplb_cache_evict, small, FAKE, FAKE, 0, 0, c, 2 * FAKE, FAKE, FAKE) == -5
+
+
 def test_calls_without_work_need_no_pointers():
     # a step without tokens is done before it begins
     for s in (step(n_tokens=0, max_tokens=0), step(n_tokens=0, max_tokens=3, cu_tokens=FAKE)):
