@@ -345,9 +345,9 @@ __device__ __forceinline__ void begin_rows(const CacheAttnArgs& a, int pair, int
   }
 }
 
-// Scores of a unit, S^T, of `groups` times sixteen rows.
+// Scores of a unit, S^T.
 template <int NT, int FMT>
-__device__ __forceinline__ void scores(const Keys& keys, const f16x8 (*lds_q)[4][64], int lane, int groups, f32x4 (&sc)[NT][4]) {
+__device__ __forceinline__ void scores(const Keys& keys, const f16x8 (*lds_q)[4][64], int lane, f32x4 (&sc)[NT][4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     f16x8 k[4];
@@ -355,7 +355,6 @@ __device__ __forceinline__ void scores(const Keys& keys, const f16x8 (*lds_q)[4]
     for (int t = 0; t < 4; ++t) k[t] = key_operand<FMT>(keys.code[t][e >> 1][2 * (e & 1)], keys.code[t][e >> 1][2 * (e & 1) + 1]);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      if (nt > 0 && nt >= groups) break;
       const f16x8 q = lds_q[nt][e][lane];
 #pragma unroll
       for (int t = 0; t < 4; ++t) sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[t], q, e == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[nt][t], 0, 0, 0);
@@ -376,7 +375,7 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
     f.page_next = page_number(a.c, pair, min(u + 2 * STEP, last));
     const int key0 = u * kUnit;
     f32x4 sc[NT][4];
-    scores<NT, FMT>(f.k, lds_q, lane, NT, sc);
+    scores<NT, FMT>(f.k, lds_q, lane, sc);
     load_keys<ONCE>(a, ahead, more, k_byte, f.k);
     __builtin_amdgcn_sched_barrier(0);
     // the reference exponent, raised where a score is more than 2^kHeadroom above it
@@ -742,54 +741,95 @@ struct Statistics {
   int seen[NT];
 };
 
-// weight_out = before + the probabilities that the rows put on each key of units first, first + STEP ..
-template <int NT, int STEP, int FMT>
-__device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first, int groups,
-                                      const f16x8 (*lds_q)[4][64], const float* before, int lane, Flight& f, const Statistics<NT>& r) {
-  const int n16 = lane & 15, g = lane >> 4;
+// The probabilities that the rows, of which there is one at least, put on each key of a unit, added up: a lane is left with those of key key_of_lane()
+// of the unit.  (A key whose product is NaN is one that a row sees, or masked: rows that are not there add nothing to others.)  The keys of
+// the next one are asked for on the way.
+__device__ __forceinline__ int key_of_lane(int lane) { return ((lane & 15) >> 2) * 16 + (lane >> 4) * 4 + (lane & 3); }
+template <int NT, int FMT>
+__device__ __forceinline__ float weigh_unit(const CacheAttnArgs& a, int key0, const Page& ahead, bool more, int seen_first,
+                                            const f16x8 (*lds_q)[4][64], int lane, Flight& f, const Statistics<NT>& r) {
+  const int g = lane >> 4;
+  const float k_scale = f.here.bad ? __uint_as_float(kNanBits) : f.here.k_scale;
+  f32x4 sc[NT][4];
+  scores<NT, FMT>(f.k, lds_q, lane, sc);
+  load_keys<false>(a, ahead, more, (lane & 15) * kHeadDim + g * 16, f.k);
+  __builtin_amdgcn_sched_barrier(0);
+  f.here = ahead;
+  float w[16];
+#pragma unroll
+  for (int x = 0; x < 16; ++x) w[x] = 0.0f;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float c = r.to_log2[nt] * k_scale;
+    if (key0 + kUnit > seen_first) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const float p = __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - r.m[nt]) * r.inv[nt];
+        w[x] += key0 + (x >> 2) * 16 + g * 4 + (x & 3) < r.seen[nt] ? p : 0.0f;
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) w[x] += __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - r.m[nt]) * r.inv[nt];
+    }
+  }
+  return sums_of_rows(w, lane);
+}
+
+// weight_out = before + those of units first, first + STEP .. (any: whether there is a row).
+template <int STEP, int FMT>
+__device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first,
+                                      const f16x8 (*lds_q)[4][64], const float* before, int lane, Flight& f, const Statistics<1>& r, bool any) {
   const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
   for (int u = first; u < end; u += STEP) {
-    const float k_scale = f.here.bad ? __uint_as_float(kNanBits) : f.here.k_scale;
     const Page ahead = page_at(a.c, f.page_next, min(u + STEP, last));
     f.page_next = page_number(a.c, pair, min(u + 2 * STEP, last));
-    const int key0 = u * kUnit, key = key0 + (n16 >> 2) * 16 + g * 4 + (n16 & 3);   // the key that is the lane's once sums over the rows are taken
+    const int key = u * kUnit + key_of_lane(lane);
     float old = 0.0f;
     if (before != nullptr && key < len) old = before[row_of_weights + key];
-    f32x4 sc[NT][4];
-    scores<NT, FMT>(f.k, lds_q, lane, groups, sc);
-    load_keys<false>(a, ahead, u + STEP < end, n16 * kHeadDim + g * 16, f.k);
-    __builtin_amdgcn_sched_barrier(0);
-    float w[16];
-#pragma unroll
-    for (int x = 0; x < 16; ++x) w[x] = 0.0f;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      if (nt >= groups) break;
-      const float c = r.to_log2[nt] * k_scale;
-      if (key0 + kUnit > seen_first) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const float p = __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - r.m[nt]) * r.inv[nt];
-          w[x] += key0 + (x >> 2) * 16 + g * 4 + (x & 3) < r.seen[nt] ? p : 0.0f;
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) w[x] += __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - r.m[nt]) * r.inv[nt];
-      }
-    }
-    const float sum = sums_of_rows(w, lane);
+    const float sum = any ? weigh_unit<1, FMT>(a, u * kUnit, ahead, u + STEP < end, seen_first, lds_q, lane, f, r) : 0.0f;
     if (key < len) a.weight_out[row_of_weights + key] = old + sum;
-    f.here = ahead;
   }
 }
 
-// The weights of the step by themselves, taken again from the keys and the rows' statistics: every key belongs to one wave, so nothing is added up
-// between workgroups.  16 NT rows at a time; where there are more, the keys are gone through again for them (of a wave's share, one time right
-// after the other).
-template <int NT, int FMT>
+// What a wave begins to weigh with: rows first_row on and the unit `first`, if it is below end.
+template <int NT>
+__device__ __forceinline__ void begin_weights(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int len, int first, int step,
+                                              int end, int last, int lane, f16x8 (*lds_q)[4][64], Flight& f, Statistics<NT>& r) {
+  const int rows = n * group, page = page_number(a.c, pair, min(first, last));
+  f.page_next = page_number(a.c, pair, min(first + step, last));
+  Query q[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = first_row + nt * 16 + (lane & 15);
+    r.m[nt] = r.inv[nt] = 0.0f;
+    r.seen[nt] = 0;
+    ask_query(a, row0, n, h, group, row, lane, q[nt]);
+    if (row < rows) {
+      const int j = row / group, head = group_head(a.groups, h, row - j * group);
+      const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head));
+      r.seen[nt] = len - n + 1 + j;
+      r.m[nt] = st.x;
+      r.inv[nt] = st.y;
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  ask_unit<false>(a, page, min(first, last), first < end ? end : 0, lane, false, f);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    f16x8 operand[4];
+    const float to_log2 = query_operands(a, q[nt], operand);
+    r.to_log2[nt] = first_row + nt * 16 + (lane & 15) < rows ? to_log2 : 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds_q[nt][e][lane] = operand[e];
+  }
+}
+
+// The weights of the step by themselves, taken again from the keys and the rows' statistics: every key belongs to one share, so nothing is added up
+// between workgroups.  Up to 16 rows every wave has a share.
+template <int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs a) {
   constexpr int kStart = start_units(1);
-  __shared__ f16x8 lds_q[kWaves][NT][4][64];
+  __shared__ f16x8 lds_q[kWaves][1][4][64];
   __shared__ int lds_i[kWaves + kThreads];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int at, end;
@@ -801,43 +841,76 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
     step_tokens<true>(a.t, s, row0, n);
     const int len = it.len, group = group_size(a.groups, h), rows = n * group;
     pair_units<true, 1>(a, rows, len, tiles, units);
-    const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at)), last = max(min(units, u1) - 1, 0);
-    int first_row = 0;
-    do {
-      const int groups = min(NT, (rows - first_row + 15) >> 4);  // of sixteen rows
+    const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at)), last = max(u1 - 1, 0);
+    Flight f;
+    Statistics<1> r;
+    begin_weights<1>(a, pair, h, group, row0, n, 0, len, u0, 1, u1, last, lane, lds_q[wave], f, r);
+    weigh<1, FMT>(a, pair, len, u0, u1, last, len - n + 1, lds_q[wave], a.weight_in, lane, f, r, rows > 0);
+    at += units - it.unit;
+    it = next_pair<kStart>(a, pair);
+  }
+}
+
+// More rows: a workgroup has the share, and its waves 32 rows each, up to 128 at a time.  Where there are fewer, 64 or 32, two or all
+// waves take turns at the units.  What the slices of rows put on the keys of kSteps units each meets in LDS.  (128 rows x 8 heads x 32768 int8
+// tokens: 30 us with a share for every wave and 64 rows at a time, of which beginning was the half, WEIGHTFIG so.)
+template <int FMT>
+__global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAttnArgs a) {
+  constexpr int kStart = start_units(kWaves), kSteps = 8, kSlice = 32;
+  __shared__ f16x8 lds_q[kWaves][2][4][64];
+  __shared__ float lds_w[kSteps][kWaves][kUnit];
+  __shared__ int lds_i[kWaves + kThreads];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int at, end;
+  Shares<true> shares;
+  Item it = locate<true, 1, kStart>(a, int(blockIdx.x), int(gridDim.x), 1, lds_i, at, end, shares);
+  while (at < end) {
+    const int pair = it.pair, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads;
+    int row0, n, tiles, units;
+    step_tokens<true>(a.t, s, row0, n);
+    const int len = it.len, group = group_size(a.groups, h), rows = n * group;
+    pair_units<true, 1>(a, rows, len, tiles, units);
+    const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
+    const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
+    for (int first_row = 0; u0 < u1 && (first_row == 0 || first_row < rows); first_row += kWaves * kSlice) {
+      const int left = rows - first_row, log2 = left > 2 * kSlice ? 2 : left > kSlice ? 1 : 0, slices = 1 << log2, step = kWaves >> log2;
+      const int phase = wave >> log2, my_row = first_row + (wave & (slices - 1)) * kSlice;
+      const int seen_first = len - n + 1 + my_row / max(group, 1);
+      const float* before = first_row == 0 ? a.weight_in : a.weight_out;
       Flight f;
-      const int page = page_number(a.c, pair, min(u0, last));
-      f.page_next = page_number(a.c, pair, min(u0 + 1, last));
-      Statistics<NT> r;
-      Query q[NT];
+      Statistics<2> r;
+      begin_weights<2>(a, pair, h, group, row0, n, my_row, len, u0 + phase, step, u1, u1 - 1, lane, lds_q[wave], f, r);
+      for (int c = u0; c < u1; c += kSteps * step) {
+        // a thread's keys of all these units: kThreads apart
+        const int key = c * kUnit + tid, key_end = min(len, min(u1, c + kSteps * step) * kUnit);
+        float old[kSteps];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int row = first_row + nt * 16 + (lane & 15);
-        r.m[nt] = r.inv[nt] = 0.0f;
-        r.seen[nt] = 0;
-        ask_query(a, row0, n, h, group, row, lane, q[nt]);
-        if (row < rows) {
-          const int j = row / group, head = group_head(a.groups, h, row - j * group);
-          const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head));
-          r.seen[nt] = len - n + 1 + j;
-          r.m[nt] = st.x;
-          r.inv[nt] = st.y;
+        for (int x = 0; x < kSteps; ++x) {
+          old[x] = 0.0f;
+          if (before != nullptr && key + x * kThreads < key_end) old[x] = before[row_of_weights + key + x * kThreads];
         }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      ask_unit<false>(a, page, min(u0, last), u0 < u1 ? u1 : 0, lane, false, f);
+#pragma unroll 1
+        for (int i = 0; i < kSteps; ++i) {
+          const int u = c + i * step + phase;
+          if (u >= u1) break;
+          const Page ahead = page_at(a.c, f.page_next, min(u + step, u1 - 1));
+          f.page_next = page_number(a.c, pair, min(u + 2 * step, u1 - 1));
+          float sum = 0.0f;
+          if (my_row < rows) sum = weigh_unit<2, FMT>(a, u * kUnit, ahead, u + step < u1, seen_first, lds_q[wave], lane, f, r);
+          lds_w[i][wave][key_of_lane(lane)] = sum;
+        }
+        __syncthreads();
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        f16x8 operand[4];
-        const float to_log2 = query_operands(a, q[nt], operand);
-        r.to_log2[nt] = first_row + nt * 16 + (lane & 15) < rows ? to_log2 : 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lds_q[wave][nt][e][lane] = operand[e];
+        for (int x = 0; x < kSteps; ++x) {
+          if (key + x * kThreads >= key_end) break;
+          const int nth = (tid + x * kThreads) >> 6, i = nth >> (2 - log2), p = nth & (step - 1);        // of these units; phase p's i-th
+          float sum = 0.0f;
+          for (int sl = 0; sl < slices; ++sl) sum += lds_w[i][(p << log2) + sl][lane];
+          a.weight_out[row_of_weights + key + x * kThreads] = old[x] + sum;
+        }
+        __syncthreads();
       }
-      weigh<NT, 1, FMT>(a, pair, len, u0, u1, last, len - n + 1 + first_row / max(group, 1), groups, lds_q[wave],
-                        first_row == 0 ? a.weight_in : a.weight_out, lane, f, r);
-      first_row += 16 * NT;
-    } while (first_row < rows);
+    }
     at += units - it.unit;
     it = next_pair<kStart>(a, pair);
   }
@@ -912,7 +985,7 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
   __syncthreads();
   const bool there = n16 < rows;
   const Statistics<1> st = {{r.to_log2[0]}, {there ? lds_ref[n16] : 0.0f}, {there ? lds_inv[n16] : 0.0f}, {r.seen[0]}};
-  weigh<1, kWholeWaves, FMT>(a, pair, len, wave, units, last, seen_before, rows > 0 ? 1 : 0, lds_q, a.weight_in, lane, f, st);
+  weigh<kWholeWaves, FMT>(a, pair, len, wave, units, last, seen_before, lds_q, a.weight_in, lane, f, st, rows > 0);
 }
 
 template <int FMT>
@@ -934,8 +1007,8 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
     else cache_join_kernel<64><<<all, 64, 0, stream>>>(a, rows);
   }
   if (a.weight_out != nullptr) {
-    if (rows == 16) cache_weight_kernel<1, FMT><<<grid, kThreads, 0, stream>>>(a);
-    else cache_weight_kernel<4, FMT><<<grid, kThreads, 0, stream>>>(a);
+    if (rows == 16) cache_weight_kernel<FMT><<<grid, kThreads, 0, stream>>>(a);
+    else cache_weight_rows_kernel<FMT><<<grid, kThreads, 0, stream>>>(a);
   }
   return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
 }
