@@ -44,7 +44,7 @@ struct Item {                                  // a place in the list of units
 };
 // How the list is divided: `each` units a share, and `more` of the shares one more.  Those of waves by themselves: the first ones.  Those of
 // workgroups: evenly among the others, or shares and items of equal lengths drift apart, and more shares have the end of one item and the
-// beginning of another (128 rows x 8 heads x 32768 tokens, eight units a beginning: 51 us, 56 with the first ones; the larger number of shares of
+// beginning of another (128 rows x 8 heads x 32768 tokens, eight units a beginning: 51 us, 56 with the first ones, before other changes; the larger number of shares of
 // waves has less of it, and some power of two apart the longer ones meet on one compute unit: weights of those rows 31 us, 33 evenly).
 template <bool EVENLY>
 struct Shares {
@@ -287,13 +287,21 @@ __device__ __forceinline__ void load_values(const CacheAttnArgs& a, const Page& 
         x.code[kk][half][i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(v, lane_byte, (kk * 32 + half * 16 + i) * kHeadDim, kOnce ? 2 : 0));
 }
 
-// The rows of a wave: what products are multiplied by, the reference exponent, the denominator, the keys seen and the output of row
-// 16 nt + lane % 16, of which a lane has dims 8 (4 (lane / 16) + i) + t.
+// The rows of a wave: the reference exponent, the denominator and the output of row 16 nt + lane % 16, of which a lane has dims
+// 8 (4 (lane / 16) + i) + t.
 template <int NT>
 struct Rows {
-  float to_log2[NT], m[NT], l[NT];
-  int seen[NT];
+  float m[NT], l[NT];
   f32x4 acc[NT][8];
+};
+// ... and what does not change, which would cost registers: the queries as operands, what products are multiplied by and the keys seen.  What a lane
+// reads it wrote itself.
+template <int NT>
+struct RowsLds {
+  f16x8 q[NT][4][64];
+  f32x2 row[NT][64];
+  __device__ __forceinline__ float to_log2(int nt, int lane) const { return row[nt][lane].x; }
+  __device__ __forceinline__ int seen(int nt, int lane) const { return __float_as_int(row[nt][lane].y); }
 };
 // What is on its way to a wave: the codes of a unit, where they come from, and the place of the next one in the page table.  Keys are
 // asked for as soon as those of the unit before are operands, values when those are: either come while the other half of the work
@@ -320,7 +328,7 @@ __device__ __forceinline__ void ask_unit(const CacheAttnArgs& a, int page, int f
 // into LDS, as each lane needs them: what it reads it wrote itself, and they cost no registers.
 template <int NT, int STEP, bool ONCE>
 __device__ __forceinline__ void begin_rows(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int seen_before, int first,
-                                           int end, int last, int lane, f16x8 (*lds_q)[4][64], Flight& f, Rows<NT>& r) {
+                                           int end, int last, int lane, RowsLds<NT>& lds, Flight& f, Rows<NT>& r) {
   const int page = page_number(a.c, pair, min(first, last));
   f.page_next = page_number(a.c, pair, min(first + STEP, last));
   Query q[NT];
@@ -334,10 +342,9 @@ __device__ __forceinline__ void begin_rows(const CacheAttnArgs& a, int pair, int
     f16x8 operand[4];
     const float to_log2 = query_operands(a, q[nt], operand);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) lds_q[nt][e][lane] = operand[e];
+    for (int e = 0; e < 4; ++e) lds.q[nt][e][lane] = operand[e];
     const bool there = row < n * group;
-    r.to_log2[nt] = there ? to_log2 : 0.0f;
-    r.seen[nt] = there ? seen_before + row / group : 0;
+    lds.row[nt][lane] = f32x2{there ? to_log2 : 0.0f, __int_as_float(there ? seen_before + row / group : 0)};
     r.m[nt] = -INFINITY;
     r.l[nt] = 0.0f;
 #pragma unroll
@@ -363,19 +370,20 @@ __device__ __forceinline__ void scores(const Keys& keys, const f16x8 (*lds_q)[4]
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Goes through the units first, first + STEP ..; seen_first: the fewest keys that a row sees.
-template <int NT, int STEP, bool ONCE, int FMT>
+// Goes through the units first, first + STEP ..; seen_first: the fewest keys that a row sees.  KEEP > 0: there are no more than that, and y of
+// each (-inf where it is masked) stays in `kept`.
+template <int NT, int STEP, bool ONCE, int FMT, int KEEP = 0>
 __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first,
-                                       const f16x8 (*lds_q)[4][64], int lane, Flight& f, Rows<NT>& r) {
+                                       const RowsLds<NT>& lds, int lane, Flight& f, Rows<NT>& r, f32x4 (*kept)[4] = nullptr) {
   const int n16 = lane & 15, g = lane >> 4, k_byte = n16 * kHeadDim + g * 16, v_byte = g * 4 * kHeadDim + n16 * 8;
-  for (int u = first; u < end; u += STEP) {
+  const auto attend_unit = [&](int u, f32x4* keep) {
     const float k_scale = f.here.bad ? __uint_as_float(kNanBits) : f.here.k_scale, v_scale = f.here.bad ? k_scale : f.here.v_scale;
     const bool more = u + STEP < end;
     const Page ahead = page_at(a.c, f.page_next, min(u + STEP, last));
     f.page_next = page_number(a.c, pair, min(u + 2 * STEP, last));
     const int key0 = u * kUnit;
     f32x4 sc[NT][4];
-    scores<NT, FMT>(f.k, lds_q, lane, sc);
+    scores<NT, FMT>(f.k, lds.q, lane, sc);
     load_keys<ONCE>(a, ahead, more, k_byte, f.k);
     __builtin_amdgcn_sched_barrier(0);
     // the reference exponent, raised where a score is more than 2^kHeadroom above it
@@ -383,12 +391,17 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
     bool raise = false;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      to[nt] = r.to_log2[nt] * k_scale;
+      to[nt] = lds.to_log2(nt, lane) * k_scale;
       if (key0 + kUnit > seen_first) {
+        const int seen = lds.seen(nt, lane);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[nt][t][i] = key0 + t * 16 + g * 4 + i < r.seen[nt] ? sc[nt][t][i] * to[nt] : -INFINITY;
+          for (int i = 0; i < 4; ++i) sc[nt][t][i] = key0 + t * 16 + g * 4 + i < seen ? sc[nt][t][i] * to[nt] : -INFINITY;
+        to[nt] = 1.0f;
+      } else if (KEEP > 0) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sc[nt][t] *= to[nt];
         to[nt] = 1.0f;
       }
       top[nt] = -INFINITY;
@@ -399,6 +412,10 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
       top[nt] = quad_max(top[nt] * to[nt]);
       raise |= top[nt] > r.m[nt] + kHeadroom;
     }
+    if constexpr (KEEP > 0) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) keep[t] = sc[0][t];
+    }
     if (__ballot(raise)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -407,7 +424,15 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
         r.m[nt] = m_new;
         r.l[nt] *= alpha;
 #pragma unroll
-        for (int t = 0; t < 8; ++t) r.acc[nt][t] *= alpha;
+        for (int t = 0; t < 8; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x = r.acc[nt][t][i];
+            // in place: as another value, every register would be moved where nothing is raised (and spilled: 51 -> 41 us for 128 rows x 8 heads x
+            // 32768 tokens)
+            asm volatile("v_mul_f32 %0, %1, %0" : "+v"(x) : "v"(alpha));
+            r.acc[nt][t][i] = x;
+          }
       }
     }
     f16x8 p[NT][2];
@@ -433,6 +458,7 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
         for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, two[4 * kk + e]);
         p[nt][kk] = __builtin_bit_cast(f16x8, w);
       }
+      asm volatile("" : "+v"(r.l[nt]));                         // here and now: added up later, all the addends would have to be kept
     }
     if (key0 + kUnit > len) {
       // codes behind the last token may be anything, NaN among them
@@ -483,7 +509,7 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
             x = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[kk], p[nt][kk], x, 0, 0, 0);
             y = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[kk], p[nt][kk], y, 0, 0, 0);
           }
-          const float scale = key0 < r.seen[nt] ? v_scale : 0.0f;
+          const float scale = key0 < lds.seen(nt, lane) ? v_scale : 0.0f;
           r.acc[nt][2 * t2] += x * scale;
           r.acc[nt][2 * t2 + 1] += y * scale;
         }
@@ -492,20 +518,27 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
     __builtin_amdgcn_sched_barrier(0);
     load_values<ONCE>(a, ahead, more, v_byte, f.v);
     f.here = ahead;
+  };
+  if constexpr (KEEP == 0) {
+    for (int u = first; u < end; u += STEP) attend_unit(u, nullptr);
+  } else {
+    static_assert(NT == 1, "of one group of rows");
+#pragma unroll
+    for (int x = 0; x < KEEP; ++x)
+      if (first + x * STEP < end) attend_unit(first + x * STEP, kept[x]);
   }
 }
 
 // Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a workgroup, which
 // take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.  (For 128 rows x 8 heads x
-// 32768 int8 tokens 54 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.  A wave of 64 rows needs half of that but
-// more registers than there are without moving them about, 84 us; tiles side by side in a workgroup, to read the codes from memory
-// once, 53 for 64 rows, 61 for 128.)
+// 32768 int8 tokens 41 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.  Tiles side by side in a workgroup,
+// to read the codes from memory once, bring nothing.)
 template <int NT, int WAVES, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a, int least) {
   constexpr bool kOwn = WAVES == 1;
   constexpr int kRows = 16 * NT, kStart = start_units(WAVES);
   static_assert(kOwn || WAVES == kWaves, "one, or all of a workgroup");
-  __shared__ f16x8 lds_q[kOwn ? kWaves : 1][NT][4][64];
+  __shared__ RowsLds<NT> lds_rows[kOwn ? kWaves : 1];
   __shared__ float lds_o[WAVES][16][kLdsRow];
   __shared__ float lds_m[WAVES][kRows], lds_l[WAVES][kRows];
   __shared__ int lds_i[kWaves + kThreads];
@@ -534,11 +567,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
     if (u1 <= u0) break;                                         // the share ends before the item's first unit
     const int first_row = it.tile * kRows, u_first = u0 + (kOwn ? 0 : wave), u_end = good && len > 0 ? u1 : 0;
-    f16x8(*q)[4][64] = lds_q[kOwn ? wave : 0];                   // (waves of one share write the same)
+    RowsLds<NT>& rows_lds = lds_rows[kOwn ? wave : 0];           // (waves of one share write the same)
     Flight f;
     Rows<NT> r;
-    begin_rows<NT, WAVES, kOwn>(a, pair, h, group, row0, n, first_row, len - n + 1, u_first, u_end, u1 - 1, lane, q, f, r);
-    attend<NT, WAVES, kOwn, FMT>(a, pair, len, u_first, u_end, u1 - 1, len - n + 1 + first_row / group, q, lane, f, r);
+    begin_rows<NT, WAVES, kOwn>(a, pair, h, group, row0, n, first_row, len - n + 1, u_first, u_end, u1 - 1, lane, rows_lds, f, r);
+    attend<NT, WAVES, kOwn, FMT>(a, pair, len, u_first, u_end, u1 - 1, len - n + 1 + first_row / group, rows_lds, lane, f, r);
 
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
@@ -775,18 +808,18 @@ __device__ __forceinline__ float weigh_unit(const CacheAttnArgs& a, int key0, co
   return sums_of_rows(w, lane);
 }
 
-// weight_out = before + those of units first, first + STEP .. (any: whether there is a row).
-template <int STEP, int FMT>
+// weight_out = before + those of units first .. end - 1 (any: whether there is a row).
+template <int FMT>
 __device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first,
                                       const f16x8 (*lds_q)[4][64], const float* before, int lane, Flight& f, const Statistics<1>& r, bool any) {
   const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
-  for (int u = first; u < end; u += STEP) {
-    const Page ahead = page_at(a.c, f.page_next, min(u + STEP, last));
-    f.page_next = page_number(a.c, pair, min(u + 2 * STEP, last));
+  for (int u = first; u < end; ++u) {
+    const Page ahead = page_at(a.c, f.page_next, min(u + 1, last));
+    f.page_next = page_number(a.c, pair, min(u + 2, last));
     const int key = u * kUnit + key_of_lane(lane);
     float old = 0.0f;
     if (before != nullptr && key < len) old = before[row_of_weights + key];
-    const float sum = any ? weigh_unit<1, FMT>(a, u * kUnit, ahead, u + STEP < end, seen_first, lds_q, lane, f, r) : 0.0f;
+    const float sum = any ? weigh_unit<1, FMT>(a, u * kUnit, ahead, u + 1 < end, seen_first, lds_q, lane, f, r) : 0.0f;
     if (key < len) a.weight_out[row_of_weights + key] = old + sum;
   }
 }
@@ -845,7 +878,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
     Flight f;
     Statistics<1> r;
     begin_weights<1>(a, pair, h, group, row0, n, 0, len, u0, 1, u1, last, lane, lds_q[wave], f, r);
-    weigh<1, FMT>(a, pair, len, u0, u1, last, len - n + 1, lds_q[wave], a.weight_in, lane, f, r, rows > 0);
+    weigh<FMT>(a, pair, len, u0, u1, last, len - n + 1, lds_q[wave], a.weight_in, lane, f, r, rows > 0);
     at += units - it.unit;
     it = next_pair<kStart>(a, pair);
   }
@@ -853,7 +886,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
 
 // More rows: a workgroup has the share, and its waves 32 rows each, up to 128 at a time.  Where there are fewer, 64 or 32, two or all
 // waves take turns at the units.  What the slices of rows put on the keys of kSteps units each meets in LDS.  (128 rows x 8 heads x 32768 int8
-// tokens: 30 us with a share for every wave and 64 rows at a time, of which beginning was the half, WEIGHTFIG so.)
+// tokens: 30 us with a share for every wave and 64 rows at a time, of which beginning was the half, 26 so; VALU work,
+// turning the codes into fp16 for every 32 rows and the exponentials.)
 template <int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAttnArgs a) {
   constexpr int kStart = start_units(kWaves), kSteps = 8, kSlice = 32;
@@ -917,12 +951,13 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
 }
 
 // A head a workgroup, eight waves taking turns at its units: output, denominators and weights in one launch, without partial results.  For
-// up to 16 rows and as many heads as there are compute units, in caches that leave a wave no more than kWholeUnits units.
+// up to 16 rows and as many heads as there are compute units, in caches that leave a wave no more than kWholeUnits units, whose products stay in
+// registers until the weights can be told (48 sequences x 4 heads of up to 2000 tokens, 7 rows: 21 us with the keys gone through again, 15 so).
 constexpr int kWholeWaves = 8, kWholeUnits = 4;
 
-template <int FMT>
+template <bool WEIGHTS, int FMT>
 __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheAttnArgs a) {
-  __shared__ f16x8 lds_q[1][4][64];
+  __shared__ RowsLds<1> lds;
   __shared__ float lds_o[kWholeWaves][16][kLdsRow];
   __shared__ float lds_m[kWholeWaves][16], lds_l[kWholeWaves][16], lds_ref[16], lds_inv[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, quad = lane >> 4;
@@ -933,13 +968,16 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
   const bool good = good_length(a.c, len);
   // (the page table is read up to its end: what is looked up does not wait for the length)
   const int rows = n * group, units = good ? (len + kUnit - 1) / kUnit : 0, last = ((a.c.max_pages << a.c.block_log2) / kUnit) - 1, seen_before = len - n + 1;
-  if (rows == 0 && a.weight_out == nullptr) return;
+  if (rows == 0 && !WEIGHTS) return;
   Flight f;
   Rows<1> r;
-  const int page = page_number(a.c, pair, min(wave, last)), page_next = page_number(a.c, pair, min(wave + kWholeWaves, last));
-  begin_rows<1, kWholeWaves, false>(a, pair, h, max(group, 1), row0, n, 0, seen_before, wave, units, last, lane, lds_q, f, r);
+  f32x4 kept[kWholeUnits][4];
+  const int key = wave * kUnit + key_of_lane(lane);              // of the first unit, whose probabilities' sum comes to this lane
+  const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
+  float old[kWholeUnits];
+  begin_rows<1, kWholeWaves, false>(a, pair, h, max(group, 1), row0, n, 0, seen_before, wave, units, last, lane, lds, f, r);
   if (rows > 0) {
-    attend<1, kWholeWaves, false, FMT>(a, pair, len, wave, units, last, seen_before, lds_q, lane, f, r);
+    attend<1, kWholeWaves, false, FMT, WEIGHTS ? kWholeUnits : 0>(a, pair, len, wave, units, last, seen_before, lds, lane, f, r, kept);
     r.l[0] = quad_sum(r.l[0]);
     if (quad == 0) {
       lds_m[wave][n16] = r.m[0];
@@ -952,9 +990,12 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
       *reinterpret_cast<f32x4*>(dst + 4) = f32x4{r.acc[0][4][i], r.acc[0][5][i], r.acc[0][6][i], r.acc[0][7][i]};
     }
   }
-  if (a.weight_out != nullptr) {                                 // the keys again
-    f.page_next = page_next;
-    ask_unit<false>(a, page, min(wave, last), wave < units ? units : 0, lane, false, f);
+  if constexpr (WEIGHTS) {
+#pragma unroll
+    for (int x = 0; x < kWholeUnits; ++x) {
+      const int at = key + x * kWholeWaves * kUnit;
+      old[x] = a.weight_in != nullptr && at < len && good ? a.weight_in[row_of_weights + at] : 0.0f;
+    }
   }
   __syncthreads();
   const int row = tid >> 5, d = (tid & 31) * 4;
@@ -981,11 +1022,23 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
       lds_inv[row] = inv;
     }
   }
-  if (a.weight_out == nullptr) return;
-  __syncthreads();
-  const bool there = n16 < rows;
-  const Statistics<1> st = {{r.to_log2[0]}, {there ? lds_ref[n16] : 0.0f}, {there ? lds_inv[n16] : 0.0f}, {r.seen[0]}};
-  weigh<kWholeWaves, FMT>(a, pair, len, wave, units, last, seen_before, lds_q, a.weight_in, lane, f, st, rows > 0);
+  if constexpr (WEIGHTS) {
+    __syncthreads();
+    const float m = n16 < rows ? lds_ref[n16] : 0.0f, inv = n16 < rows ? lds_inv[n16] : 0.0f;
+#pragma unroll
+    for (int x = 0; x < kWholeUnits; ++x) {
+      if (wave + x * kWholeWaves >= units) break;
+      float sum = 0.0f;
+      if (rows > 0) {
+        float p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(kept[x][e >> 2][e & 3] - m) * inv;
+        sum = sums_of_rows(p, lane);
+      }
+      const int at = key + x * kWholeWaves * kUnit;
+      if (at < len) a.weight_out[row_of_weights + at] = old[x] + sum;
+    }
+  }
 }
 
 template <int FMT>
@@ -993,7 +1046,8 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
   const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2), pairs = a.c.n_seq * a.c.n_kv_heads;
   const int64_t capacity = int64_t(a.c.max_pages) << a.c.block_log2;
   if (rows == 16 && pairs <= compute_units && capacity <= kWholeWaves * kWholeUnits * kUnit) {
-    cache_whole_kernel<FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
+    if (a.weight_out != nullptr) cache_whole_kernel<true, FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
+    else cache_whole_kernel<false, FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
     return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
   }
   if (a.t.n_tokens > 0) {
