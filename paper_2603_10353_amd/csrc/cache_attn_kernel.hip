@@ -10,18 +10,23 @@
 // token of a KV head is 256 bytes and, for a group of four heads, 4 KFLOP.  So the matrix instructions are used for what they save in
 // registers and lanes, with most of their rows empty in a plain decoding step.
 //
-// Split.  All heads' keys together are one list of units of 64 keys, of which every workgroup takes an equal, contiguous share
-// whatever the heads' lengths are: lengths differ between sequences, and between heads after an eviction.  The lengths are on the
-// device (they change while a captured launch stays), so each workgroup adds them up by itself.  A (sequence, KV head, tile of rows)
-// whose units lie in several workgroups has partial results (m, l, unnormalised output), which a second kernel joins in order.
+// Split.  All heads' keys together are one list of units of 64 keys, which is cut into equal, contiguous shares whatever the heads'
+// lengths are: lengths differ between sequences, and between heads after an eviction.  A share is a wave's where a head has up to 16
+// rows, and a workgroup's where it has more (tiles of 32 rows).  The lengths are on the device (they change while a captured
+// launch stays), so each wave adds them up by itself.  A (sequence, KV head, tile of rows) whose units lie in several shares has
+// partial results (m, l, unnormalised output), which a second kernel joins in order.  Short caches of few heads are worked on head by head
+// in one launch.
 //
-// Tile.  A wave works on units of its own: keys are the rows of the first product (S^T = K Q^T), so a lane has scores of one query
+// Tile.  A wave works on a unit at a time: keys are the rows of the first product (S^T = K Q^T), so a lane has scores of one query
 // and four adjacent keys of each 16; the second one is O^T = V^T P^T, whose operand P^T needs exactly those (the order of the keys
-// inside a product is free, as long as V's are taken alike).  Codes come straight from global memory into registers, are turned to fp16
-// there (exact in both formats), V's after a byte transposition of key pairs; nothing goes through LDS.
+// inside a product is free, as long as V's are taken alike).  Codes come straight from global memory into registers and are turned to fp16
+// there (exact in both formats), V's after a byte transposition of key pairs; queries wait in LDS as operands.
 // Q is brought to fp16 by a power of two per row, so that its largest magnitude lies in [2^13, 2^14): exact down to 2^-27 of it.
 // Probabilities are rounded to fp16 at 2^7 times their size: eleven bits down to 2^-21 of the reference, steps of 2^-31 of it below.  Values are
-// fp16 numbers, too, scale and all, where the scale lies between 2^-15 and 2^7.  All sums are fp32.
+// fp16 numbers, too, scale and all, where the scale lies between 2^-15 and 2^7 (int8 2^-14 and 2^5).  All sums are fp32.
+//
+// Measured: 128 sequences x 8 heads of 100 to 16000 tokens (570 MB) 98 us, 5.8 TB/s; one sequence of 131072 tokens x 8 heads 47 us, and
+// 6 to join; a sequence of 777 tokens 10 us, of which the launch and three reads that wait for one another are eight.
 #include "cache_common.h"
 
 namespace shplb {
@@ -429,7 +434,8 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
           for (int i = 0; i < 4; ++i) {
             float x = r.acc[nt][t][i];
             // in place: as another value, every register would be moved where nothing is raised (and spilled: 51 -> 41 us for 128 rows x 8 heads x
-            // 32768 tokens)
+            // 32768 tokens).  The products that write and read the outputs are a hundred instructions away on either side: the compiler, which does
+            // not look into this line, puts no wait states between them
             asm volatile("v_mul_f32 %0, %1, %0" : "+v"(x) : "v"(alpha));
             r.acc[nt][t][i] = x;
           }

@@ -302,12 +302,12 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
       } else {
         static_assert(kAll || kPer == 2, "eight bytes of each part");
         const uint32_t* from = a.bins + (int64_t(pair) * parts * 3 + pass) * kBins + (kBins - kPer - kPer * tid);
-        for (int p0 = 0; p0 < parts; p0 += 16) {                 // all of them in flight
-          u32x2 y[16];
+        for (int p0 = 0; p0 < parts; p0 += 32) {                 // all of them in flight
+          u32x2 y[32];
 #pragma unroll
-          for (int p = 0; p < 16; ++p) y[p] = p0 + p < parts ? *reinterpret_cast<const u32x2*>(from + int64_t(p0 + p) * 3 * kBins) : u32x2{0, 0};
+          for (int p = 0; p < 32; ++p) y[p] = p0 + p < parts ? *reinterpret_cast<const u32x2*>(from + int64_t(p0 + p) * 3 * kBins) : u32x2{0, 0};
 #pragma unroll
-          for (int p = 0; p < 16; ++p)
+          for (int p = 0; p < 32; ++p)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               n[i] += y[p][1 - i];
