@@ -100,11 +100,11 @@ __device__ __forceinline__ int lane_sums(int x) {
   return x;
 }
 
-// The place where a worker's share [begin, end) of all units begins.  Up to 512 pairs every wave adds them up by itself, a lane a run of
+// The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more than `few` of them.  Up to 512 pairs every wave adds them up by itself, a lane a run of
 // them; beyond, the four waves do it together, and each looks for its place in the run where it lies, 64 pairs at a time.  (All
 // units, beginnings and all, are below 2^30: the entry point sees to that.)
 template <bool WEIGHTS, int ROWS, int START, class SHARES>
-__device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int* lds, int& begin, int& end, SHARES& shares) {
+__device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int few, int* lds, int& begin, int& end, SHARES& shares) {
   const int pairs = a.c.n_seq * a.c.n_kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool together = pairs > 512;
   const int me = together ? threadIdx.x : lane, each = together ? (pairs + kThreads - 1) / kThreads : (pairs + 63) / 64;
@@ -129,7 +129,7 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
     lds[kWaves + threadIdx.x] = sum;
     __syncthreads();
   }
-  if (total < workers * least) workers = max((total + least - 1) / least, 1);
+  if (total < workers * least) workers = max((total + least - 1) / least, max(min(total, few), 1));
   shares.each = total / workers;
   shares.more = total - shares.each * workers;
   shares.n = workers;
@@ -553,7 +553,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
   Shares<!kOwn> shares;
   // neighbouring shares in different workgroups, on different compute units
   const int worker = kOwn ? int(blockIdx.x) + wave * int(gridDim.x) : int(blockIdx.x);
-  Item it = locate<false, kRows, kStart>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, lds_i, at, end, shares);
+  Item it = locate<false, kRows, kStart>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, kOwn ? int(gridDim.x) : 1, lds_i, at, end, shares);
   while (at < end) {
     // (the lane as a number of which the compiler knows nothing: what follows from it is worked out here and again at the item's end, and
     // takes no registers in between)
@@ -873,7 +873,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int at, end;
   Shares<false> shares;
-  Item it = locate<true, 1, kStart>(a, int(blockIdx.x) + wave * int(gridDim.x), int(gridDim.x) * kWaves, 1, lds_i, at, end, shares);
+  Item it = locate<true, 1, kStart>(a, int(blockIdx.x) + wave * int(gridDim.x), int(gridDim.x) * kWaves, 1, 1, lds_i, at, end, shares);
   while (at < end) {
     const int pair = it.pair, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads;
     int row0, n, tiles, units;
@@ -903,7 +903,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int at, end;
   Shares<true> shares;
-  Item it = locate<true, 1, kStart>(a, int(blockIdx.x), int(gridDim.x), 1, lds_i, at, end, shares);
+  Item it = locate<true, 1, kStart>(a, int(blockIdx.x), int(gridDim.x), 1, 1, lds_i, at, end, shares);
   while (at < end) {
     const int pair = it.pair, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads;
     int row0, n, tiles, units;
@@ -1057,7 +1057,10 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
     return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
   }
   if (a.t.n_tokens > 0) {
-    if (rows == 16) cache_attn_kernel<1, 1, FMT><<<grid, kThreads, 0, stream>>>(a, 1);
+    // (three units at least where there is more than one share for every workgroup: waves that share a compute unit wait for one another's beginnings, and
+    // pieces are joined; five sequences of up to 39284 tokens x 2 heads 15 and 9 us with one unit, 13 and 5 with three, 12 and 5 with four; 16 up
+    // to 8000 13 and 7, 11 and 5, 12 and 4; one of 2048 x 8 heads, 272 units, 7 and 4 with one, 10 and 4 with three)
+    if (rows == 16) cache_attn_kernel<1, 1, FMT><<<grid, kThreads, 0, stream>>>(a, 3);
     else cache_attn_kernel<2, kWaves, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
     // few rows are of many pieces, many of few: 32 rows of 256 pieces (131072 tokens x 8 heads) take 6.6 us with 1024 threads each, 9 with 256; 4096 rows
     // of one to four 5.4 with 64, 7 with 256

@@ -159,11 +159,12 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // Which tokens of a head stay: the want-th largest key among the tokens that may go is found eleven, eleven and ten bits at a time by counting
 // keys in bins; the tokens' places follow from how many keys in front of them lie above it or at it.
 //
-// Of caches of up to kRun positions a head is one workgroup's, from the first count to the last token written.  Longer
+// Of caches of up to 2 kRun positions a head is one workgroup's, from the first count to the last token written.  Longer
 // heads are cut into parts of up to kRun positions, and counting, counting, counting and writing are launches of their own: each begins by adding
-// up what the parts of its head counted in the launch before.  (One workgroup for a head of 131072 tokens took 195 us.)
-constexpr int kBins = 2048, kEach = 8;                           // bins of a count, weights that a thread holds
-constexpr int kSelectThreads = 1024, kFewThreads = 256, kRun = kSelectThreads * kEach;
+// up what the parts of its head counted in the launch before.  (8 heads of 13269 tokens: 19 us by one workgroup each, 28 and what lies
+// between launches in two parts; of 32525 35, and 29 in four; of 131072 195, and 30.)
+constexpr int kBins = 2048, kEach = 8;                           // bins of a count, weights that a thread holds (of one workgroup's heads up to kMostEach)
+constexpr int kSelectThreads = 1024, kFewThreads = 256, kMostEach = 16, kRun = kSelectThreads * kEach;
 static_assert((int64_t(SHPLB_MAX_BLOCKS) * 128 + kRun - 1) / kRun * SHPLB_MAX_SEQ_HEADS * kSelectThreads <= int64_t(UINT32_MAX), "a grid for all parts");
 
 struct SelectArgs {
@@ -208,15 +209,17 @@ __device__ __forceinline__ uint32_t pass_mask(int pass) { return pass == 0 ? 0u 
 
 // Counts the keys that agree with the threshold in the bits settled so far, by the next bits.  A thread's keys are those of positions
 // p + 64 i, of which those in [first, last) count.
-template <int THREADS>
-__device__ __forceinline__ void count_keys(const uint32_t (&key)[kEach], int p, int first, int last, int pass, uint32_t threshold, SelectLds& lds) {
+template <int THREADS, int EACH>
+__device__ __forceinline__ void count_keys(const float (&x)[EACH], int p, int first, int last, int pass, uint32_t threshold, SelectLds& lds) {
   for (int b = threadIdx.x; b < kBins; b += THREADS) lds.bins[b] = 0;
   __syncthreads();
   const uint32_t mask = pass_mask(pass), low = pass == 2 ? 1023 : 2047;
   const int shift = pass_shift(pass);
 #pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if (p + 64 * i >= first && p + 64 * i < last && (key[i] & mask) == threshold) atomicAdd(&lds.bins[(key[i] >> shift) & low], 1u);
+  for (int i = 0; i < EACH; ++i) {
+    const uint32_t key = weight_key(x[i]);
+    if (p + 64 * i >= first && p + 64 * i < last && (key & mask) == threshold) atomicAdd(&lds.bins[(key >> shift) & low], 1u);
+  }
   __syncthreads();
 }
 
@@ -257,7 +260,7 @@ __device__ __forceinline__ void pick_bin(const uint32_t (&all)[PER], const uint3
 }
 
 // STAGE 0, 1, 2 count, 3 writes; -1: all of it.
-template <int STAGE, int THREADS>
+template <int STAGE, int THREADS, int EACH>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
   constexpr bool kAll = STAGE < 0;
   constexpr int kPer = kBins / THREADS;
@@ -274,12 +277,9 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
   // every wave has a run of positions, all of whose weights it keeps in registers
   const int run = (end - begin + THREADS - 1) / THREADS * 64, run_begin = min(begin + wave * run, end), run_end = min(run_begin + run, end);
   const int first = plan.from, last = min(run_end, plan.to), mine = run_begin + lane;
-  float x[kEach];
-  uint32_t key[kEach];
+  float x[EACH];
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) x[i] = mine + 64 * i < run_end ? w[mine + 64 * i] : 0.0f;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) key[i] = weight_key(x[i]);
+  for (int i = 0; i < EACH; ++i) x[i] = mine + 64 * i < run_end ? w[mine + 64 * i] : 0.0f;
   uint32_t* bins = kAll ? nullptr : a.bins + int64_t(blockIdx.x) * 3 * kBins;
   uint32_t* found = kAll ? nullptr : a.found + int64_t(blockIdx.x) * 4;
 
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
     for (int pass = kAll ? 0 : max(STAGE - 1, 0); pass < (kAll ? 3 : STAGE); ++pass) {
       uint32_t n[kPer] = {}, front[kPer] = {};
       if (kAll) {
-        count_keys<THREADS>(key, mine, first, last, pass, threshold, lds);
+        count_keys<THREADS, EACH>(x, mine, first, last, pass, threshold, lds);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) n[i] = lds.bins[kBins - 1 - (kPer * tid + i)];
       } else {
@@ -324,7 +324,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
     }
     ties = want;
     if (!kAll && STAGE < 3) {
-      count_keys<THREADS>(key, mine, first, last, STAGE, threshold, lds);
+      count_keys<THREADS, EACH>(x, mine, first, last, STAGE, threshold, lds);
       for (int b = tid; b < kBins / 4; b += THREADS) reinterpret_cast<u32x4*>(bins + STAGE * kBins)[b] = reinterpret_cast<const u32x4*>(lds.bins)[b];
       if (tid == 0 && STAGE > 0) {
         found[0] = threshold;
@@ -337,11 +337,12 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
   // tokens that stay in any case count as above; those of the parts in front of this one are known
   uint32_t above = 0, equal = 0;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     const int p = mine + 64 * i;
+    const uint32_t key = weight_key(x[i]);
     const bool there = p < run_end, forced = all || p < plan.from || p >= plan.to;
-    above += there && (forced || key[i] > threshold);
-    equal += there && !forced && key[i] == threshold;
+    above += there && (forced || key > threshold);
+    equal += there && !forced && key == threshold;
   }
   uint64_t both = uint64_t(equal) << 32 | above;
 #pragma unroll
@@ -357,11 +358,12 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
   const int64_t row = int64_t(pair) * a.dst.max_pages << a.dst.block_log2;
   const uint64_t below = (uint64_t(1) << lane) - 1;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     const int p = mine + 64 * i;
+    const uint32_t key = weight_key(x[i]);
     if (run_begin + 64 * i >= run_end) break;
     const bool there = p < run_end, forced = there && (all || p < plan.from || p >= plan.to);
-    const uint64_t over = __ballot(forced || (there && key[i] > threshold)), at = __ballot(there && !forced && key[i] == threshold);
+    const uint64_t over = __ballot(forced || (there && key > threshold)), at = __ballot(there && !forced && key == threshold);
     const uint32_t rank = equal + __popcll(at & below);
     if ((over >> lane & 1) || ((at >> lane & 1) && rank < ties)) {
       const uint32_t place = above + __popcll(over & below) + min(rank, ties);
@@ -468,7 +470,7 @@ int32_t launch_cache_load(const CacheArgs& c, const StepArgs& t, void* k, void* 
 
 static int evict_parts(const CacheArgs& c) {
   const int64_t capacity = int64_t(c.max_pages) << c.block_log2;
-  return int((capacity + kRun - 1) / kRun);
+  return capacity <= kSelectThreads * kMostEach ? 1 : int((capacity + kRun - 1) / kRun);
 }
 int64_t cache_evict_workspace(const CacheArgs& c) {
   const int64_t parts = evict_parts(c);
@@ -484,14 +486,16 @@ int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int3
   const SelectArgs a{src, dst, weight, keep, n_sink, n_recent, parts, weight_out, kept, bins, bins + pairs * parts * 3 * kBins};
   const dim3 all(uint32_t(pairs * parts));
   if (parts == 1) {
-    // (48 sequences x 4 heads of up to 2000 tokens: 13 us with 1024 threads, 9 with 256)
-    if (int64_t(src.max_pages) << src.block_log2 <= kFewThreads * kEach) evict_select_kernel<-1, kFewThreads><<<all, kFewThreads, 0, stream>>>(a);
-    else evict_select_kernel<-1, kSelectThreads><<<all, kSelectThreads, 0, stream>>>(a);
+    // as few threads and weights of each as there can be (48 sequences x 4 heads of up to 2000 tokens: 13 us with 1024 threads, 9 with 256)
+    const int64_t capacity = int64_t(src.max_pages) << src.block_log2;
+    if (capacity <= kFewThreads * kEach) evict_select_kernel<-1, kFewThreads, kEach><<<all, kFewThreads, 0, stream>>>(a);
+    else if (capacity <= kRun) evict_select_kernel<-1, kSelectThreads, kEach><<<all, kSelectThreads, 0, stream>>>(a);
+    else evict_select_kernel<-1, kSelectThreads, kMostEach><<<all, kSelectThreads, 0, stream>>>(a);
   } else {
-    evict_select_kernel<0, kSelectThreads><<<all, kSelectThreads, 0, stream>>>(a);
-    evict_select_kernel<1, kSelectThreads><<<all, kSelectThreads, 0, stream>>>(a);
-    evict_select_kernel<2, kSelectThreads><<<all, kSelectThreads, 0, stream>>>(a);
-    evict_select_kernel<3, kSelectThreads><<<all, kSelectThreads, 0, stream>>>(a);
+    evict_select_kernel<0, kSelectThreads, kEach><<<all, kSelectThreads, 0, stream>>>(a);
+    evict_select_kernel<1, kSelectThreads, kEach><<<all, kSelectThreads, 0, stream>>>(a);
+    evict_select_kernel<2, kSelectThreads, kEach><<<all, kSelectThreads, 0, stream>>>(a);
+    evict_select_kernel<3, kSelectThreads, kEach><<<all, kSelectThreads, 0, stream>>>(a);
   }
   const auto run = src.format == SHPLB_CACHE_E4M3 ? evict_gather_kernel<SHPLB_CACHE_E4M3> : evict_gather_kernel<SHPLB_CACHE_INT8>;
   run<<<dim3(uint32_t(grid)), kThreads, 0, stream>>>(src, dst, kept);
