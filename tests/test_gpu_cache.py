@@ -379,8 +379,9 @@ def test_evict_long_head():
     evict_case(rng, [[70001, 2000, 64]], [[9000, 1999, 1]], 128, 128, 128, 128, orc.E4M3, 80, "ties")
 
 
-# tokens of three heads: where one workgroup still sees all of a head's weights, and where parts of 8192 are counted by themselves
-EVICTS = {"one_part": [5000, 8000, 2049], "whole_part": [8064, 3, 8000], "parts": [16385, 8193, 8192], "last_of_a_part": [24448, 16384, 0]}
+# tokens of three heads: where one workgroup sees all of a head's weights, and where parts of 8192 are counted by themselves
+EVICTS = {"one_part": [5000, 8000, 2049], "whole_part": [8064, 3, 8000], "twice_that": [12001, 16256, 8193],
+          "parts": [16385, 8193, 8192], "last_of_a_part": [24448, 16384, 0]}
 
 
 @pytest.mark.parametrize("kind", ["heavy", "ties", "zeros"])
