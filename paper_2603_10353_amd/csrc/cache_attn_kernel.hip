@@ -414,7 +414,7 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top[nt] = fmaxf(top[nt], sc[nt][t][i]);
-      top[nt] = quad_max(top[nt] * to[nt]);
+      top[nt] *= to[nt];
       raise |= top[nt] > r.m[nt] + kHeadroom;
     }
     if constexpr (KEEP > 0) {
@@ -424,6 +424,7 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
     if (__ballot(raise)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
+        top[nt] = quad_max(top[nt]);
         const float m_new = top[nt] > r.m[nt] + kHeadroom ? top[nt] : r.m[nt];
         const float alpha = m_new == r.m[nt] ? 1.0f : __builtin_amdgcn_exp2f(r.m[nt] - m_new);
         r.m[nt] = m_new;
