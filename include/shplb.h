@@ -297,10 +297,11 @@ SHPLB_API int32_t shplb_token_recovery_heads(const shplb_problem* p, const float
  *     max_pages * block: the head's outputs are NaN, nothing is written into it, read out of
  *     it or counted for it, and eviction hands it on as length -1.
  *   - Pages may be shared (a common prefix) by heads that only read them.
- * Errors of all calls: SHPLB_E_NULL, SHPLB_E_SHAPE (sizes below those below, strides that are no multiple of 8 or smaller than what they
- * hold, pointers not aligned to their elements, of tensors and pages to 16 bytes), SHPLB_E_UNSUPPORTED (more than stands below, element strides
- * from 2^24 on, 2^23 pages or more that a call may touch, in attention 2^24 rows of a KV head, 2^26 tiles of 32 rows or
- * 2^30 - 8 tiles units of 64 tokens, of page tables' capacity, for all tiles). */
+ * Errors of all calls: SHPLB_E_NULL; SHPLB_E_SHAPE (a size smaller than stated, strides smaller than what they step
+ * over or no multiple of 8, tensors and pages not aligned to 16 bytes, other arrays not to their elements);
+ * SHPLB_E_UNSUPPORTED (a size larger than stated, element strides from 2^24 on, 2^23 pages or more that a call may touch; in
+ * attention 2^24 rows of a KV head, 2^26 tiles of 32 rows, or 2^30 units of 64 tokens, of the page tables' capacity, a tile
+ * counting eight more). */
 #define SHPLB_CACHE_E4M3 0
 #define SHPLB_CACHE_INT8 1
 

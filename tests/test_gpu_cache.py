@@ -231,6 +231,30 @@ def test_attn_many_short_sequences():
 
 
 @FORMATS
+@pytest.mark.parametrize("tokens", [1, 5, 9, 17, 33, 80])
+@pytest.mark.parametrize("room", [None, 64])
+def test_attn_weights_in_place(room, tokens, fmt):
+    # added to where they come from, bit for bit what goes elsewhere: 4 to 320 rows, those behind the 128th added to what the others left
+    rng = np.random.default_rng([tokens, fmt])
+    c = filled(rng, [[700, 321], [130, 1025]], 64, fmt, max_pages=room)
+    q, q64 = bf16(rng.standard_normal((2 * tokens, 8, D)))
+    dev = Device(c)
+    step, cu = step_of(dev, [tokens] * 2, 8, False)
+    w = rng.random((2, 2, c.capacity)).astype(np.float32)
+    out, lse, elsewhere = run_attn(c, q, cu, dev, step, w)
+    check_attn(c, out, lse, q64, cu, [h // 4 for h in range(8)], got_weight=elsewhere, weight_in=w)
+    here = torch.from_numpy(w).to(DEV)
+    o = torch.empty((2 * tokens, 8, D), dtype=torch.bfloat16, device=DEV)
+    for _ in range(3):
+        here.copy_(torch.from_numpy(w))
+        S.shplb_cache_attn(dev.cache, step, q.to(DEV), o, None, here, here, attn_workspace(dev, step), stream())
+        there = np.arange(c.capacity) < c.lens[..., None]
+        np.testing.assert_array_equal(here.double().cpu().numpy()[there], elsewhere[there])
+        np.testing.assert_array_equal(here.cpu().numpy()[~there], w[~there])
+        np.testing.assert_array_equal(o.double().cpu().numpy(), out)
+
+
+@FORMATS
 @pytest.mark.parametrize("tokens", [2, 11])
 def test_attn_few_of_many_sequences(tokens, fmt):
     # 700 sequences of which seven have tokens in this step, the first and the last among them, and a KV head without query heads
