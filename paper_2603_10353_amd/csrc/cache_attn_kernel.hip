@@ -89,17 +89,6 @@ __device__ __forceinline__ void pair_units(const CacheAttnArgs& a, int rows, int
   }
 }
 
-// Sums over the lanes up to and with one's own.
-__device__ __forceinline__ int lane_sums(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // from 1, 2, 4, 8 lanes below in the row of 16
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // the last lane of a row to the next one, of 32 to the others
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
-
 // The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more than `few` of them.  Up to 512 pairs every wave adds them up by itself, a lane a run of
 // them; beyond, the four waves do it together, and each looks for its place in the run where it lies, 64 pairs at a time.  (All
 // units, beginnings and all, are below 2^30: the entry point sees to that.)

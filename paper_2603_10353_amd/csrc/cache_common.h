@@ -73,12 +73,22 @@ int64_t cache_evict_workspace(const CacheArgs& c);
 int32_t cache_attn_rows(int64_t most_rows);
 int32_t launch_cache_attn(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
 
-
 // A load of what no kernel of the launch writes, at an address that is the same in all lanes: by way of the scalar cache, which leaves
 // the vector loads in flight alone.
 template <typename T>
 __device__ __forceinline__ T scalar_load(const T* p) {
   return *reinterpret_cast<const __attribute__((address_space(4))) T*>(reinterpret_cast<uintptr_t>(p));
+}
+
+// Sums over the lanes up to and with one's own.
+__device__ __forceinline__ int lane_sums(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // from 1, 2, 4, 8 lanes below in the row of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // the last lane of a row to the next one, of 32 to the others
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
 }
 
 // The rows of sequence s in this step (SCALAR: s is the same in all lanes).

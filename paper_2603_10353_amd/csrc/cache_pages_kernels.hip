@@ -161,8 +161,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 //
 // Of caches of up to 2 kRun positions a head is one workgroup's, from the first count to the last token written.  Longer
 // heads are cut into parts of up to kRun positions, and counting, counting, counting and writing are launches of their own: each begins by adding
-// up what the parts of its head counted in the launch before.  (8 heads of 13269 tokens: 19 us by one workgroup each, 28 and what lies
-// between launches in two parts; of 32525 35, and 29 in four; of 131072 195, and 30.)
+// up what the parts of its head counted in the launch before.  (8 heads of 13269 tokens: 15 us by one workgroup each, 25 and what lies
+// between launches in two parts; of 32525 53, with more weights than registers, and 26 in four; of 131072 28.)
 constexpr int kBins = 2048, kEach = 8;                           // bins of a count, weights that a thread holds (of one workgroup's heads up to kMostEach)
 constexpr int kSelectThreads = 1024, kFewThreads = 256, kMostEach = 16, kRun = kSelectThreads * kEach;
 static_assert((int64_t(SHPLB_MAX_BLOCKS) * 128 + kRun - 1) / kRun * SHPLB_MAX_SEQ_HEADS * kSelectThreads <= int64_t(UINT32_MAX), "a grid for all parts");
@@ -199,10 +199,16 @@ __device__ __forceinline__ Plan plan_of(const SelectArgs& a, int pair) {
 }
 
 struct SelectLds {
-  uint32_t bins[kBins];
-  uint64_t sums[kSelectThreads / 64];
+  alignas(16) uint32_t bins[kBins];
+  int sums[2][kSelectThreads / 64];
   uint32_t picked[4];
 };
+
+// Of sums that every wave has left in LDS, those of the waves in front of one's own, added up.
+__device__ __forceinline__ int waves_in_front(const int (&sums)[kSelectThreads / 64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  return __builtin_amdgcn_readlane(lane_sums(lane < wave ? sums[lane] : 0), 63);
+}
 
 __device__ __forceinline__ int pass_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
 __device__ __forceinline__ uint32_t pass_mask(int pass) { return pass == 0 ? 0u : pass == 1 ? 0xffe00000u : 0xfffffc00u; }
@@ -211,7 +217,7 @@ __device__ __forceinline__ uint32_t pass_mask(int pass) { return pass == 0 ? 0u 
 // p + 64 i, of which those in [first, last) count.
 template <int THREADS, int EACH>
 __device__ __forceinline__ void count_keys(const float (&x)[EACH], int p, int first, int last, int pass, uint32_t threshold, SelectLds& lds) {
-  for (int b = threadIdx.x; b < kBins; b += THREADS) lds.bins[b] = 0;
+  for (int b = threadIdx.x; b < kBins / 4; b += THREADS) reinterpret_cast<u32x4*>(lds.bins)[b] = u32x4{0, 0, 0, 0};
   __syncthreads();
   const uint32_t mask = pass_mask(pass), low = pass == 2 ? 1023 : 2047;
   const int shift = pass_shift(pass);
@@ -225,22 +231,24 @@ __device__ __forceinline__ void count_keys(const float (&x)[EACH], int p, int fi
 
 // Finds the bin of the want-th key from the top: `all` are the keys of all parts in the thread's bins, `front` those of the parts in front.
 // Writes the bin, how many keys lie above it, how many of those in the parts in front, and how many of these at it.
-template <int PER>
+template <bool FRONT, int PER>
 __device__ __forceinline__ void pick_bin(const uint32_t (&all)[PER], const uint32_t (&front)[PER], uint32_t want, SelectLds& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint64_t mine = 0;
+  int mine = 0, mine_front = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) mine += uint64_t(front[i]) << 32 | all[i];
-  uint64_t sum = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t up = __shfl_up((unsigned long long)sum, d);
-    if (lane >= d) sum += up;
+  for (int i = 0; i < PER; ++i) {
+    mine += all[i];
+    mine_front += front[i];
   }
-  if (lane == 63) lds.sums[wave] = sum;
+  int sum = lane_sums(mine), sum_front = FRONT ? lane_sums(mine_front) : 0;
+  if (lane == 63) {
+    lds.sums[0][wave] = sum;
+    if (FRONT) lds.sums[1][wave] = sum_front;
+  }
   __syncthreads();
-  for (int x = 0; x < wave; ++x) sum += lds.sums[x];
-  uint32_t above = uint32_t(sum - mine), above_front = uint32_t((sum - mine) >> 32);
+  sum += waves_in_front(lds.sums[0]);
+  if (FRONT) sum_front += waves_in_front(lds.sums[1]);
+  uint32_t above = sum - mine, above_front = sum_front - mine_front;
   if (above < want && uint32_t(sum) >= want) {                   // one thread; its bins from the top
     bool search = true;
 #pragma unroll
@@ -298,7 +306,11 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
       if (kAll) {
         count_keys<THREADS, EACH>(x, mine, first, last, pass, threshold, lds);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) n[i] = lds.bins[kBins - 1 - (kPer * tid + i)];
+        for (int i = 0; i < kPer; i += 2) {
+          const u32x2 two = *reinterpret_cast<const u32x2*>(lds.bins + (kBins - kPer - kPer * tid) + (kPer - 2 - i));
+          n[i] = two.y;
+          n[i + 1] = two.x;
+        }
       } else {
         static_assert(kAll || kPer == 2, "eight bytes of each part");
         const uint32_t* from = a.bins + (int64_t(pair) * parts * 3 + pass) * kBins + (kBins - kPer - kPer * tid);
@@ -315,12 +327,11 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
             }
         }
       }
-      pick_bin<kPer>(n, front, want, lds);
+      pick_bin<!kAll>(n, front, want, lds);
       threshold |= lds.picked[0] << pass_shift(pass);
       want -= lds.picked[1];
       above_front += lds.picked[2];
       equal_front = lds.picked[3];
-      __syncthreads();
     }
     ties = want;
     if (!kAll && STAGE < 3) {
@@ -344,17 +355,16 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(SelectArgs a) {
     above += there && (forced || key > threshold);
     equal += there && !forced && key == threshold;
   }
-  uint64_t both = uint64_t(equal) << 32 | above;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) both += __shfl_xor((unsigned long long)both, d);
-  if (lane == 0) lds.sums[wave] = both;
-  __syncthreads();
-  above = above_front + (all ? begin : min(begin, plan.from) + max(begin - plan.to, 0));
-  equal = equal_front;
-  for (int x = 0; x < wave; ++x) {
-    above += uint32_t(lds.sums[x]);
-    equal += uint32_t(lds.sums[x] >> 32);
+  // (a wave has up to 64 EACH of both)
+  static_assert(64 * EACH < 0x10000, "both in 32 bits");
+  const int both = lane_sums(int(equal << 16 | above));
+  if (lane == 63) {
+    lds.sums[0][wave] = both & 0xffff;
+    lds.sums[1][wave] = int(uint32_t(both) >> 16);
   }
+  __syncthreads();
+  above = above_front + (all ? begin : min(begin, plan.from) + max(begin - plan.to, 0)) + waves_in_front(lds.sums[0]);
+  equal = equal_front + waves_in_front(lds.sums[1]);
   const int64_t row = int64_t(pair) * a.dst.max_pages << a.dst.block_log2;
   const uint64_t below = (uint64_t(1) << lane) - 1;
 #pragma unroll
@@ -486,7 +496,7 @@ int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int3
   const SelectArgs a{src, dst, weight, keep, n_sink, n_recent, parts, weight_out, kept, bins, bins + pairs * parts * 3 * kBins};
   const dim3 all(uint32_t(pairs * parts));
   if (parts == 1) {
-    // as few threads and weights of each as there can be (48 sequences x 4 heads of up to 2000 tokens: 13 us with 1024 threads, 9 with 256)
+    // as few threads and weights of each as there can be (48 sequences x 4 heads of up to 2000 tokens: 7.8 us with 1024 threads, 7.3 with 256)
     const int64_t capacity = int64_t(src.max_pages) << src.block_log2;
     if (capacity <= kFewThreads * kEach) evict_select_kernel<-1, kFewThreads, kEach><<<all, kFewThreads, 0, stream>>>(a);
     else if (capacity <= kRun) evict_select_kernel<-1, kSelectThreads, kEach><<<all, kSelectThreads, 0, stream>>>(a);
