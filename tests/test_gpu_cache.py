@@ -484,6 +484,57 @@ def test_damaged_pages_lengths_and_offsets(room):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("which", ["k", "v", "number"])
+@pytest.mark.parametrize("hq,tokens", [(1, 5), (8, 5), (8, 20)])
+@pytest.mark.parametrize("room", [None, 64])
+def test_rows_that_see_nothing_of_a_damaged_page(room, hq, tokens, which):
+    # the last page has no scale, or is none: rows that see none of it are as if it were not there, their weights, too
+    rng = np.random.default_rng([hq, tokens])
+    c = filled(rng, [[130], [64 + 2]], 64, orc.INT8, max_pages=room)
+    for s, i in ((0, 2), (1, 1)):
+        if which == "number":
+            c.table[s, 0, i] = c.n_pages
+        else:
+            (c.k_scale if which == "k" else c.v_scale)[c.table[s, 0, i]] = np.nan
+    dev = Device(c)
+    q, q64 = bf16(rng.standard_normal((2 * tokens, hq, D)))
+    step, cu = step_of(dev, [tokens] * 2, hq, False)
+    w = rng.random((2, 1, c.capacity)).astype(np.float32)
+    out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+    check_attn(c, out, lse, q64, cu, [0] * hq, got_weight=w_out, weight_in=w)
+    seen = np.array([tokens - 2, tokens - 1, 2 * tokens - 2, 2 * tokens - 1])
+    assert np.isnan(out[seen]).all() and np.isfinite(np.delete(out, seen, 0)).all()
+
+
+@FORMATS
+def test_heads_apart(fmt):
+    # heads further from one another than their 128 dims, rows further than their heads, at addresses of 16 bytes
+    rng = np.random.default_rng([26, fmt])
+    hq, hkv, n, far = 4, 2, 5, 152
+    apart = lambda heads: (torch.full((3 * n * (heads + 1) * far + 8,), 9.0, dtype=torch.bfloat16, device=DEV)[8:]
+                           .view(3 * n, heads + 1, far)[:, :heads, :D])
+    c = filled(rng, [[100, 30], [n, 64], [300, 299]], 64, fmt, spare=1)
+    dev = Device(c)
+    (k, k64), (v, v64) = (bf16(rng.standard_normal((3 * n, hkv, D))) for _ in "kv")
+    q, q64 = bf16(rng.standard_normal((3 * n, hq, D)))
+    kd, vd, qd, od, bk, bv = (apart(x) for x in (hkv, hkv, hq, hq, hkv, hkv))
+    kd.copy_(k), vd.copy_(v), qd.copy_(q)
+    step, cu = step_of(dev, [n] * 3, hq, False, q_stride_h=far, q_stride_t=(hq + 1) * far, kv_stride_h=far, kv_stride_t=(hkv + 1) * far)
+    S.shplb_cache_append(dev.cache, step, kd, vd, stream())
+    orc.append(c, k64, v64, cu)
+    dev.check_same(c)
+    S.shplb_cache_load(dev.cache, step, bk, bv, stream())
+    want = [np.full((3 * n, hkv, D), 9.0) for _ in "kv"]
+    orc.load(c, *want, cu)
+    np.testing.assert_array_equal(bk.double().cpu().numpy(), want[0])
+    np.testing.assert_array_equal(bv.double().cpu().numpy(), want[1])
+    S.shplb_cache_attn(dev.cache, step, qd, od, None, None, None, attn_workspace(dev, step), stream())
+    check_attn(c, od.double().cpu().numpy(), None, q64, cu, [0, 0, 1, 1])
+    for x, heads in ((od, hq), (bk, hkv)):               # what lies between the heads is as it was
+        whole = torch.as_strided(x, (3 * n, heads + 1, far), ((heads + 1) * far, far, 1))
+        assert (whole[:, :, D:] == 9).all() and (whole[:, heads] == 9).all()
+
+
 def test_pages_far_into_a_pool():
     # byte offsets beyond 32 bits: a pool of 4.9 GB of keys and as much of values, of which the last pages are used
     n_pages = 300000
