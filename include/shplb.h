@@ -356,7 +356,8 @@ SHPLB_API int32_t shplb_cache_load(const shplb_cache* cache, const shplb_step* s
  * last one all of them.  Products of bf16 queries and 8-bit codes are exact, sums,
  * softmax and its statistics fp32, probabilities are rounded to fp16 before they meet the
  * values.  (Sums are taken at 2^7 times their size or more: values whose magnitude times the head's tokens is beyond 2^112 may
- * come out as infinity.)  A query that sees no token has the output 0 and the denominator's logarithm -inf.
+ * come out as infinity.)  A query that sees no token has the output 0 and the denominator's logarithm -inf; one whose
+ * products with the keys it sees are not finite has NaN, and so has the weight of those keys.
  *   q: device bf16 [n_tokens, n_q_heads, 128]; out: likewise, strides as Q, in other memory.
  *   lse_out: device fp32 [n_q_heads, n_tokens], natural logarithm of the softmax denominators, or NULL.
  *   weight_in, weight_out: device fp32 [n_seq][n_kv_heads][max_pages * block]:

@@ -525,6 +525,15 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
   }
 }
 
+// 1 / denominator of a row: 0 of one that sees nothing, so that its output is; of a head whose length cannot be, NaN.  A row that sees
+// tokens and whose products are all -inf (a query that is not finite) has 1 / 0, which makes NaN of its output, its weights and its logarithm.
+__device__ __forceinline__ float row_inverse(bool good, int sees, float sum) {
+  return !good ? __uint_as_float(kNanBits) : sees > 0 ? 1.0f / sum : 0.0f;
+}
+__device__ __forceinline__ float row_lse(float top, float sum, float inv) {
+  return (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f + 0.0f * inv;
+}
+
 // Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a workgroup, which
 // take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.  (For 128 rows x 8 heads x
 // 32768 int8 tokens 41 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.  Tiles side by side in a workgroup,
@@ -578,7 +587,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     // what a whole row has beside its output; of a length that cannot be all is NaN
     const auto row_done = [&](int j, int head, float top, float sum, float inv) {
       if (a.lse != nullptr)
-        a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = good ? (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f : inv;
+        a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = row_lse(top, sum, inv);
       if (a.weight_out != nullptr)
         *reinterpret_cast<f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head)) = f32x2{(top == -INFINITY ? 0.0f : top) - kLift, inv};
     };
@@ -591,7 +600,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
         if (row >= n * group) continue;
         if (whole) {
           const int j = row / group, head = group_head(a.groups, h, row - j * group);
-          const float inv = !good ? __uint_as_float(kNanBits) : r.l[nt] == 0.0f ? 0.0f : 1.0f / r.l[nt];
+          const float inv = row_inverse(good, len - n + 1 + j, r.l[nt]);
           uint16_t* dst = a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + quad * 32;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -642,7 +651,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
           }
           if (whole) {
             const int j = row / group, head = group_head(a.groups, h, row - j * group);
-            const float inv = !good ? __uint_as_float(kNanBits) : sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float inv = row_inverse(good, len - n + 1 + j, sum);
             *reinterpret_cast<u32x4*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d) =
                 u32x4{pack_bf16(o0.x * inv, o0.y * inv), pack_bf16(o0.z * inv, o0.w * inv), pack_bf16(o1.x * inv, o1.y * inv), pack_bf16(o1.z * inv, o1.w * inv)};
             if (d == 0) row_done(j, head, top, sum, inv);
@@ -737,11 +746,11 @@ __global__ __launch_bounds__(THREADS) void cache_join_kernel(CacheAttnArgs a, in
 #pragma unroll
   for (int x = 1; x < min(kGroups, kGroups > 8 ? 4 : 8); ++x) o += lds_o[x][d4];
   const int j = row / group, head = group_head(a.groups, h, row - j * group);
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float inv = row_inverse(true, a.c.lens[pair] - n + 1 + j, sum);     // (of a length that cannot be there are no pieces)
   *reinterpret_cast<u32x2*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d4 * 4) =
       u32x2{pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)};
   if (tid == 0) {
-    if (a.lse != nullptr) a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f;
+    if (a.lse != nullptr) a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = row_lse(top, sum, inv);
     if (a.weight_out != nullptr)
       *reinterpret_cast<f32x2*>(a.stats + 2 * ((int64_t(row0) + j) * a.n_q_heads + head)) = f32x2{ref - kLift, inv};
   }
@@ -1008,12 +1017,12 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
       o += x * *reinterpret_cast<const f32x4*>(&lds_o[w][row][d]);
     }
     const int j = row / group, head = group_head(a.groups, h, row - j * group);
-    const float inv = !good ? __uint_as_float(kNanBits) : sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = row_inverse(good, seen_before + j, sum);
     *reinterpret_cast<u32x2*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d) =
         u32x2{pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)};
     if (d == 0) {
       if (a.lse != nullptr)
-        a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = good ? (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f : inv;
+        a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = row_lse(top, sum, inv);
       lds_ref[row] = ref - kLift;
       lds_inv[row] = inv;
     }
@@ -1029,6 +1038,12 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
         float p[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(kept[x][e >> 2][e & 3] - m) * inv;
+        const int key0 = (wave + x * kWholeWaves) * kUnit;
+        if (key0 + kUnit > seen_before) {                        // (1 / denominator may be NaN: keys that a row does not see are none of its business)
+          const int seen = lds.seen(0, lane);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = key0 + (e >> 2) * 16 + quad * 4 + (e & 3) < seen ? p[e] : 0.0f;
+        }
         sum = sums_of_rows(p, lane);
       }
       const int at = key + x * kWholeWaves * kUnit;

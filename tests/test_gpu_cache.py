@@ -507,6 +507,33 @@ def test_rows_that_see_nothing_of_a_damaged_page(room, hq, tokens, which):
 
 
 @FORMATS
+@pytest.mark.parametrize("tokens", [3, 20])
+@pytest.mark.parametrize("room", [None, 64])
+def test_queries_that_are_not_finite(room, tokens, fmt):
+    # an infinity that meets keys of both signs, of one sign, or none at all, and a NaN: what it reaches is NaN, the other rows are as they are
+    rng = np.random.default_rng([tokens, fmt])
+    lens = np.array([[150], [400], [tokens - 2], [200]])
+    c = state(rng, lens, 64, fmt, max_pages=room)
+    cu = np.concatenate([[0], np.cumsum(lens[:, 0])])
+    (k, _), (v, v64) = (bf16(rng.standard_normal((int(cu[-1]), 1, D))) for _ in "kv")
+    k[:, 0, 7] = -k[:, 0, 7].abs() - 0.5                 # never zero, always negative
+    orc.append(c, k.double().numpy(), v64, cu)
+    q, _ = bf16(rng.standard_normal((4 * tokens, 4, D)))
+    q[1, 0, 7], q[2, 3, 7], q[2, 2, 9] = np.inf, -np.inf, np.inf
+    q[2 * tokens + 1, 0, 7] = np.inf                     # sees nothing
+    q[3 * tokens, 1, 0] = np.nan
+    dev = Device(c)
+    step, cu = step_of(dev, [tokens] * 4, 4, False)
+    w = np.zeros((4, 1, c.capacity), np.float32)
+    with np.errstate(invalid="ignore"):
+        out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+        check_attn(c, out, lse, q.double().numpy(), cu, [0] * 4, got_weight=w_out, weight_in=w)
+    bad = np.isnan(out).all(2)
+    assert bad.sum() == 4 and bad[1, 0] and bad[2, 3] and bad[2, 2] and bad[3 * tokens, 1] and not np.isnan(out[~bad]).any()
+    assert (out[2 * tokens + 1] == 0).all() and np.isneginf(lse[:, 2 * tokens + 1]).all()
+
+
+@FORMATS
 def test_heads_apart(fmt):
     # heads further from one another than their 128 dims, rows further than their heads, at addresses of 16 bytes
     rng = np.random.default_rng([26, fmt])
