@@ -674,17 +674,21 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
 }
 
 // Joins the pieces of one row of an item: with M the largest m, out = sum 2^(m - M) O / sum 2^(m - M) l.  A workgroup a row (y) of an
-// item (x).  The first piece lies in slot 2 w + 1 of the share w it begins in, the others in 2 (w + 1), 2 (w + 2) ...; groups of
+// item (x), or, where there are many of few pieces, a wave (THREADS = 64, four of them in a workgroup: a grid of 32768 rows, of which most have
+// nothing to join, takes 8 us, 10 with a workgroup each).  The first piece lies in slot 2 w + 1 of the share w it begins in, the others in 2 (w + 1), 2 (w + 2) ...; groups of
 // 32 lanes take turns at the pieces, a lane four dims, and what they have is added up in order.  What the first pieces hold is asked for
 // together with the statistics.
+constexpr int join_threads(int threads) { return threads > 64 ? threads : kThreads; }
+
 template <int THREADS>
-__global__ __launch_bounds__(THREADS) void cache_join_kernel(CacheAttnArgs a, int rows_per_tile) {
+__global__ __launch_bounds__(join_threads(THREADS)) void cache_join_kernel(CacheAttnArgs a, int rows_per_tile) {
   constexpr int kGroups = THREADS / 32;
   constexpr bool kShared = THREADS > 64;       // each piece's statistics are read by one thread and shared
   __shared__ float lds_m[kShared ? kCacheMaxWorkers : 1], lds_l[kShared ? kCacheMaxWorkers : 1];
-  __shared__ f32x4 lds_o[kGroups][32];
-  const int tid = threadIdx.x, lane = tid & 63, d4 = tid & 31, part = tid >> 5;
-  const int pair = blockIdx.x / uint32_t(a.tiles), tile = blockIdx.x - pair * a.tiles, in_tile = blockIdx.y, row = tile * rows_per_tile + in_tile;
+  __shared__ f32x4 lds_o[kShared ? kGroups : 1][32];
+  const int tid = kShared ? threadIdx.x : threadIdx.x & 63, lane = tid & 63, d4 = tid & 31, part = tid >> 5;
+  const int pair = blockIdx.x / uint32_t(a.tiles), tile = blockIdx.x - pair * a.tiles;
+  const int in_tile = kShared ? int(blockIdx.y) : int(blockIdx.y) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = tile * rows_per_tile + in_tile;
   const int2 begun = *reinterpret_cast<const int2*>(a.begun + 2 * int64_t(blockIdx.x));
   const int s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads, group = group_size(a.groups, h);
   int row0, n;
@@ -731,8 +735,13 @@ __global__ __launch_bounds__(THREADS) void cache_join_kernel(CacheAttnArgs a, in
     if (part + kGroups * x < pieces) o += __builtin_amdgcn_exp2f((kShared ? lds_m[part + kGroups * x] : early_m[x]) - ref) * early[x];
 #pragma unroll 8
   for (int x = part + kGroups * kEarly; x < pieces; x += kGroups) o += __builtin_amdgcn_exp2f(m(x) - ref) * values(x);
-  lds_o[part][d4] = o;
-  __syncthreads();
+  if constexpr (!kShared) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], 32);
+  } else {
+    lds_o[part][d4] = o;
+    __syncthreads();
+  }
   if constexpr (kGroups > 8) {
     if (part < 4) {
 #pragma unroll
@@ -743,8 +752,10 @@ __global__ __launch_bounds__(THREADS) void cache_join_kernel(CacheAttnArgs a, in
     __syncthreads();
   }
   if (tid >= 32) return;
+  if constexpr (kShared) {
 #pragma unroll
-  for (int x = 1; x < min(kGroups, kGroups > 8 ? 4 : 8); ++x) o += lds_o[x][d4];
+    for (int x = 1; x < min(kGroups, kGroups > 8 ? 4 : 8); ++x) o += lds_o[x][d4];
+  }
   const int j = row / group, head = group_head(a.groups, h, row - j * group);
   const float inv = row_inverse(true, a.c.lens[pair] - n + 1 + j, sum);     // (of a length that cannot be there are no pieces)
   *reinterpret_cast<u32x2*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d4 * 4) =
@@ -813,10 +824,10 @@ __device__ __forceinline__ float weigh_unit(const CacheAttnArgs& a, int key0, co
   return sums_of_rows(w, lane);
 }
 
-// weight_out = before + those of units first .. end - 1 (any: whether there is a row).
+// weight_out = before + those of units first .. end - 1.
 template <int FMT>
 __device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first,
-                                      const f16x8 (*lds_q)[4][64], const float* before, int lane, Flight& f, const Statistics<1>& r, bool any) {
+                                      const f16x8 (*lds_q)[4][64], const float* before, int lane, Flight& f, const Statistics<1>& r) {
   const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
   for (int u = first; u < end; ++u) {
     const Page ahead = page_at(a.c, f.page_next, min(u + 1, last));
@@ -824,7 +835,7 @@ __device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len,
     const int key = u * kUnit + key_of_lane(lane);
     float old = 0.0f;
     if (before != nullptr && key < len) old = before[row_of_weights + key];
-    const float sum = any ? weigh_unit<1, FMT>(a, u * kUnit, ahead, u + 1 < end, seen_first, lds_q, lane, f, r) : 0.0f;
+    const float sum = weigh_unit<1, FMT>(a, u * kUnit, ahead, u + 1 < end, seen_first, lds_q, lane, f, r);
     if (key < len) a.weight_out[row_of_weights + key] = old + sum;
   }
 }
@@ -862,6 +873,13 @@ __device__ __forceinline__ void begin_weights(const CacheAttnArgs& a, int pair, 
   }
 }
 
+// Weights of keys first .. end - 1 of a head that has no rows in this step: what they were.
+__device__ __forceinline__ void copy_weights(const CacheAttnArgs& a, int64_t row_of_weights, int first, int end, int me, int threads) {
+  if (a.weight_in == a.weight_out) return;
+#pragma unroll 4
+  for (int key = first + me; key < end; key += threads) a.weight_out[row_of_weights + key] = a.weight_in != nullptr ? a.weight_in[row_of_weights + key] : 0.0f;
+}
+
 // The weights of the step by themselves, taken again from the keys and the rows' statistics: every key belongs to one share, so nothing is added up
 // between workgroups.  Up to 16 rows every wave has a share.
 template <int FMT>
@@ -880,10 +898,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
     const int len = it.len, group = group_size(a.groups, h), rows = n * group;
     pair_units<true, 1>(a, rows, len, tiles, units);
     const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at)), last = max(u1 - 1, 0);
-    Flight f;
-    Statistics<1> r;
-    begin_weights<1>(a, pair, h, group, row0, n, 0, len, u0, 1, u1, last, lane, lds_q[wave], f, r);
-    weigh<FMT>(a, pair, len, u0, u1, last, len - n + 1, lds_q[wave], a.weight_in, lane, f, r, rows > 0);
+    if (rows == 0) {
+      copy_weights(a, int64_t(pair) * a.c.max_pages << a.c.block_log2, u0 * kUnit, min(u1 * kUnit, len), lane, 64);
+    } else {
+      Flight f;
+      Statistics<1> r;
+      begin_weights<1>(a, pair, h, group, row0, n, 0, len, u0, 1, u1, last, lane, lds_q[wave], f, r);
+      weigh<FMT>(a, pair, len, u0, u1, last, len - n + 1, lds_q[wave], a.weight_in, lane, f, r);
+    }
     at += units - it.unit;
     it = next_pair<kStart>(a, pair);
   }
@@ -911,10 +933,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
     pair_units<true, 1>(a, rows, len, tiles, units);
     const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
     const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
-    for (int first_row = 0; u0 < u1 && (first_row == 0 || first_row < rows); first_row += kWaves * kSlice) {
+    if (rows == 0) copy_weights(a, row_of_weights, u0 * kUnit, min(u1 * kUnit, len), tid, kThreads);
+    for (int first_row = 0; u0 < u1 && first_row < rows; first_row += kWaves * kSlice) {
       const int left = rows - first_row, log2 = left > 2 * kSlice ? 2 : left > kSlice ? 1 : 0, slices = 1 << log2, step = kWaves >> log2;
       const int phase = wave >> log2, my_row = first_row + (wave & (slices - 1)) * kSlice;
-      const int seen_first = len - n + 1 + my_row / max(group, 1);
+      const int seen_first = len - n + 1 + my_row / group;
       const float* before = first_row == 0 ? a.weight_in : a.weight_out;
       Flight f;
       Statistics<2> r;
@@ -1072,7 +1095,7 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
     const dim3 all(pairs * a.tiles, min(rows, most_rows));
     if (int64_t(all.x) * all.y <= 256) cache_join_kernel<1024><<<all, 1024, 0, stream>>>(a, rows);
     else if (int64_t(all.x) * all.y < 2048) cache_join_kernel<256><<<all, 256, 0, stream>>>(a, rows);
-    else cache_join_kernel<64><<<all, 64, 0, stream>>>(a, rows);
+    else cache_join_kernel<64><<<dim3(all.x, (all.y + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, stream>>>(a, rows);
   }
   if (a.weight_out != nullptr) {
     if (rows == 16) cache_weight_kernel<FMT><<<grid, kThreads, 0, stream>>>(a);
