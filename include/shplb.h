@@ -300,7 +300,7 @@ SHPLB_API int32_t shplb_token_recovery_heads(const shplb_problem* p, const float
  * Errors of all calls: SHPLB_E_NULL; SHPLB_E_SHAPE (a size smaller than stated, strides smaller than what they step
  * over or no multiple of 8, tensors and pages not aligned to 16 bytes, other arrays not to their elements);
  * SHPLB_E_UNSUPPORTED (a size larger than stated, element strides from 2^24 on, 2^23 pages or more that a call may touch; in
- * attention 2^24 rows of a KV head, 2^26 tiles of 32 rows, or 2^30 units of 64 tokens, of the page tables' capacity, a tile
+ * attention 2^24 rows of a KV head, 2^24 tiles of 32 rows, or 2^30 units of 64 tokens, of the page tables' capacity, a tile
  * counting eight more). */
 #define SHPLB_CACHE_E4M3 0
 #define SHPLB_CACHE_INT8 1

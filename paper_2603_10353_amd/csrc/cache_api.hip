@@ -61,10 +61,10 @@ int32_t check_queries(const shplb_cache* c, const shplb_step* t, HeadGroups* g, 
   }
   *most_rows = int64_t(most) * t->max_tokens;
   if (t->n_q_heads > SHPLB_MAX_SEQ_HEADS || *most_rows > (1 << 24)) return SHPLB_E_UNSUPPORTED;
-  // places in the list of all units are 32-bit numbers, and a grid has one workgroup of 64 threads for every row of a tile
+  // places in the list of all units are 32-bit numbers, and a grid, whose threads are, has workgroups of 256 for every tile
   const int rows = cache_attn_rows(*most_rows);
   const int64_t tiles = *most_rows > rows ? (*most_rows + rows - 1) / rows : 1, items = int64_t(c->n_seq) * c->n_kv_heads * tiles;
-  if (items >= int64_t(1) << 26 || items * (int64_t(c->max_pages) * c->block / 64 + kCacheMostStart) >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
+  if (items >= int64_t(1) << 24 || items * (int64_t(c->max_pages) * c->block / 64 + kCacheMostStart) >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
   return SHPLB_OK;
 }
 

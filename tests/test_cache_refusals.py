@@ -137,8 +137,8 @@ def test_strides_whose_product_is_past_64_bits():
 
 @pytest.mark.parametrize("n_seq,max_pages,max_tokens,fits", [
     (2048, 4096, 1, True), (8192, 4096, 32, True), (8192, 4096, 224, True), (8192, 4096, 256, False),       # units of 64 keys: below 2^30
-    (16000, 1, 34000, False), (8000, 1, 34000, True),                                                    # tiles of 32 rows: below 2^26
-    (16000, 1, 20000, True), (16000, 20, 20000, False),                                                  # ... and eight units more for each
+    (4000, 1, 34000, False), (3900, 1, 34000, True),                                                     # tiles of 32 rows: below 2^24
+    (4000, 58, 32000, True), (4000, 60, 32000, False),                                                   # ... and eight units more for each
 ])
 def test_most_that_attention_takes(n_seq, max_pages, max_tokens, fits):
     c = cache(n_seq=n_seq, n_kv_heads=4, max_pages=max_pages, block=64)
