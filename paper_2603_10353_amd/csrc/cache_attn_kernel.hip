@@ -14,8 +14,8 @@
 // lengths are: lengths differ between sequences, and between heads after an eviction.  A share is a wave's where a head has up to 16
 // rows, and a workgroup's where it has more (tiles of 32 rows).  The lengths are on the device (they change while a captured
 // launch stays), so each wave adds them up by itself.  A (sequence, KV head, tile of rows) whose units lie in several shares has
-// partial results (m, l, unnormalised output), which a second kernel joins in order.  Short caches of few heads are worked on head by head
-// in one launch.
+// partial results (m, l, unnormalised output), which a second kernel joins in order.  Short caches are worked on head by head or
+// item by item, without partial results.
 //
 // Tile.  A wave works on a unit at a time: keys are the rows of the first product (S^T = K Q^T), so a lane has scores of one query
 // and four adjacent keys of each 16; the second one is O^T = V^T P^T, whose operand P^T needs exactly those (the order of the keys
@@ -537,8 +537,8 @@ __device__ __forceinline__ float row_lse(float top, float sum, float inv) {
 // Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a workgroup, which
 // take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.  (For 128 rows x 8 heads x
 // 32768 int8 tokens 41 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.  Tiles side by side in a workgroup,
-// to read the codes from memory once, bring nothing.)
-template <int NT, int WAVES, int FMT>
+// to read the codes from memory once, bring nothing.)  ITEMS: no shares, a workgroup an item, for short caches.
+template <int NT, int WAVES, bool ITEMS, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a, int least) {
   constexpr bool kOwn = WAVES == 1;
   constexpr int kRows = 16 * NT, kStart = start_units(WAVES);
@@ -548,11 +548,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
   __shared__ float lds_m[WAVES][kRows], lds_l[WAVES][kRows];
   __shared__ int lds_i[kWaves + kThreads];
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  int at, end;
+  int at = 0, end = 1 << 30;
   Shares<!kOwn> shares;
   // neighbouring shares in different workgroups, on different compute units
   const int worker = kOwn ? int(blockIdx.x) + wave * int(gridDim.x) : int(blockIdx.x);
-  Item it = locate<false, kRows, kStart>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, kOwn ? int(gridDim.x) : 1, lds_i, at, end, shares);
+  Item it;
+  if constexpr (ITEMS) {
+    const int pair = worker / uint32_t(a.tiles);
+    it = {pair, scalar_load(a.c.lens + pair), worker - pair * a.tiles, 0};
+  } else {
+    it = locate<false, kRows, kStart>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, kOwn ? int(gridDim.x) : 1, lds_i, at, end, shares);
+  }
   while (at < end) {
     // (the lane as a number of which the compiler knows nothing: what follows from it is worked out here and again at the item's end, and
     // takes no registers in between)
@@ -563,6 +569,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     step_tokens<true>(a.t, s, row0, n);
     const int len = it.len, group = group_size(a.groups, h);
     pair_units<false, kRows>(a, n * group, len, tiles, units);
+    if (ITEMS && it.tile >= tiles) break;
     if (tiles == 0) {
       if (n > 0) it = next_pair<kStart>(a, pair);               // no query heads of this KV head
       else if (!next_sequence<kStart>(a, s, lane, it)) break;
@@ -582,7 +589,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     asm volatile("" : "+v"(tid));
     const int col = tid & 15, quad = (tid & 63) >> 4;
     // a lane has dims 8 (4 quad + i) + t of rows 16 nt + col
-    const bool whole = u0 == 0 && u1 == units;
+    const bool whole = ITEMS || (u0 == 0 && u1 == units);
     const int64_t slot_row = (2 * int64_t(worker) + (u0 == 0 ? 1 : 0)) * kRows;
     // what a whole row has beside its output; of a length that cannot be all is NaN
     const auto row_done = [&](int j, int head, float top, float sum, float inv) {
@@ -665,6 +672,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
       }
       __syncthreads();
     }
+    if (ITEMS) break;
     if (u0 == 0 && (kOwn ? (tid & 63) == 0 : tid == 0))         // for the joining kernel: pieces of the item, if it ends in another share
       *reinterpret_cast<int2*>(a.begun + 2 * (int64_t(pair) * a.tiles + it.tile)) = int2{worker, whole ? 0 : shares.of(at - it.unit + units - 1) - worker + 1};
     at += u1 - it.unit;
@@ -979,7 +987,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
 }
 
 // A head a workgroup, eight waves taking turns at its units: output, denominators and weights in one launch, without partial results.  For
-// up to 16 rows and as many heads as there are compute units, in caches that leave a wave no more than kWholeUnits units, whose products stay in
+// up to 16 rows and twice as many heads as there are compute units, in caches that leave a wave no more than kWholeUnits units, whose products stay in
 // registers until the weights can be told (48 sequences x 4 heads of up to 2000 tokens, 7 rows: 21 us with the keys gone through again, 15 so).
 constexpr int kWholeWaves = 8, kWholeUnits = 4;
 
@@ -1079,17 +1087,24 @@ template <int FMT>
 int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compute_units, hipStream_t stream) {
   const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2), pairs = a.c.n_seq * a.c.n_kv_heads;
   const int64_t capacity = int64_t(a.c.max_pages) << a.c.block_log2;
-  if (rows == 16 && pairs <= compute_units && capacity <= kWholeWaves * kWholeUnits * kUnit) {
+  constexpr int kShort = kWholeWaves * kWholeUnits * kUnit;
+  if (rows == 16 && pairs <= 2 * compute_units && capacity <= kShort) {
+    // (twice as many heads as compute units: 100 sequences x 4 heads of up to 1492 tokens with weights 18 us, and 13, 4 and 7 by shares; three times:
+    // 100 x 8 of up to 719 21, and 14 and 4)
     if (a.weight_out != nullptr) cache_whole_kernel<true, FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
     else cache_whole_kernel<false, FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
     return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
   }
-  if (a.t.n_tokens > 0) {
+  if (a.t.n_tokens > 0 && rows > 16 && capacity <= kShort) {
+    // item by item (48 sequences x 8 heads of up to 1498 tokens, 32 rows, 23 us, and 24 and 6 to join by shares; 100 x 8 of up to 615, 160 rows,
+    // 46, and 51 and 20; one of 900 x 8 heads, 128 rows, 14, and 11 and 4)
+    cache_attn_kernel<2, kWaves, true, FMT><<<uint32_t(pairs) * a.tiles, kThreads, 0, stream>>>(a, 0);
+  } else if (a.t.n_tokens > 0) {
     // (three units at least where there is more than one share for every workgroup: waves that share a compute unit wait for one another's beginnings, and
     // pieces are joined; five sequences of up to 39284 tokens x 2 heads 15 and 9 us with one unit, 13 and 5 with three, 12 and 5 with four; 16 up
     // to 8000 13 and 7, 11 and 5, 12 and 4; one of 2048 x 8 heads, 272 units, 7 and 4 with one, 10 and 4 with three)
-    if (rows == 16) cache_attn_kernel<1, 1, FMT><<<grid, kThreads, 0, stream>>>(a, 3);
-    else cache_attn_kernel<2, kWaves, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
+    if (rows == 16) cache_attn_kernel<1, 1, false, FMT><<<grid, kThreads, 0, stream>>>(a, 3);
+    else cache_attn_kernel<2, kWaves, false, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
     // few rows are of many pieces, many of few: 32 rows of 256 pieces (131072 tokens x 8 heads) take 6.6 us with 1024 threads each, 9 with 256; 4096 rows
     // of one to four 5.4 with 64, 7 with 256
     const dim3 all(pairs * a.tiles, min(rows, most_rows));

@@ -255,14 +255,14 @@ def test_attn_weights_in_place(room, tokens, fmt):
 
 
 @FORMATS
-@pytest.mark.parametrize("tokens", [2, 11])
-def test_attn_few_of_many_sequences(tokens, fmt):
+@pytest.mark.parametrize("tokens,room", [(2, None), (11, None), (11, 40)])
+def test_attn_few_of_many_sequences(tokens, room, fmt):
     # 700 sequences of which seven have tokens in this step, the first and the last among them, and a KV head without query heads
     rng = np.random.default_rng([tokens, fmt])
     new = np.zeros(700, int)
     new[[0, 1, 63, 64, 65, 400, 699]] = tokens
     lens = rng.integers(0, 150, size=(700, 3))
-    c = filled(rng, lens, 64, fmt)
+    c = filled(rng, lens, 64, fmt, max_pages=room)
     kv_of = [2, 0, 2]
     q, q64 = bf16(rng.standard_normal((int(new.sum()), 3, D)))
     dev = Device(c)
@@ -293,6 +293,21 @@ def test_attn_one_token_of_every_scale(room, fmt):
     want = np.stack([c.values("v", s, 0, 1)[0] for s in range(scales.size)])
     np.testing.assert_array_equal(out, np.stack([want, want], 1))
     assert (np.abs(w_out[:, 0, 0] - 2) <= 2 * 2.0 ** -20).all()
+
+
+@FORMATS
+@pytest.mark.parametrize("tokens", [1, 6])
+def test_attn_more_heads_than_compute_units(tokens, fmt):
+    # 110 sequences x 4 heads in short caches: a head a workgroup, or a tile of one, whatever finds a place first
+    rng = np.random.default_rng([tokens, fmt])
+    lens = np.maximum(rng.integers(0, 300, size=(110, 4)), np.where(np.arange(110) == 50, 1900, 0)[:, None])
+    c = filled(rng, lens, 128, fmt)
+    q, q64 = bf16(rng.standard_normal((110 * tokens, 16, D)))
+    dev = Device(c)
+    step, cu = step_of(dev, [tokens] * 110, 16, False)
+    w = rng.random((110, 4, c.capacity)).astype(np.float32)
+    out, lse, w_out = run_attn(c, q, cu, dev, step, w)
+    check_attn(c, out, lse, q64, cu, [h // 4 for h in range(16)], got_weight=w_out, weight_in=w)
 
 
 @pytest.mark.parametrize("room", [None, 64])
