@@ -1095,9 +1095,10 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
     else cache_whole_kernel<false, FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
     return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
   }
-  if (a.t.n_tokens > 0 && rows > 16 && capacity <= kShort) {
+  if (a.t.n_tokens > 0 && rows > 16 && (capacity <= kShort || (capacity <= 2 * kShort && int64_t(pairs) * a.tiles >= 2 * compute_units))) {
     // item by item (48 sequences x 8 heads of up to 1498 tokens, 32 rows, 23 us, and 24 and 6 to join by shares; 100 x 8 of up to 615, 160 rows,
-    // 46, and 51 and 20; one of 900 x 8 heads, 128 rows, 14, and 11 and 4)
+    // 46, and 51 and 20; one of 900 x 8 heads, 128 rows, 14, and 11 and 4), also twice as long if there are items for all compute units (100 x 2 of
+    // up to 2861, 128 rows, 35, and 34 and 7): one that is much longer than the others keeps a compute unit for 30 us
     cache_attn_kernel<2, kWaves, true, FMT><<<uint32_t(pairs) * a.tiles, kThreads, 0, stream>>>(a, 0);
   } else if (a.t.n_tokens > 0) {
     // (three units at least where there is more than one share for every workgroup: waves that share a compute unit wait for one another's beginnings, and

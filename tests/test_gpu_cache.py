@@ -255,7 +255,7 @@ def test_attn_weights_in_place(room, tokens, fmt):
 
 
 @FORMATS
-@pytest.mark.parametrize("tokens,room", [(2, None), (11, None), (11, 40)])
+@pytest.mark.parametrize("tokens,room", [(2, None), (11, None), (11, 80)])
 def test_attn_few_of_many_sequences(tokens, room, fmt):
     # 700 sequences of which seven have tokens in this step, the first and the last among them, and a KV head without query heads
     rng = np.random.default_rng([tokens, fmt])
