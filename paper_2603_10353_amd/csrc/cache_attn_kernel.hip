@@ -89,9 +89,9 @@ __device__ __forceinline__ void pair_units(const CacheAttnArgs& a, int rows, int
   }
 }
 
-// The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more than `few` of them.  Up to 512 pairs every wave adds them up by itself, a lane a run of
-// them; beyond, the four waves do it together, and each looks for its place in the run where it lies, 64 pairs at a time.  (All
-// units, beginnings and all, are below 2^30: the entry point sees to that.)
+// The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more than `few`
+// of them.  Up to 512 pairs every wave adds them up by itself, a lane a run of them; beyond, the four waves do it together, and each looks for
+// its place in the run where it lies, 64 pairs at a time.  (All units, beginnings and all, are below 2^30: the entry point sees to that.)
 template <bool WEIGHTS, int ROWS, int START, class SHARES>
 __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int few, int* lds, int& begin, int& end, SHARES& shares) {
   const int pairs = a.c.n_seq * a.c.n_kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

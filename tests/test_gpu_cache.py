@@ -674,6 +674,30 @@ def test_decoding_step_in_a_hip_graph(room):
         w64 = w.double().cpu().numpy()
 
 
+@pytest.mark.parametrize("n,length,tokens", [(1, 30000, 1), (3, 700, 40), (300, 65, 1), (1, 9000, 100)])
+def test_workspaces_end_where_they_say(n, length, tokens):
+    # what lies behind a workspace is as it was
+    rng = np.random.default_rng(n)
+    c = filled(rng, np.full((n, 2), length), 128, orc.E4M3, max_pages=300)
+    dev = Device(c)
+    step, _ = step_of(dev, [tokens] * n, 8, False)
+    q = torch.randn((n * tokens, 8, D), device=DEV).to(torch.bfloat16)
+    w = torch.zeros((n, 2, c.capacity), device=DEV)
+    to = state(rng, np.full((n, 2), 64), 64, orc.E4M3, spare=0)
+    dto = Device(to)
+    w_out = torch.zeros((n, 2, to.capacity), device=DEV)
+    kept = torch.zeros((n, 2, to.capacity), dtype=torch.int32, device=DEV)
+    keep = torch.full((n, 2), 60, dtype=torch.int32, device=DEV)
+    for size, call in (
+            (S.shplb_cache_attn_workspace_bytes(dev.cache, step),
+             lambda ws: S.shplb_cache_attn(dev.cache, step, q, torch.empty_like(q), None, None, w, ws, stream())),
+            (S.shplb_cache_evict_workspace_bytes(dev.cache),
+             lambda ws: S.shplb_cache_evict(dev.cache, w, keep, 1, 1, dto.cache, w_out, kept, ws, stream()))):
+        ws = torch.full((size + (1 << 20),), 0x5a, dtype=torch.uint8, device=DEV)
+        call(ws)
+        assert (ws[size:] == 0x5a).all()
+
+
 @FORMATS
 def test_two_graphs_of_one_workspace(fmt):
     # a decoding step and a prompt's window with the eviction behind it, captured each, share one workspace and take turns, with the
