@@ -578,7 +578,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     const bool good = good_length(a.c, len);
     const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
     if (u1 <= u0) break;                                         // the share ends before the item's first unit
-    const int first_row = it.tile * kRows, u_first = u0 + (kOwn ? 0 : wave), u_end = good && len > 0 ? u1 : 0;
+    const int first_row = it.tile * kRows, u_first = u0 + (kOwn ? 0 : wave);
+    int u_end = good && len > 0 ? u1 : 0;
+    // units behind what the tile's last row sees are none (a step that is a whole prompt: half of them)
+    if (!kOwn) u_end = min(u_end, (max(len - n + 1 + (min(first_row + kRows, n * group) - 1) / group, 0) + kUnit - 1) / kUnit);
     RowsLds<NT>& rows_lds = lds_rows[kOwn ? wave : 0];           // (waves of one share write the same)
     Flight f;
     Rows<NT> r;
@@ -945,7 +948,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
     for (int first_row = 0; u0 < u1 && first_row < rows; first_row += kWaves * kSlice) {
       const int left = rows - first_row, log2 = left > 2 * kSlice ? 2 : left > kSlice ? 1 : 0, slices = 1 << log2, step = kWaves >> log2;
       const int phase = wave >> log2, my_row = first_row + (wave & (slices - 1)) * kSlice;
-      const int seen_first = len - n + 1 + my_row / group;
+      const int seen_first = len - n + 1 + my_row / group, seen_last = my_row < rows ? len - n + 1 + (min(my_row + kSlice, rows) - 1) / group : 0;
       const float* before = first_row == 0 ? a.weight_in : a.weight_out;
       Flight f;
       Statistics<2> r;
@@ -966,7 +969,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
           const Page ahead = page_at(a.c, f.page_next, min(u + step, u1 - 1));
           f.page_next = page_number(a.c, pair, min(u + 2 * step, u1 - 1));
           float sum = 0.0f;
-          if (my_row < rows) sum = weigh_unit<2, FMT>(a, u * kUnit, ahead, u + step < u1, seen_first, lds_q[wave], lane, f, r);
+          if (u * kUnit < seen_last) sum = weigh_unit<2, FMT>(a, u * kUnit, ahead, u + step < u1, seen_first, lds_q[wave], lane, f, r);
           lds_w[i][wave][key_of_lane(lane)] = sum;
         }
         __syncthreads();
