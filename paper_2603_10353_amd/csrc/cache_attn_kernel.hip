@@ -230,8 +230,8 @@ __device__ __forceinline__ f16x8 key_operand(uint32_t x, uint32_t y) {
 __device__ __forceinline__ int page_number(const CacheArgs& c, int pair, int unit) {
   return scalar_load(c.table + int64_t(pair) * c.max_pages + (unit * kUnit >> c.block_log2));
 }
-// Where a unit's codes are: of a page that is not in the pool those of the first one, with scales of NaN.  (The scales
-// come later than the codes are asked for, and are looked at when they are used.)
+// Where a unit's codes are.  Those of a page that is not in the pool are not loaded, zeros with scales of NaN: codes that are NaN themselves would reach
+// rows that see none of them.  (The scales come later than the codes are asked for, and are looked at when they are used.)
 struct Page {
   int64_t byte;
   bool bad;
@@ -262,7 +262,7 @@ __device__ __forceinline__ SlotBuffer unit_buffer(const uint8_t* base, int64_t b
 // sequence of 131072 tokens 52 -> 46)
 template <bool kOnce>
 __device__ __forceinline__ void load_keys(const CacheAttnArgs& a, const Page& page, bool there, int lane_byte, Keys& x) {
-  const SlotBuffer k = unit_buffer(a.c.k, page.byte, there);
+  const SlotBuffer k = unit_buffer(a.c.k, page.byte, there && !page.bad);
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -271,7 +271,7 @@ __device__ __forceinline__ void load_keys(const CacheAttnArgs& a, const Page& pa
 }
 template <bool kOnce>
 __device__ __forceinline__ void load_values(const CacheAttnArgs& a, const Page& page, bool there, int lane_byte, Values& x) {
-  const SlotBuffer v = unit_buffer(a.c.v, page.byte, there);
+  const SlotBuffer v = unit_buffer(a.c.v, page.byte, there && !page.bad);
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk)
 #pragma unroll

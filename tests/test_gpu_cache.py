@@ -499,13 +499,20 @@ def test_damaged_pages_lengths_and_offsets(room):
     torch.cuda.synchronize()
 
 
+@FORMATS
 @pytest.mark.parametrize("which", ["k", "v", "number"])
 @pytest.mark.parametrize("hq,tokens", [(1, 5), (8, 5), (8, 20)])
 @pytest.mark.parametrize("room", [None, 64])
-def test_rows_that_see_nothing_of_a_damaged_page(room, hq, tokens, which):
-    # the last page has no scale, or is none: rows that see none of it are as if it were not there, their weights, too
+def test_rows_that_see_nothing_of_a_damaged_page(room, hq, tokens, which, fmt):
+    # the last page has no scale, or is none: rows that see none of it are as if it were not there, their weights, too, whatever the pool's first
+    # page holds
     rng = np.random.default_rng([hq, tokens])
-    c = filled(rng, [[130], [64 + 2]], 64, orc.INT8, max_pages=room)
+    c = filled(rng, [[130], [64 + 2]], 64, fmt, max_pages=room)
+    free = sorted(set(range(c.n_pages)) - set(c.table[c.table >= 0].tolist()))[-1]
+    for pages, scale in ((c.k_pages, c.k_scale), (c.v_pages, c.v_scale)):
+        pages[free], scale[free] = pages[0], scale[0]
+        pages[0] = 0x7f
+    c.table[c.table == 0] = free
     for s, i in ((0, 2), (1, 1)):
         if which == "number":
             c.table[s, 0, i] = c.n_pages
