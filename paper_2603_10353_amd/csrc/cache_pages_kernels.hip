@@ -432,12 +432,15 @@ __global__ __launch_bounds__(kThreads) void evict_gather_kernel(CacheArgs src, C
   for (int u = 0; u < 4; ++u) {
     const int slot = r + 32 * u;
     if (slot >= end) continue;
+    // A token of zeros may come from a scale 2^128 times the new one, or more: an infinite ratio would make NaN of it.  (Codes other
+    // than zero come from at most 448 * 2^9 times the new scale.)
+    const float ratio = fminf(scale[u] * inv, 0x1p127f);
     u32x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float y[4];
       from_codes<FMT>(in[u][e], y);
-      o[e] = none ? 0 : to_codes<FMT>(y[0], y[1], y[2], y[3], scale[u] * inv, last);
+      o[e] = none ? 0 : to_codes<FMT>(y[0], y[1], y[2], y[3], ratio, last);
     }
     *reinterpret_cast<u32x4*>(to + slot * kHeadDim + d) = o;
   }
