@@ -364,6 +364,8 @@ SHPLB_API int32_t shplb_cache_load(const shplb_cache* cache, const shplb_step* s
  *     weight_out[s][h][t] = weight_in[s][h][t] + the attention weights that all rows of the
  *     step (all its queries, all heads that read h) give token t, t < lens[s][h]; nothing is
  *     written behind.  weight_in may be weight_out, or NULL for zeros; both NULL: not computed.
+ *     weight_in is read for all of these tokens, the step's own among them: whoever keeps one
+ *     buffer fills it with zeros before its first call, or before eviction writes into it.
  *   workspace: device, shplb_cache_attn_workspace_bytes() (of this step or of one with at least as many n_tokens and
  *     max_tokens of the same heads), 256-byte aligned; needs no clearing; must not be shared with a call in flight on another
  *     stream.
@@ -384,7 +386,8 @@ SHPLB_API int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* s
  * may be another, its format not.
  *   weight: device fp32 [n_seq][n_kv_heads][max_pages * block]; keep: device int32 [n_seq][n_kv_heads].
  *   weight_out, kept_out: device fp32 and int32 [n_seq][n_kv_heads][to->max_pages * to->block]: weights and former
- *   positions of the tokens that stay; nothing is written behind them.  workspace:
+ *   positions of the tokens that stay; nothing is written behind them (weight_out as weight_in of a later attention needs
+ *   zeros there: tokens that come have no weight yet).  workspace:
  *   device, shplb_cache_evict_workspace_bytes(cache), 256-byte aligned; no clearing.
  * Errors: SHPLB_E_BUDGET (negative n_sink or n_recent). */
 SHPLB_API int32_t shplb_cache_evict_workspace_bytes(const shplb_cache* cache, int64_t* bytes_out /*host*/);
