@@ -389,7 +389,8 @@ SHPLB_API int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* s
  *   positions of the tokens that stay; nothing is written behind them (weight_out as weight_in of a later attention needs
  *   zeros there: tokens that come have no weight yet).  workspace:
  *   device, shplb_cache_evict_workspace_bytes(cache), 256-byte aligned; no clearing.
- * Errors: SHPLB_E_BUDGET (negative n_sink or n_recent). */
+ * to->lens, weight_out, kept_out and the workspace are arrays apart from one another and from all that is read.
+ * Errors: SHPLB_E_BUDGET (negative n_sink or n_recent); SHPLB_E_SHAPE where one of those arrays begins where another does. */
 SHPLB_API int32_t shplb_cache_evict_workspace_bytes(const shplb_cache* cache, int64_t* bytes_out /*host*/);
 SHPLB_API int32_t shplb_cache_evict(const shplb_cache* cache, const float* weight, const int32_t* keep,
                           int32_t n_sink, int32_t n_recent, const shplb_cache* to, float* weight_out,

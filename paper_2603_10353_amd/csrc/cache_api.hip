@@ -175,12 +175,16 @@ int32_t shplb_cache_evict(const shplb_cache* cache, const float* weight, const i
   if (int32_t st = check_cache(cache, &c)) return st;
   if (int32_t st = check_cache(to, &d)) return st;
   if (n_sink < 0 || n_recent < 0) return SHPLB_E_BUDGET;
-  if (c.n_seq != d.n_seq || c.n_kv_heads != d.n_kv_heads || c.format != d.format || c.lens == d.lens || c.table == d.table)
-    return SHPLB_E_SHAPE;
+  if (c.n_seq != d.n_seq || c.n_kv_heads != d.n_kv_heads || c.format != d.format || c.table == d.table) return SHPLB_E_SHAPE;
   if (!weight || !keep || !weight_out || !kept_out || !workspace) return SHPLB_E_NULL;
-  if (weight == weight_out || misaligned(weight, 4) || misaligned(keep, 4) || misaligned(weight_out, 4) || misaligned(kept_out, 4) ||
-      misaligned(workspace, 256))
+  if (misaligned(weight, 4) || misaligned(keep, 4) || misaligned(weight_out, 4) || misaligned(kept_out, 4) || misaligned(workspace, 256))
     return SHPLB_E_SHAPE;
+  if (int64_t(d.n_seq) * d.n_kv_heads * d.max_pages >= int64_t(1) << 23) return SHPLB_E_UNSUPPORTED;
+  // heads are worked on side by side: what one writes is nothing that another reads, or writes in another meaning
+  const void* arrays[] = {d.lens, weight_out, kept_out, workspace, weight, keep, c.lens, c.table, d.table};
+  for (int written = 0; written < 4; ++written)
+    for (int other = written + 1; other < 9; ++other)
+      if (arrays[written] == arrays[other]) return SHPLB_E_SHAPE;
   return launch_cache_evict(c, weight, keep, n_sink, n_recent, d, weight_out, kept_out, workspace, static_cast<hipStream_t>(stream));
 }
 

@@ -493,8 +493,7 @@ int64_t cache_evict_workspace(const CacheArgs& c) {
 int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int32_t* keep, int32_t n_sink, int32_t n_recent,
                            const CacheArgs& dst, float* weight_out, int32_t* kept, void* workspace, hipStream_t stream) {
   const int parts = evict_parts(src);
-  const int64_t pairs = int64_t(src.n_seq) * src.n_kv_heads, grid = pairs * dst.max_pages * 2;
-  if (!grid_holds(grid)) return SHPLB_E_UNSUPPORTED;
+  const int64_t pairs = int64_t(src.n_seq) * src.n_kv_heads, grid = pairs * dst.max_pages * 2;    // (the entry point sees to it that a grid holds them)
   uint32_t* bins = static_cast<uint32_t*>(workspace);
   const SelectArgs a{src, dst, weight, keep, n_sink, n_recent, parts, weight_out, kept, bins, bins + pairs * parts * 3 * kBins};
   const dim3 all(uint32_t(pairs * parts));

@@ -177,3 +177,17 @@ def test_workspace_sizes():
     with pytest.raises(ValueError):
         step(n_q_heads=5, kv_head_of=[0, 1])
     assert np.asarray(step(n_q_heads=5, kv_head_of=[0, 1, 2, 3, 0]).kv_head_of).size == 5
+
+
+# arrays of an eviction, each at an address of its own
+EVICT_ARRAYS = ["lens", "table", "to_lens", "to_table", "weight", "keep", "weight_out", "kept_out", "workspace"]
+
+
+@pytest.mark.parametrize("written,other", [(x, y) for x in ("to_lens", "weight_out", "kept_out", "workspace") for y in EVICT_ARRAYS if x != y])
+def test_arrays_that_eviction_writes_are_no_others(written, other):
+    # budgets, lengths, weights and positions are read while others' lengths, weights and positions are written
+    at = {x: (i + 2) * FAKE for i, x in enumerate(EVICT_ARRAYS)}
+    at[written] = at[other]
+    to = cache(page_table=at["to_table"], lens=at["to_lens"])
+    assert status(S.shplb_cache_evict, cache(page_table=at["table"], lens=at["lens"]), at["weight"], at["keep"], 1, 1, to,
+                  at["weight_out"], at["kept_out"], at["workspace"]) == -2
