@@ -296,6 +296,8 @@ SHPLB_API int32_t shplb_token_recovery_heads(const shplb_problem* p, const float
  *     read or written there, what is computed from it is NaN.  A length below 0 or above
  *     max_pages * block: the head's outputs are NaN, nothing is written into it, read out of
  *     it or counted for it, and eviction hands it on as length -1.
+ *   - Offsets of a step's sequences below 0 or above n_tokens are taken as those; a sequence whose end lies in front of its beginning
+ *     has no rows, one of more than max_tokens its first max_tokens.
  *   - Pages may be shared (a common prefix) by heads that only read them.
  * Errors of all calls: SHPLB_E_NULL; SHPLB_E_SHAPE (a size smaller than stated, strides smaller than what they step
  * over or no multiple of 8, tensors and pages not aligned to 16 bytes, other arrays not to their elements);

@@ -98,8 +98,9 @@ __device__ __forceinline__ void step_tokens(const StepArgs& t, int s, int& row0,
     row0 = s * t.max_tokens;
     n = t.max_tokens;
   } else {
+    // (offsets that go backwards or lie outside the rows: none of a difference's operands is negative, whatever they are)
     row0 = min(max(SCALAR ? scalar_load(t.cu + s) : t.cu[s], 0), t.n_tokens);
-    n = min(max(min(SCALAR ? scalar_load(t.cu + s + 1) : t.cu[s + 1], t.n_tokens) - row0, 0), t.max_tokens);
+    n = min(max(min(SCALAR ? scalar_load(t.cu + s + 1) : t.cu[s + 1], t.n_tokens), row0) - row0, t.max_tokens);
   }
 }
 
