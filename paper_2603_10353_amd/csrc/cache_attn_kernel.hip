@@ -411,6 +411,10 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
       for (int t = 0; t < 4; ++t) keep[t] = sc[0][t];
     }
     if (__ballot(raise)) {
+      // The outputs are scaled in place: as other values, every register would be moved where nothing is raised (and spilled: 51 -> 41 us
+      // for 128 rows x 8 heads x 32768 tokens).  The compiler does not look into these lines and puts no wait states between them and the
+      // products that write and read the outputs: here they are, 20 on either side, which no product needs more of.
+      asm volatile("s_nop 15\n\ts_nop 3");
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         top[nt] = quad_max(top[nt]);
@@ -423,13 +427,11 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float x = r.acc[nt][t][i];
-            // in place: as another value, every register would be moved where nothing is raised (and spilled: 51 -> 41 us for 128 rows x 8 heads x
-            // 32768 tokens).  The products that write and read the outputs are a hundred instructions away on either side: the compiler, which does
-            // not look into this line, puts no wait states between them
             asm volatile("v_mul_f32 %0, %1, %0" : "+v"(x) : "v"(alpha));
             r.acc[nt][t][i] = x;
           }
       }
+      asm volatile("s_nop 15\n\ts_nop 3");
     }
     f16x8 p[NT][2];
 #pragma unroll

@@ -1,0 +1,43 @@
+"""GPU parity of attention over the cache where the scores themselves are the difficulty."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_10353_amd as S
+from cache_harness import D, DEV, Device, attn_workspace, bf16, check_attn, state, step_of
+from oracle import cache_oracle as orc
+
+pytestmark = pytest.mark.gpu
+FORMATS = pytest.mark.parametrize("fmt", [orc.E4M3, orc.INT8], ids=["e4m3", "int8"])
+
+
+@FORMATS
+@pytest.mark.parametrize("room", [None, 128], ids=["short", "long"])
+@pytest.mark.parametrize("tokens", [1, 4, 5, 30])        # 4, 16, 20 and 120 rows of a KV head
+def test_scores_that_grow(tokens, room, fmt):
+    # every 64 keys weigh 2^10 times what those before them do, so that what was added up so far is scaled down by that each time; the values in
+    # front of a head's last 64 keys are as much larger, so that the scaling shows
+    rng = np.random.default_rng([tokens, fmt])
+    lens = np.array([[1300, 641], [64, 65], [200, 1000]])
+    c = state(rng, lens, 64, fmt, max_pages=room)
+    most = int(lens.max())
+    direction = rng.choice([-1.0, 1.0], size=(3, 2, D))
+    from_end = -(-lens // 64)[:, None, :] - 1 - np.arange(most)[None, :, None] // 64                 # [sequence, place, head]
+    q = 2.0 * direction[:, None].repeat(tokens, 1).repeat(4, 2) + 0.1 * rng.standard_normal((3, tokens, 8, D))
+    step_up = 10 / (2.0 * D / np.sqrt(D) * np.log2(np.e))
+    k = -step_up * from_end[..., None] * direction[:, None] + 0.02 * rng.standard_normal((3, most, 2, D))
+    v = rng.standard_normal((3, most, 2, D)) * 2.0 ** (10 * np.clip(from_end, 0, 1))[..., None]
+    for s in range(3):                                   # heads of lengths of their own: the tokens of each end where it does
+        for h in range(2):
+            k[s, :, h], v[s, :, h] = (np.roll(x[s, :, h], most - lens[s, h], 0) for x in (k, v))
+    (kt, k64), (vt, v64) = (bf16(x.reshape(-1, 2, D)) for x in (k, v))
+    orc.append(c, k64, v64, np.arange(4) * most)
+    dev = Device(c)
+    q, q64 = bf16(q.reshape(-1, 8, D))
+    step, cu = step_of(dev, [tokens] * 3, 8, False)
+    out = torch.empty((3 * tokens, 8, D), dtype=torch.bfloat16, device=DEV)
+    lse = torch.empty((8, 3 * tokens), device=DEV)
+    w = torch.zeros((3, 2, c.capacity), device=DEV)
+    S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, lse, None, w, attn_workspace(dev, step), torch.cuda.current_stream())
+    check_attn(c, out.double().cpu().numpy(), lse.double().cpu().numpy(), q64, cu, [h // 4 for h in range(8)],
+               got_weight=w.double().cpu().numpy(), weight_in=np.zeros(w.shape, np.float32))
