@@ -1016,7 +1016,8 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
   const int key = wave * kUnit + key_of_lane(lane);              // of the first unit, whose probabilities' sum comes to this lane
   const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
   float old[kWholeUnits];
-  begin_rows<1, kWholeWaves, false>(a, pair, h, max(group, 1), row0, n, 0, seen_before, wave, units, last, lane, lds, f, r);
+  // (a KV head without query heads has no rows to ask for)
+  begin_rows<1, kWholeWaves, false>(a, pair, h, max(group, 1), row0, group > 0 ? n : 0, 0, seen_before, wave, units, last, lane, lds, f, r);
   if (rows > 0) {
     attend<1, kWholeWaves, false, FMT, WEIGHTS ? kWholeUnits : 0>(a, pair, len, wave, units, last, seen_before, lds, lane, f, r, kept);
     r.l[0] = quad_sum(r.l[0]);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2603_10353_amd as S
-from cache_harness import D, DEV, Device, attn_workspace, bf16, check_attn, state, step_of
+from cache_harness import D, DEV, Device, attn_workspace, bf16, check_attn, filled, state, step_of
 from oracle import cache_oracle as orc
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +41,19 @@ def test_scores_that_grow(tokens, room, fmt):
     S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, lse, None, w, attn_workspace(dev, step), torch.cuda.current_stream())
     check_attn(c, out.double().cpu().numpy(), lse.double().cpu().numpy(), q64, cu, [h // 4 for h in range(8)],
                got_weight=w.double().cpu().numpy(), weight_in=np.zeros(w.shape, np.float32))
+
+
+@pytest.mark.parametrize("room", [None, 64], ids=["short", "long"])
+def test_as_many_mapped_heads_as_there_may_be(room):
+    # 256 query heads, sixteen of each of the first sixteen KV heads; the last one has none
+    rng = np.random.default_rng(31)
+    c = filled(rng, [[130] * 16 + [70]], 64, orc.E4M3, max_pages=room)
+    dev = Device(c)
+    kv_of = [h % 16 for h in range(256)]
+    q, q64 = bf16(rng.standard_normal((1, 256, D)))
+    step, cu = step_of(dev, [1], 256, False, kv_head_of=kv_of)
+    w = rng.random((1, 17, c.capacity)).astype(np.float32)
+    out, w_out = torch.empty((1, 256, D), dtype=torch.bfloat16, device=DEV), torch.zeros(w.shape, device=DEV)
+    S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, None, torch.from_numpy(w).to(DEV), w_out, attn_workspace(dev, step),
+                       torch.cuda.current_stream())
+    check_attn(c, out.double().cpu().numpy(), None, q64, cu, kv_of, got_weight=w_out.double().cpu().numpy(), weight_in=w)
