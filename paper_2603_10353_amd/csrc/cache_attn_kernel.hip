@@ -218,6 +218,12 @@ __device__ __forceinline__ float query_operands(const CacheAttnArgs& a, const Qu
   return a.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
 }
 
+// Whether what a row's products are multiplied by, times the scale of some page, may be infinite (its queries are in the hundreds of thousands, then).  The
+// products themselves may be small, or 0 where a query and a key have no dim in common.  A wave that has such a row multiplies by one factor after the
+// other where the two are infinite together, and takes every unit for one that not all rows see: its "fewest keys that a row sees" are kFar.
+__device__ __forceinline__ bool far_row(float to_log2) { return to_log2 >= 2.0f; }
+constexpr int kFar = INT32_MIN;
+
 // Eight bytes of a K row as operand.
 template <int FMT>
 __device__ __forceinline__ f16x8 key_operand(uint32_t x, uint32_t y) {
@@ -320,8 +326,9 @@ __device__ __forceinline__ void ask_unit(const CacheAttnArgs& a, int page, int f
 // What a wave begins with: the rows from first_row on and the first unit of first, first + STEP .. below end (last: a unit whose place in the page
 // table can be read in any case).  Queries are on their way while the page is looked up, and are worked on while its codes are.  They go
 // into LDS, as each lane needs them: what it reads it wrote itself, and they cost no registers.
+// Returns whether there is a far_row().
 template <int NT, int STEP, bool ONCE>
-__device__ __forceinline__ void begin_rows(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int seen_before, int first,
+__device__ __forceinline__ bool begin_rows(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int seen_before, int first,
                                            int end, int last, int lane, RowsLds<NT>& lds, Flight& f, Rows<NT>& r) {
   const int page = page_number(a.c, pair, min(first, last));
   f.page_next = page_number(a.c, pair, min(first + STEP, last));
@@ -330,11 +337,13 @@ __device__ __forceinline__ void begin_rows(const CacheAttnArgs& a, int pair, int
   for (int nt = 0; nt < NT; ++nt) ask_query(a, row0, n, h, group, first_row + nt * 16 + (lane & 15), lane, q[nt]);
   __builtin_amdgcn_sched_barrier(0);
   ask_unit<ONCE>(a, page, min(first, last), first < end ? end : 0, lane, true, f);
+  bool far = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = first_row + nt * 16 + (lane & 15);
     f16x8 operand[4];
     const float to_log2 = query_operands(a, q[nt], operand);
+    far |= far_row(to_log2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) lds.q[nt][e][lane] = operand[e];
     const bool there = row < n * group;
@@ -344,6 +353,7 @@ __device__ __forceinline__ void begin_rows(const CacheAttnArgs& a, int pair, int
 #pragma unroll
     for (int t = 0; t < 8; ++t) r.acc[nt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
+  return __ballot(far) != 0;
 }
 
 // Scores of a unit, S^T.
@@ -364,7 +374,7 @@ __device__ __forceinline__ void scores(const Keys& keys, const f16x8 (*lds_q)[4]
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Goes through the units first, first + STEP ..; seen_first: the fewest keys that a row sees.  KEEP > 0: there are no more than that, and y of
+// Goes through the units first, first + STEP ..; seen_first: the fewest keys that a row sees (or kFar).  KEEP > 0: there are no more than that, and y of
 // each (-inf where it is masked) stays in `kept`.
 template <int NT, int STEP, bool ONCE, int FMT, int KEEP = 0>
 __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first,
@@ -386,6 +396,12 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       to[nt] = lds.to_log2(nt, lane) * k_scale;
+      if (seen_first == kFar) {
+        const float first = to[nt] == INFINITY ? lds.to_log2(nt, lane) : 1.0f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sc[nt][t] *= first;
+        to[nt] = to[nt] == INFINITY ? k_scale : to[nt];
+      }
       if (key0 + kUnit > seen_first) {
         const int seen = lds.seen(nt, lane);
 #pragma unroll
@@ -587,8 +603,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
     RowsLds<NT>& rows_lds = lds_rows[kOwn ? wave : 0];           // (waves of one share write the same)
     Flight f;
     Rows<NT> r;
-    begin_rows<NT, WAVES, kOwn>(a, pair, h, group, row0, n, first_row, len - n + 1, u_first, u_end, u1 - 1, lane, rows_lds, f, r);
-    attend<NT, WAVES, kOwn, FMT>(a, pair, len, u_first, u_end, u1 - 1, len - n + 1 + first_row / group, rows_lds, lane, f, r);
+    const bool far = begin_rows<NT, WAVES, kOwn>(a, pair, h, group, row0, n, first_row, len - n + 1, u_first, u_end, u1 - 1, lane, rows_lds, f, r);
+    attend<NT, WAVES, kOwn, FMT>(a, pair, len, u_first, u_end, u1 - 1, far ? kFar : len - n + 1 + first_row / group, rows_lds, lane, f, r);
 
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
@@ -822,7 +838,13 @@ __device__ __forceinline__ float weigh_unit(const CacheAttnArgs& a, int key0, co
   for (int x = 0; x < 16; ++x) w[x] = 0.0f;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const float c = r.to_log2[nt] * k_scale;
+    float c = r.to_log2[nt] * k_scale;
+    if (seen_first == kFar) {
+      const float first = c == INFINITY ? r.to_log2[nt] : 1.0f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sc[nt][x] *= first;
+      c = c == INFINITY ? k_scale : c;
+    }
     if (key0 + kUnit > seen_first) {
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
@@ -853,9 +875,9 @@ __device__ __forceinline__ void weigh(const CacheAttnArgs& a, int pair, int len,
   }
 }
 
-// What a wave begins to weigh with: rows first_row on and the unit `first`, if it is below end.
+// What a wave begins to weigh with: rows first_row on and the unit `first`, if it is below end.  Returns whether there is a far_row().
 template <int NT>
-__device__ __forceinline__ void begin_weights(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int len, int first, int step,
+__device__ __forceinline__ bool begin_weights(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int len, int first, int step,
                                               int end, int last, int lane, f16x8 (*lds_q)[4][64], Flight& f, Statistics<NT>& r) {
   const int rows = n * group, page = page_number(a.c, pair, min(first, last));
   f.page_next = page_number(a.c, pair, min(first + step, last));
@@ -876,14 +898,17 @@ __device__ __forceinline__ void begin_weights(const CacheAttnArgs& a, int pair, 
   }
   __builtin_amdgcn_sched_barrier(0);
   ask_unit<false>(a, page, min(first, last), first < end ? end : 0, lane, false, f);
+  bool far = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     f16x8 operand[4];
     const float to_log2 = query_operands(a, q[nt], operand);
+    far |= far_row(to_log2);
     r.to_log2[nt] = first_row + nt * 16 + (lane & 15) < rows ? to_log2 : 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) lds_q[nt][e][lane] = operand[e];
   }
+  return __ballot(far) != 0;
 }
 
 // Weights of keys first .. end - 1 of a head that has no rows in this step: what they were.
@@ -916,8 +941,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
     } else {
       Flight f;
       Statistics<1> r;
-      begin_weights<1>(a, pair, h, group, row0, n, 0, len, u0, 1, u1, last, lane, lds_q[wave], f, r);
-      weigh<FMT>(a, pair, len, u0, u1, last, len - n + 1, lds_q[wave], a.weight_in, lane, f, r);
+      const bool far = begin_weights<1>(a, pair, h, group, row0, n, 0, len, u0, 1, u1, last, lane, lds_q[wave], f, r);
+      weigh<FMT>(a, pair, len, u0, u1, last, far ? kFar : len - n + 1, lds_q[wave], a.weight_in, lane, f, r);
     }
     at += units - it.unit;
     it = next_pair<kStart>(a, pair);
@@ -950,11 +975,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
     for (int first_row = 0; u0 < u1 && first_row < rows; first_row += kWaves * kSlice) {
       const int left = rows - first_row, log2 = left > 2 * kSlice ? 2 : left > kSlice ? 1 : 0, slices = 1 << log2, step = kWaves >> log2;
       const int phase = wave >> log2, my_row = first_row + (wave & (slices - 1)) * kSlice;
-      const int seen_first = len - n + 1 + my_row / group, seen_last = my_row < rows ? len - n + 1 + (min(my_row + kSlice, rows) - 1) / group : 0;
+      const int seen_last = my_row < rows ? len - n + 1 + (min(my_row + kSlice, rows) - 1) / group : 0;
       const float* before = first_row == 0 ? a.weight_in : a.weight_out;
       Flight f;
       Statistics<2> r;
-      begin_weights<2>(a, pair, h, group, row0, n, my_row, len, u0 + phase, step, u1, u1 - 1, lane, lds_q[wave], f, r);
+      const bool far = begin_weights<2>(a, pair, h, group, row0, n, my_row, len, u0 + phase, step, u1, u1 - 1, lane, lds_q[wave], f, r);
+      const int seen_first = far ? kFar : len - n + 1 + my_row / group;
       for (int c = u0; c < u1; c += kSteps * step) {
         // a thread's keys of all these units: kThreads apart
         const int key = c * kUnit + tid, key_end = min(len, min(u1, c + kSteps * step) * kUnit);
@@ -1017,9 +1043,9 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
   const int64_t row_of_weights = int64_t(pair) * a.c.max_pages << a.c.block_log2;
   float old[kWholeUnits];
   // (a KV head without query heads has no rows to ask for)
-  begin_rows<1, kWholeWaves, false>(a, pair, h, max(group, 1), row0, group > 0 ? n : 0, 0, seen_before, wave, units, last, lane, lds, f, r);
+  const bool far = begin_rows<1, kWholeWaves, false>(a, pair, h, max(group, 1), row0, group > 0 ? n : 0, 0, seen_before, wave, units, last, lane, lds, f, r);
   if (rows > 0) {
-    attend<1, kWholeWaves, false, FMT, WEIGHTS ? kWholeUnits : 0>(a, pair, len, wave, units, last, seen_before, lds, lane, f, r, kept);
+    attend<1, kWholeWaves, false, FMT, WEIGHTS ? kWholeUnits : 0>(a, pair, len, wave, units, last, far ? kFar : seen_before, lds, lane, f, r, kept);
     r.l[0] = quad_sum(r.l[0]);
     if (quad == 0) {
       lds_m[wave][n16] = r.m[0];

@@ -57,3 +57,41 @@ def test_as_many_mapped_heads_as_there_may_be(room):
     S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, None, torch.from_numpy(w).to(DEV), w_out, attn_workspace(dev, step),
                        torch.cuda.current_stream())
     check_attn(c, out.double().cpu().numpy(), None, q64, cu, kv_of, got_weight=w_out.double().cpu().numpy(), weight_in=w)
+
+
+@FORMATS
+@pytest.mark.parametrize("room", [None, 64], ids=["short", "long"])
+@pytest.mark.parametrize("tokens", [1, 6])
+def test_large_queries_and_large_keys_apart(tokens, room, fmt):
+    # queries and keys of 1e30 and more that have no dim in common, or keys of zeros beside one of 3e38 that the row does not see: scores of 0
+    rng = np.random.default_rng([tokens, fmt])
+    lens = np.array([[200], [64 + tokens]])
+    c = state(rng, lens, 64, fmt, max_pages=room)
+    k = rng.standard_normal((200 + 64 + tokens, 1, D)) * 1e30
+    k[:, :, 64:] = 0.0
+    k[200:] = 0.0
+    k[-1] = 3e38
+    (k, k64), (v, v64) = (bf16(x) for x in (k, rng.standard_normal(k.shape)))
+    orc.append(c, k64, v64, np.array([0, 200, 264 + tokens]))
+    dev = Device(c)
+    q = rng.standard_normal((2 * tokens, 4, D)) * 1e30
+    q[:, :, :64] = 0.0
+    if tokens == 1:                                      # ... but the last row sees it: not finite, or not at all large
+        q[1] = rng.standard_normal((4, D)) * 1e-38
+    q, q64 = bf16(q)
+    step, cu = step_of(dev, [tokens] * 2, 4, False)
+    out = torch.empty((2 * tokens, 4, D), dtype=torch.bfloat16, device=DEV)
+    lse = torch.empty((4, 2 * tokens), device=DEV)
+    w = torch.zeros((2, 1, c.capacity), device=DEV)
+    S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, lse, None, w, attn_workspace(dev, step), torch.cuda.current_stream())
+    got, got_lse, got_w = (x.double().cpu().numpy() for x in (out, lse, w))
+    finite = slice(0, 2 * tokens - (tokens > 1))
+    assert np.isfinite(got[finite]).all() and np.isfinite(got_lse[:, finite]).all() and np.isfinite(got_w[0]).all()
+    # the first sequence's scores are 0, and so are the second's but for its last row's: means of the values, within bf16's half step and fp16's of
+    # equal probabilities
+    one = orc.CacheState(c.k_pages, c.v_pages, c.k_scale, c.v_scale, c.table[:1], c.lens[:1], fmt)
+    check_attn(one, got[:tokens], got_lse[:, :tokens], q64[:tokens], cu[:2], [0] * 4, got_weight=got_w[:1], weight_in=np.zeros((1, 1, c.capacity)))
+    for j in range(tokens - 1):
+        values = c.values("v", 1, 0, 65 + j)
+        tol = 2.0 ** -8 * np.abs(values.mean(0)) + 2.0 ** -11 * 1.01 * np.abs(values).mean(0)
+        assert (np.abs(got[tokens + j] - values.mean(0)) <= tol).all()
