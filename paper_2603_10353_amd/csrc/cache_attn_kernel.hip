@@ -203,7 +203,8 @@ __device__ __forceinline__ float query_operands(const CacheAttnArgs& a, const Qu
     for (int e = 0; e < 4; ++e) top = max(top, max(in.part[x][e] << 16 & 0x7fff0000u, in.part[x][e] & 0x7fff0000u));
   top = max(top, uint32_t(__shfl_xor(int(top), 16)));
   top = max(top, uint32_t(__shfl_xor(int(top), 32)));
-  const int up = top == 0 ? 0 : min(max(13 - (int(top >> 23) - 127), -120), 100);
+  // (at most 2^120: 2^-133, which all bf16 numbers are multiples of, becomes 2^-13, and a softmax scale of about 1 over it is no subnormal)
+  const int up = top == 0 ? 0 : min(max(13 - (int(top >> 23) - 127), -120), 120);
   const float f = __uint_as_float(uint32_t(up + 127) << 23);
 #pragma unroll
   for (int x = 0; x < 4; ++x) {

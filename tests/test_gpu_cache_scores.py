@@ -95,3 +95,25 @@ def test_large_queries_and_large_keys_apart(tokens, room, fmt):
         values = c.values("v", 1, 0, 65 + j)
         tol = 2.0 ** -8 * np.abs(values.mean(0)) + 2.0 ** -11 * 1.01 * np.abs(values).mean(0)
         assert (np.abs(got[tokens + j] - values.mean(0)) <= tol).all()
+
+
+@FORMATS
+@pytest.mark.parametrize("room", [None, 64], ids=["short", "long"])
+@pytest.mark.parametrize("tokens", [1, 6])
+@pytest.mark.parametrize("size", [1e-40, 1e-38, 1e-36, 1e-31])
+def test_small_queries_and_large_keys(size, tokens, room, fmt):
+    # queries down to bf16's subnormals, and keys as large as makes scores of ordinary size of them
+    rng = np.random.default_rng([tokens, fmt])
+    lens = np.array([[200, 70]])
+    c = state(rng, lens, 64, fmt, max_pages=room)
+    k = np.clip(rng.standard_normal((200, 2, D)) * min(1 / size, 1e38), -3e38, 3e38)
+    (k, k64), (v, v64) = (bf16(x) for x in (k, rng.standard_normal(k.shape)))
+    orc.append(c, k64, v64, np.array([0, 200]))
+    dev = Device(c)
+    q, q64 = bf16(rng.standard_normal((tokens, 8, D)) * size)
+    step, cu = step_of(dev, [tokens], 8, False)
+    out, lse = torch.empty((tokens, 8, D), dtype=torch.bfloat16, device=DEV), torch.empty((8, tokens), device=DEV)
+    w = torch.zeros((1, 2, c.capacity), device=DEV)
+    S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, lse, None, w, attn_workspace(dev, step), torch.cuda.current_stream())
+    check_attn(c, out.double().cpu().numpy(), lse.double().cpu().numpy(), q64, cu, [h // 4 for h in range(8)],
+               got_weight=w.double().cpu().numpy(), weight_in=np.zeros(w.shape, np.float32))
