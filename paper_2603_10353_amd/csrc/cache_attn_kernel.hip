@@ -219,11 +219,15 @@ __device__ __forceinline__ float query_operands(const CacheAttnArgs& a, const Qu
   return a.scale_log2 * __uint_as_float(uint32_t(127 - up) << 23);
 }
 
-// Whether what a row's products are multiplied by, times the scale of some page, may be infinite (its queries are in the hundreds of thousands, then).  The
-// products themselves may be small, or 0 where a query and a key have no dim in common.  A wave that has such a row multiplies by one factor after the
-// other where the two are infinite together, and takes every unit for one that not all rows see: its "fewest keys that a row sees" are kFar.
-__device__ __forceinline__ bool far_row(float to_log2) { return to_log2 >= 2.0f; }
+// What lies far outside of what a model computes with, and is right all the same.
+//  - Rows whose products' factor, times the scale of some page, may be infinite (their queries are in the hundreds of thousands): the products
+//    themselves may be small, or 0 where a query and a key have no dim in common.  They are multiplied by one after the other.
+//  - Rows whose reference is 2^22 or more: a product that is rounded, as the reference was, and one inside of a multiply-add differ by
+//    so much there that a probability may be above all that fp16 holds.  Their products are rounded.
+// A wave with such a row takes every unit for one that not all rows see all of: its "fewest keys that a row sees" are kFar.
 constexpr int kFar = INT32_MIN;
+__device__ __forceinline__ bool far_row(float to_log2) { return to_log2 >= 2.0f; }
+__device__ __forceinline__ bool far_reference(float m) { return fabsf(m) >= 0x1p22f && fabsf(m) < INFINITY; }
 
 // Eight bytes of a K row as operand.
 template <int FMT>
@@ -398,10 +402,11 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
     for (int nt = 0; nt < NT; ++nt) {
       to[nt] = lds.to_log2(nt, lane) * k_scale;
       if (seen_first == kFar) {
-        const float first = to[nt] == INFINITY ? lds.to_log2(nt, lane) : 1.0f;
+        const bool far = to[nt] == INFINITY;
+        const float first = far ? lds.to_log2(nt, lane) : to[nt];
 #pragma unroll
         for (int t = 0; t < 4; ++t) sc[nt][t] *= first;
-        to[nt] = to[nt] == INFINITY ? k_scale : to[nt];
+        to[nt] = far ? k_scale : 1.0f;
       }
       if (key0 + kUnit > seen_first) {
         const int seen = lds.seen(nt, lane);
@@ -449,6 +454,18 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
           }
       }
       asm volatile("s_nop 15\n\ts_nop 3");
+      bool far = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) far |= far_reference(r.m[nt]);
+      if (__ballot(far) && seen_first != kFar) {
+        seen_first = kFar;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) sc[nt][t] *= to[nt];
+          to[nt] = 1.0f;
+        }
+      }
     }
     f16x8 p[NT][2];
 #pragma unroll
@@ -841,10 +858,11 @@ __device__ __forceinline__ float weigh_unit(const CacheAttnArgs& a, int key0, co
   for (int nt = 0; nt < NT; ++nt) {
     float c = r.to_log2[nt] * k_scale;
     if (seen_first == kFar) {
-      const float first = c == INFINITY ? r.to_log2[nt] : 1.0f;
+      const bool far = c == INFINITY;
+      const float first = far ? r.to_log2[nt] : c;
 #pragma unroll
       for (int x = 0; x < 4; ++x) sc[nt][x] *= first;
-      c = c == INFINITY ? k_scale : c;
+      c = far ? k_scale : 1.0f;
     }
     if (key0 + kUnit > seen_first) {
 #pragma unroll
@@ -904,7 +922,7 @@ __device__ __forceinline__ bool begin_weights(const CacheAttnArgs& a, int pair, 
   for (int nt = 0; nt < NT; ++nt) {
     f16x8 operand[4];
     const float to_log2 = query_operands(a, q[nt], operand);
-    far |= far_row(to_log2);
+    far |= far_row(to_log2) || far_reference(r.m[nt]);
     r.to_log2[nt] = first_row + nt * 16 + (lane & 15) < rows ? to_log2 : 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) lds_q[nt][e][lane] = operand[e];

@@ -117,3 +117,33 @@ def test_small_queries_and_large_keys(size, tokens, room, fmt):
     S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, lse, None, w, attn_workspace(dev, step), torch.cuda.current_stream())
     check_attn(c, out.double().cpu().numpy(), lse.double().cpu().numpy(), q64, cu, [h // 4 for h in range(8)],
                got_weight=w.double().cpu().numpy(), weight_in=np.zeros(w.shape, np.float32))
+
+
+@FORMATS
+@pytest.mark.parametrize("room", [None, 128], ids=["short", "long"])
+@pytest.mark.parametrize("tokens", [1, 6])
+@pytest.mark.parametrize("size", [1e7, 3e8, 1e10, 1e25])
+def test_scores_past_24_bits(size, tokens, room, fmt):
+    # scores whose last place in fp32 is a factor of two and more between probabilities: nearly all of a row's lies on one key, which may be one of
+    # those within that; what comes out is finite
+    rng = np.random.default_rng([tokens, fmt])
+    lens = np.array([[500, 130], [64, 1000]])
+    c = state(rng, lens, 64, fmt, max_pages=room)
+    near = np.round(2 * rng.standard_normal((2000, 2, 1))) * 1e-7            # many keys that are nearly the largest
+    k = np.sqrt(size) * (1 + near) * rng.choice([-1.0, 1.0], size=(1, 1, D)) * np.ones((1, 1, D))
+    k = np.where(rng.random((2000, 2, 1)) < 0.5, k, k * rng.uniform(-1, 1, size=(2000, 2, 1)))
+    (k, k64), (v, v64) = (bf16(x) for x in (k, rng.standard_normal(k.shape)))
+    orc.append(c, k64, v64, np.array([0, 1000, 2000]))
+    dev = Device(c)
+    q, q64 = bf16(np.sqrt(size) * rng.standard_normal((2 * tokens, 8, D)))
+    step, cu = step_of(dev, [tokens] * 2, 8, False)
+    out, lse = torch.empty((2 * tokens, 8, D), dtype=torch.bfloat16, device=DEV), torch.empty((8, 2 * tokens), device=DEV)
+    w = rng.uniform(0.5, 1.0, size=(2, 2, c.capacity)).astype(np.float32)
+    w_out = torch.zeros(w.shape, device=DEV)
+    S.shplb_cache_attn(dev.cache, step, q.to(DEV), out, lse, torch.from_numpy(w).to(DEV), w_out, attn_workspace(dev, step),
+                       torch.cuda.current_stream())
+    got, got_lse, got_w = (x.double().cpu().numpy() for x in (out, lse, w_out))
+    check_attn(c, got, got_lse, q64, cu, [h // 4 for h in range(8)], got_weight=got_w, weight_in=w)
+    # every row's weights are those of one softmax
+    given = [(got_w[s, h, :lens[s, h]] - w[s, h, :lens[s, h]]).sum() for s in range(2) for h in range(2)]
+    assert np.isfinite(got).all() and np.isfinite(got_lse).all() and (np.abs(np.array(given) / (4 * tokens) - 1) < 0.01).all()
