@@ -401,14 +401,14 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       to[nt] = lds.to_log2(nt, lane) * k_scale;
-      if (seen_first == kFar) {
-        const bool far = to[nt] == INFINITY;
-        const float first = far ? lds.to_log2(nt, lane) : to[nt];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) sc[nt][t] *= first;
-        to[nt] = far ? k_scale : 1.0f;
-      }
       if (key0 + kUnit > seen_first) {
+        if (seen_first == kFar) {
+          const bool far = to[nt] == INFINITY;
+          const float first = far ? lds.to_log2(nt, lane) : to[nt];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) sc[nt][t] *= first;
+          to[nt] = far ? k_scale : 1.0f;
+        }
         const int seen = lds.seen(nt, lane);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -857,14 +857,14 @@ __device__ __forceinline__ float weigh_unit(const CacheAttnArgs& a, int key0, co
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     float c = r.to_log2[nt] * k_scale;
-    if (seen_first == kFar) {
-      const bool far = c == INFINITY;
-      const float first = far ? r.to_log2[nt] : c;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) sc[nt][x] *= first;
-      c = far ? k_scale : 1.0f;
-    }
     if (key0 + kUnit > seen_first) {
+      if (seen_first == kFar) {
+        const bool far = c == INFINITY;
+        const float first = far ? r.to_log2[nt] : c;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) sc[nt][x] *= first;
+        c = far ? k_scale : 1.0f;
+      }
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         const float p = __builtin_amdgcn_exp2f(sc[nt][x >> 2][x & 3] * c - r.m[nt]) * r.inv[nt];
