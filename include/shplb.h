@@ -288,16 +288,18 @@ SHPLB_API int32_t shplb_token_recovery_heads(const shplb_problem* p, const float
  *   - A scale is the smallest power of two (at least 2^-126) with which the page's
  *     largest value fits the format, 448 in SHPLB_CACHE_E4M3, 127 in SHPLB_CACHE_INT8
  *     (two's complement, -128 is not used): a code is one rounding, to nearest, ties to
- *     even, of its value (near the largest float to the code below, where the next one would stand for 2^128).  A page into which a value comes that is not finite gets the
- *     scale NaN, and everything read from it is NaN.
+ *     even, of its value.  (Where the code it is nearest to would stand for 2^128, it is the
+ *     one below.)  A page into which a value comes that is not finite gets the scale NaN, and
+ *     everything read from it is NaN.
  *   - What lies in a page behind its head's last token is never used, whatever it is, nor
  *     is a page table entry without tokens.
  *   - A page number outside 0 .. n_pages-1 where a token needs one: nothing is
  *     read or written there, what is computed from it is NaN.  A length below 0 or above
  *     max_pages * block: the head's outputs are NaN, nothing is written into it, read out of
  *     it or counted for it, and eviction hands it on as length -1.
- *   - Offsets of a step's sequences below 0 or above n_tokens are taken as those; a sequence whose end lies in front of its beginning
- *     has no rows, one of more than max_tokens its first max_tokens.
+ *   - Offsets of a step's sequences below 0 or above n_tokens are taken as those; a sequence
+ *     whose end lies in front of its beginning has no rows, one of more than max_tokens its
+ *     first max_tokens.
  *   - Pages may be shared (a common prefix) by heads that only read them.
  * Errors of all calls: SHPLB_E_NULL; SHPLB_E_SHAPE (a size smaller than stated, strides smaller than what they step
  * over or no multiple of 8, tensors and pages not aligned to 16 bytes, other arrays not to their elements);
@@ -355,11 +357,17 @@ SHPLB_API int32_t shplb_cache_load(const shplb_cache* cache, const shplb_step* s
 
 /* Attention of the step's queries over the cache (Eq. 1 over the tokens the head holds):
  * the j-th of a sequence's n queries sees the head's first lens - n + 1 + j tokens, the
- * last one all of them.  Products of bf16 queries and 8-bit codes are exact, sums,
- * softmax and its statistics fp32, probabilities are rounded to fp16 before they meet the
- * values.  (Sums are taken at 2^7 times their size or more: values whose magnitude times the head's tokens is beyond 2^112 may
- * come out as infinity.)  A query that sees no token has the output 0 and the denominator's logarithm -inf; one whose
- * products with the keys it sees are not finite has NaN, and so has the weight of those keys.
+ * last one all of them.
+ *   - Queries are brought to fp16 by a power of two a row: exactly where a dim is 2^-27 of the
+ *     row's largest or more, within 2^-38 of that below.  Products of these and the 8-bit codes
+ *     are exact; sums, softmax and its statistics are fp32.
+ *   - Probabilities are rounded to fp16 before they meet the values: that moves an output by up
+ *     to 2^-11 of what the values' magnitudes would give, beside bf16's own rounding.
+ *   - Sums are taken at 2^7 times their size or more: values whose magnitude times the head's
+ *     tokens is beyond 2^112 may come out as infinity.
+ *   - A query that sees no token has the output 0 and the denominator's logarithm -inf; one
+ *     whose products with the keys it sees are not finite fp32 numbers has NaN, and so has the
+ *     weight of those keys.
  *   q: device bf16 [n_tokens, n_q_heads, 128]; out: likewise, strides as Q, in other memory.
  *   lse_out: device fp32 [n_q_heads, n_tokens], natural logarithm of the softmax denominators, or NULL.
  *   weight_in, weight_out: device fp32 [n_seq][n_kv_heads][max_pages * block]:
@@ -368,11 +376,15 @@ SHPLB_API int32_t shplb_cache_load(const shplb_cache* cache, const shplb_step* s
  *     written behind.  weight_in may be weight_out, or NULL for zeros; both NULL: not computed.
  *     weight_in is read for all of these tokens, the step's own among them: whoever keeps one
  *     buffer fills it with zeros before its first call, or before eviction writes into it.
- *   workspace: device, shplb_cache_attn_workspace_bytes() (of this step or of one with at least as many n_tokens and
- *     max_tokens of the same heads), 256-byte aligned; needs no clearing; must not be shared with a call in flight on another
- *     stream.
- * Any number of queries is taken; the kernel is made for few (a decoding step, a draft of some tokens, a window of the
- * prompt's last ones): all rows of a KV head read its keys again for every 32 of them. */
+ *   workspace: device, shplb_cache_attn_workspace_bytes() (of this step or of one with at least
+ *     as many n_tokens and max_tokens, of as many sequences and the same heads), 256-byte
+ *     aligned; needs no clearing; must not be shared with a call in flight on another stream.
+ * Any number of queries is taken; the kernel is made for few (a decoding step, a draft of some
+ * tokens, a window of the prompt's last ones): all rows of a KV head read its keys again for
+ * every 32 of them.  The lengths are on the device, so how the work is divided is chosen by what
+ * the page table has room for: heads of up to 2048 tokens (with more than 16 rows of a KV head up
+ * to 4096) take fewer launches in a table of about their size than in one for the longest context.
+ */
 SHPLB_API int32_t shplb_cache_attn_workspace_bytes(const shplb_cache* cache, const shplb_step* step,
                                          int64_t* bytes_out /*host*/);
 SHPLB_API int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const void* q, void* out,
@@ -383,16 +395,21 @@ SHPLB_API int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* s
  * position; +0 = -0, NaN above all), in the order of their positions,
  *     n = min(lens, capacity of `to`, max(keep, n_sink + n_recent))
  * in all (where that is fewer than n_sink + n_recent: the first ones before the last ones).
- * They go to the pages of another cache, `to`, whose scales are taken afresh, and whose lens are written.  `to` may be in
- * the same pool; its pages must be others than those in use here, its page table and lens other arrays.  Its block
- * may be another, its format not.
+ * They go to the pages of another cache, `to`, whose scales are taken afresh, and whose lens are
+ * written.  `to` may be in the same pool; its pages must be others than those in use here, its
+ * page table and lens other arrays.  Its block may be another, its format not.
  *   weight: device fp32 [n_seq][n_kv_heads][max_pages * block]; keep: device int32 [n_seq][n_kv_heads].
- *   weight_out, kept_out: device fp32 and int32 [n_seq][n_kv_heads][to->max_pages * to->block]: weights and former
- *   positions of the tokens that stay; nothing is written behind them (weight_out as weight_in of a later attention needs
- *   zeros there: tokens that come have no weight yet).  workspace:
- *   device, shplb_cache_evict_workspace_bytes(cache), 256-byte aligned; no clearing.
- * to->lens, weight_out, kept_out and the workspace are arrays apart from one another and from all that is read.
- * Errors: SHPLB_E_BUDGET (negative n_sink or n_recent); SHPLB_E_SHAPE where one of those arrays begins where another does. */
+ *   weight_out, kept_out: device fp32 and int32 [n_seq][n_kv_heads][to->max_pages * to->block]:
+ *     weights and former positions of the tokens that stay; nothing is written behind them
+ *     (weight_out as weight_in of a later attention needs zeros there: tokens that come have no
+ *     weight yet).
+ *   workspace: device, shplb_cache_evict_workspace_bytes(cache), 256-byte aligned; no clearing.
+ *     It grows with the room of the cache's page table beyond 16384 tokens: 24 KB for every 8192
+ *     places of a head.
+ * to->lens, weight_out, kept_out and the workspace are arrays apart from one another and from all
+ * that is read.
+ * Errors: SHPLB_E_BUDGET (negative n_sink or n_recent); SHPLB_E_SHAPE where one of those arrays
+ * begins where another does. */
 SHPLB_API int32_t shplb_cache_evict_workspace_bytes(const shplb_cache* cache, int64_t* bytes_out /*host*/);
 SHPLB_API int32_t shplb_cache_evict(const shplb_cache* cache, const float* weight, const int32_t* keep,
                           int32_t n_sink, int32_t n_recent, const shplb_cache* to, float* weight_out,

@@ -21,7 +21,8 @@
 // and four adjacent keys of each 16; the second one is O^T = V^T P^T, whose operand P^T needs exactly those (the order of the keys
 // inside a product is free, as long as V's are taken alike).  Codes come straight from global memory into registers and are turned to fp16
 // there (exact in both formats), V's after a byte transposition of key pairs; queries wait in LDS as operands.
-// Q is brought to fp16 by a power of two per row, so that its largest magnitude lies in [2^13, 2^14): exact down to 2^-27 of it.
+// Q is brought to fp16 by a power of two per row, so that its largest magnitude lies in [2^13, 2^14), or as far up as 2^120 takes it: exact
+// down to 2^-27 of it.
 // Probabilities are rounded to fp16 at 2^7 times their size: eleven bits down to 2^-21 of the reference, steps of 2^-31 of it below.  Values are
 // fp16 numbers, too, scale and all, where the scale lies between 2^-15 and 2^7 (int8 2^-14 and 2^5).  All sums are fp32.
 //
