@@ -5,9 +5,9 @@
 //
 //   y_t = (q . k_t) * scale * log2(e) * a,   m = max y,   l = sum 2^(y_t - m),   out = sum 2^(y_t - m) b v_t / l,   lse = (m + log2 l) ln 2,
 //
-// in one pass over the keys with a running m: a reference exponent, raised to the largest y (and l and the output scaled down) only where a y
-// is more than 8 above it, which after the first keys is hardly ever.  Bound by reading the codes once: a
-// token of a KV head is 256 bytes and, for a group of four heads, 4 KFLOP.  So the matrix instructions are used for what they save in
+// in one pass over the keys with a running m: a reference exponent, raised to the largest y (and l and the output scaled down)
+// only where a y is more than 8 above it, which after the first keys is hardly ever.  Bound by reading the codes once: a token of
+// a KV head is 256 bytes and, for a group of four heads, 4 KFLOP.  So the matrix instructions are used for what they save in
 // registers and lanes, with most of their rows empty in a plain decoding step.
 //
 // Split.  All heads' keys together are one list of units of 64 keys, which is cut into equal, contiguous shares whatever the heads'
@@ -17,14 +17,14 @@
 // partial results (m, l, unnormalised output), which a second kernel joins in order.  Short caches are worked on head by head or
 // item by item, without partial results.
 //
-// Tile.  A wave works on a unit at a time: keys are the rows of the first product (S^T = K Q^T), so a lane has scores of one query
-// and four adjacent keys of each 16; the second one is O^T = V^T P^T, whose operand P^T needs exactly those (the order of the keys
-// inside a product is free, as long as V's are taken alike).  Codes come straight from global memory into registers and are turned to fp16
-// there (exact in both formats), V's after a byte transposition of key pairs; queries wait in LDS as operands.
-// Q is brought to fp16 by a power of two per row, so that its largest magnitude lies in [2^13, 2^14), or as far up as 2^120 takes it: exact
-// down to 2^-27 of it.
-// Probabilities are rounded to fp16 at 2^7 times their size: eleven bits down to 2^-21 of the reference, steps of 2^-31 of it below.  Values are
-// fp16 numbers, too, scale and all, where the scale lies between 2^-15 and 2^7 (int8 2^-14 and 2^5).  All sums are fp32.
+// Tile.  A wave works on a unit at a time: keys are the rows of the first product (S^T = K Q^T), so a lane has scores of one
+// query and four adjacent keys of each 16; the second one is O^T = V^T P^T, whose operand P^T needs exactly those (the order of
+// the keys inside a product is free, as long as V's are taken alike).  Codes come straight from global memory into registers and
+// are turned to fp16 there (exact in both formats), V's after a byte transposition of key pairs; queries wait in LDS as operands.
+// Q is brought to fp16 by a power of two per row, so that its largest magnitude lies in [2^13, 2^14), or as far up as 2^120 takes
+// it: exact down to 2^-27 of it.  Probabilities are rounded to fp16 at 2^7 times their size: eleven bits down to 2^-21 of the
+// reference, steps of 2^-31 of it below.  Values are fp16 numbers, too, scale and all, where the scale lies between 2^-15 and 2^7
+// (int8 2^-14 and 2^5).  All sums are fp32.
 //
 // Measured: 128 sequences x 8 heads of 100 to 16000 tokens (570 MB) 98 us, 5.8 TB/s; one sequence of 131072 tokens x 8 heads 47 us, and
 // 6 to join; a sequence of 777 tokens 10 us, of which the launch and three reads that wait for one another are eight.
@@ -48,10 +48,11 @@ struct Item {                                  // a place in the list of units
   int pair, len;                               // the head, and its length
   int tile, unit;                              // tile of rows, unit inside it; below 0 the beginning
 };
-// How the list is divided: `each` units a share, and `more` of the shares one more.  Those of waves by themselves: the first ones.  Those of
-// workgroups: evenly among the others, or shares and items of equal lengths drift apart, and more shares have the end of one item and the
-// beginning of another (128 rows x 8 heads x 32768 tokens, eight units a beginning: 51 us, 56 with the first ones, before other changes; the larger number of shares of
-// waves has less of it, and some power of two apart the longer ones meet on one compute unit: weights of those rows 31 us, 33 evenly).
+// How the list is divided: `each` units a share, and `more` of the shares one more.  Those of waves by themselves: the first
+// ones.  Those of workgroups: evenly among the others, or shares and items of equal lengths drift apart, and more shares have the
+// end of one item and the beginning of another (128 rows x 8 heads x 32768 tokens, eight units a beginning: 51 us, 56 with the
+// first ones, before other changes; the larger number of shares of waves has less of it, and some power of two apart the longer
+// ones meet on one compute unit: weights of those rows 31 us, 33 evenly).
 template <bool EVENLY>
 struct Shares {
   int each, more, n;                           // n: of shares, at most kCacheMaxWorkers; more is less
@@ -90,9 +91,10 @@ __device__ __forceinline__ void pair_units(const CacheAttnArgs& a, int rows, int
   }
 }
 
-// The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more than `few`
-// of them.  Up to 512 pairs every wave adds them up by itself, a lane a run of them; beyond, the four waves do it together, and each looks for
-// its place in the run where it lies, 64 pairs at a time.  (All units, beginnings and all, are below 2^30: the entry point sees to that.)
+// The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more
+// than `few` of them.  Up to 512 pairs every wave adds them up by itself, a lane a run of them; beyond, the four waves do it
+// together, and each looks for its place in the run where it lies, 64 pairs at a time.  (All units, beginnings and all, are below
+// 2^30: the entry point sees to that.)
 template <bool WEIGHTS, int ROWS, int START, class SHARES>
 __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int few, int* lds, int& begin, int& end, SHARES& shares) {
   const int pairs = a.c.n_seq * a.c.n_kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -242,8 +244,9 @@ __device__ __forceinline__ f16x8 key_operand(uint32_t x, uint32_t y) {
 __device__ __forceinline__ int page_number(const CacheArgs& c, int pair, int unit) {
   return scalar_load(c.table + int64_t(pair) * c.max_pages + (unit * kUnit >> c.block_log2));
 }
-// Where a unit's codes are.  Those of a page that is not in the pool are not loaded, zeros with scales of NaN: codes that are NaN themselves would reach
-// rows that see none of them.  (The scales come later than the codes are asked for, and are looked at when they are used.)
+// Where a unit's codes are.  Those of a page that is not in the pool are not loaded, zeros with scales of NaN: codes that are NaN
+// themselves would reach rows that see none of them.  (The scales come later than the codes are asked for, and are looked at when
+// they are used.)
 struct Page {
   int64_t byte;
   bool bad;
@@ -256,7 +259,8 @@ __device__ __forceinline__ Page page_at(const CacheArgs& c, int page, int unit) 
           scalar_load(c.v_scale + page)};
 }
 
-// Codes of a unit as a lane holds them: of K row 16 t + n16 bytes 64 x + 16 g and on, of V rows 32 kk + 16 half + 4 g + i dims 8 n16 and on.
+// Codes of a unit as a lane holds them: of K row 16 t + n16 bytes 64 x + 16 g and on, of V rows 32 kk + 16 half + 4 g + i dims 8
+// n16 and on.
 struct Keys {
   u32x4 code[4][2];
 };
@@ -300,8 +304,8 @@ struct Rows {
   float m[NT], l[NT];
   f32x4 acc[NT][8];
 };
-// ... and what does not change, which would cost registers: the queries as operands, what products are multiplied by and the keys seen.  What a lane
-// reads it wrote itself.
+// ... and what does not change, which would cost registers: the queries as operands, what products are multiplied by and the keys
+// seen.  What a lane reads it wrote itself.
 template <int NT>
 struct RowsLds {
   f16x8 q[NT][4][64];
@@ -329,9 +333,9 @@ __device__ __forceinline__ void ask_unit(const CacheAttnArgs& a, int page, int f
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// What a wave begins with: the rows from first_row on and the first unit of first, first + STEP .. below end (last: a unit whose place in the page
-// table can be read in any case).  Queries are on their way while the page is looked up, and are worked on while its codes are.  They go
-// into LDS, as each lane needs them: what it reads it wrote itself, and they cost no registers.
+// What a wave begins with: the rows from first_row on and the first unit of first, first + STEP .. below end (last: a unit whose
+// place in the page table can be read in any case).  Queries are on their way while the page is looked up, and are worked on
+// while its codes are.  They go into LDS, as each lane needs them: what it reads it wrote itself, and they cost no registers.
 // Returns whether there is a far_row().
 template <int NT, int STEP, bool ONCE>
 __device__ __forceinline__ bool begin_rows(const CacheAttnArgs& a, int pair, int h, int group, int row0, int n, int first_row, int seen_before, int first,
@@ -380,8 +384,8 @@ __device__ __forceinline__ void scores(const Keys& keys, const f16x8 (*lds_q)[4]
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Goes through the units first, first + STEP ..; seen_first: the fewest keys that a row sees (or kFar).  KEEP > 0: there are no more than that, and y of
-// each (-inf where it is masked) stays in `kept`.
+// Goes through the units first, first + STEP ..; seen_first: the fewest keys that a row sees (or kFar).  KEEP > 0: there are no
+// more than that, and y of each (-inf where it is masked) stays in `kept`.
 template <int NT, int STEP, bool ONCE, int FMT, int KEEP = 0>
 __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len, int first, int end, int last, int seen_first,
                                        const RowsLds<NT>& lds, int lane, Flight& f, Rows<NT>& r, f32x4 (*kept)[4] = nullptr) {
@@ -562,8 +566,9 @@ __device__ __forceinline__ void attend(const CacheAttnArgs& a, int pair, int len
   }
 }
 
-// 1 / denominator of a row: 0 of one that sees nothing, so that its output is; of a head whose length cannot be, NaN.  A row that sees
-// tokens and whose products are all -inf (a query that is not finite) has 1 / 0, which makes NaN of its output, its weights and its logarithm.
+// 1 / denominator of a row: 0 of one that sees nothing, so that its output is; of a head whose length cannot be, NaN.  A row that
+// sees tokens and whose products are all -inf (a query that is not finite) has 1 / 0, which makes NaN of its output, its weights
+// and its logarithm.
 __device__ __forceinline__ float row_inverse(bool good, int sees, float sum) {
   return !good ? __uint_as_float(kNanBits) : sees > 0 ? 1.0f / sum : 0.0f;
 }
@@ -571,10 +576,11 @@ __device__ __forceinline__ float row_lse(float top, float sum, float inv) {
   return (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f + 0.0f * inv;
 }
 
-// Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a workgroup, which
-// take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.  (For 128 rows x 8 heads x
-// 32768 int8 tokens 41 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.  Tiles side by side in a workgroup,
-// to read the codes from memory once, bring nothing.)  ITEMS: no shares, a workgroup an item, for short caches.
+// Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a
+// workgroup, which take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.
+// (For 128 rows x 8 heads x 32768 int8 tokens 41 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.
+// Tiles side by side in a workgroup, to read the codes from memory once, bring nothing.)  ITEMS: no shares, a workgroup an item,
+// for short caches.
 template <int NT, int WAVES, bool ITEMS, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a, int least) {
   constexpr bool kOwn = WAVES == 1;
@@ -721,11 +727,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
   }
 }
 
-// Joins the pieces of one row of an item: with M the largest m, out = sum 2^(m - M) O / sum 2^(m - M) l.  A workgroup a row (y) of an
-// item (x), or, where there are many of few pieces, a wave (THREADS = 64, four of them in a workgroup: a grid of 32768 rows, of which most have
-// nothing to join, takes 8 us, 10 with a workgroup each).  The first piece lies in slot 2 w + 1 of the share w it begins in, the others in 2 (w + 1), 2 (w + 2) ...; groups of
-// 32 lanes take turns at the pieces, a lane four dims, and what they have is added up in order.  What the first pieces hold is asked for
-// together with the statistics.
+// Joins the pieces of one row of an item: with M the largest m, out = sum 2^(m - M) O / sum 2^(m - M) l.  A workgroup a row (y)
+// of an item (x), or, where there are many of few pieces, a wave (THREADS = 64, four of them in a workgroup: a grid of 32768
+// rows, of which most have nothing to join, takes 8 us, 10 with a workgroup each).  The first piece lies in slot 2 w + 1 of the
+// share w it begins in, the others in 2 (w + 1), 2 (w + 2) ...; groups of 32 lanes take turns at the pieces, a lane four dims,
+// and what they have is added up in order.  What the first pieces hold is asked for together with the statistics.
 constexpr int join_threads(int threads) { return threads > 64 ? threads : kThreads; }
 
 template <int THREADS>
@@ -815,7 +821,8 @@ __global__ __launch_bounds__(join_threads(THREADS)) void cache_join_kernel(Cache
   }
 }
 
-// Sums over the sixteen lanes of a row of lanes, of which lane j is left with that of x[j]: every step halves the values a lane looks after.
+// Sums over the sixteen lanes of a row of lanes, of which lane j is left with that of x[j]: every step halves the values a lane
+// looks after.
 __device__ __forceinline__ float sums_of_rows(float (&x)[16], int lane) {
   const auto halve = [&](auto dpp, int n, bool upper) {
 #pragma unroll
@@ -838,9 +845,9 @@ struct Statistics {
   int seen[NT];
 };
 
-// The probabilities that the rows, of which there is one at least, put on each key of a unit, added up: a lane is left with those of key key_of_lane()
-// of the unit.  (A key whose product is NaN is one that a row sees, or masked: rows that are not there add nothing to others.)  The keys of
-// the next one are asked for on the way.
+// The probabilities that the rows, of which there is one at least, put on each key of a unit, added up: a lane is left with those
+// of key key_of_lane() of the unit.  (A key whose product is NaN is one that a row sees, or masked: rows that are not there add
+// nothing to others.)  The keys of the next one are asked for on the way.
 __device__ __forceinline__ int key_of_lane(int lane) { return ((lane & 15) >> 2) * 16 + (lane >> 4) * 4 + (lane & 3); }
 template <int NT, int FMT>
 __device__ __forceinline__ float weigh_unit(const CacheAttnArgs& a, int key0, const Page& ahead, bool more, int seen_first,
@@ -938,8 +945,8 @@ __device__ __forceinline__ void copy_weights(const CacheAttnArgs& a, int64_t row
   for (int key = first + me; key < end; key += threads) a.weight_out[row_of_weights + key] = a.weight_in != nullptr ? a.weight_in[row_of_weights + key] : 0.0f;
 }
 
-// The weights of the step by themselves, taken again from the keys and the rows' statistics: every key belongs to one share, so nothing is added up
-// between workgroups.  Up to 16 rows every wave has a share.
+// The weights of the step by themselves, taken again from the keys and the rows' statistics: every key belongs to one share, so
+// nothing is added up between workgroups.  Up to 16 rows every wave has a share.
 template <int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs a) {
   constexpr int kStart = start_units(1);
@@ -969,10 +976,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_kernel(CacheAttnArgs
   }
 }
 
-// More rows: a workgroup has the share, and its waves 32 rows each, up to 128 at a time.  Where there are fewer, 64 or 32, two or all
-// waves take turns at the units.  What the slices of rows put on the keys of kSteps units each meets in LDS.  (128 rows x 8 heads x 32768 int8
-// tokens: 30 us with a share for every wave and 64 rows at a time, of which beginning was the half, 26 so; VALU work,
-// turning the codes into fp16 for every 32 rows and the exponentials.)
+// More rows: a workgroup has the share, and its waves 32 rows each, up to 128 at a time.  Where there are fewer, 64 or 32, two or
+// all waves take turns at the units.  What the slices of rows put on the keys of kSteps units each meets in LDS.  (128 rows x 8
+// heads x 32768 int8 tokens: 30 us with a share for every wave and 64 rows at a time, of which beginning was the half, 26 so;
+// VALU work, turning the codes into fp16 for every 32 rows and the exponentials.)
 template <int FMT>
 __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAttnArgs a) {
   constexpr int kStart = start_units(kWaves), kSteps = 8, kSlice = 32;
@@ -1037,9 +1044,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_weight_rows_kernel(CacheAtt
   }
 }
 
-// A head a workgroup, eight waves taking turns at its units: output, denominators and weights in one launch, without partial results.  For
-// up to 16 rows and twice as many heads as there are compute units, in caches that leave a wave no more than kWholeUnits units, whose products stay in
-// registers until the weights can be told (48 sequences x 4 heads of up to 2000 tokens, 7 rows: 21 us with the keys gone through again, 15 so).
+// A head a workgroup, eight waves taking turns at its units: output, denominators and weights in one launch, without partial
+// results.  For up to 16 rows and twice as many heads as there are compute units, in caches that leave a wave no more than
+// kWholeUnits units, whose products stay in registers until the weights can be told (48 sequences x 4 heads of up to 2000 tokens,
+// 7 rows: 21 us with the keys gone through again, 15 so).
 constexpr int kWholeWaves = 8, kWholeUnits = 4;
 
 template <bool WEIGHTS, int FMT>
@@ -1141,25 +1149,27 @@ int32_t launch_format(const CacheAttnArgs& a, int rows, int most_rows, int compu
   const int64_t capacity = int64_t(a.c.max_pages) << a.c.block_log2;
   constexpr int kShort = kWholeWaves * kWholeUnits * kUnit;
   if (rows == 16 && pairs <= 2 * compute_units && capacity <= kShort) {
-    // (twice as many heads as compute units: 100 sequences x 4 heads of up to 1492 tokens with weights 18 us, and 13, 4 and 7 by shares; three times:
-    // 100 x 8 of up to 719 21, and 14 and 4)
+    // (twice as many heads as compute units: 100 sequences x 4 heads of up to 1492 tokens with weights 18 us, and 13, 4 and 7 by
+    // shares; three times: 100 x 8 of up to 719 21, and 14 and 4)
     if (a.weight_out != nullptr) cache_whole_kernel<true, FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
     else cache_whole_kernel<false, FMT><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
     return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
   }
   if (a.t.n_tokens > 0 && rows > 16 && (capacity <= kShort || (capacity <= 2 * kShort && int64_t(pairs) * a.tiles >= 2 * compute_units))) {
-    // item by item (48 sequences x 8 heads of up to 1498 tokens, 32 rows, 23 us, and 24 and 6 to join by shares; 100 x 8 of up to 615, 160 rows,
-    // 46, and 51 and 20; one of 900 x 8 heads, 128 rows, 14, and 11 and 4), also twice as long if there are items for all compute units (100 x 2 of
-    // up to 2861, 128 rows, 35, and 34 and 7): one that is much longer than the others keeps a compute unit for 30 us
+    // item by item (48 sequences x 8 heads of up to 1498 tokens, 32 rows, 23 us, and 24 and 6 to join by shares; 100 x 8 of up to
+    // 615, 160 rows, 46, and 51 and 20; one of 900 x 8 heads, 128 rows, 14, and 11 and 4), also twice as long if there are items
+    // for all compute units (100 x 2 of up to 2861, 128 rows, 35, and 34 and 7): one that is much longer than the others keeps a
+    // compute unit for 30 us
     cache_attn_kernel<2, kWaves, true, FMT><<<uint32_t(pairs) * a.tiles, kThreads, 0, stream>>>(a, 0);
   } else if (a.t.n_tokens > 0) {
-    // (three units at least where there is more than one share for every workgroup: waves that share a compute unit wait for one another's beginnings, and
-    // pieces are joined; five sequences of up to 39284 tokens x 2 heads 15 and 9 us with one unit, 13 and 5 with three, 12 and 5 with four; 16 up
-    // to 8000 13 and 7, 11 and 5, 12 and 4; one of 2048 x 8 heads, 272 units, 7 and 4 with one, 10 and 4 with three)
+    // (three units at least where there is more than one share for every workgroup: waves that share a compute unit wait for one
+    // another's beginnings, and pieces are joined; five sequences of up to 39284 tokens x 2 heads 15 and 9 us with one unit, 13
+    // and 5 with three, 12 and 5 with four; 16 up to 8000 13 and 7, 11 and 5, 12 and 4; one of 2048 x 8 heads, 272 units, 7 and 4
+    // with one, 10 and 4 with three)
     if (rows == 16) cache_attn_kernel<1, 1, false, FMT><<<grid, kThreads, 0, stream>>>(a, 3);
     else cache_attn_kernel<2, kWaves, false, FMT><<<grid, kThreads, 0, stream>>>(a, kWaves);
-    // few rows are of many pieces, many of few: 32 rows of 256 pieces (131072 tokens x 8 heads) take 6.6 us with 1024 threads each, 9 with 256; 4096 rows
-    // of one to four 5.4 with 64, 7 with 256
+    // few rows are of many pieces, many of few: 32 rows of 256 pieces (131072 tokens x 8 heads) take 6.6 us with 1024 threads
+    // each, 9 with 256; 4096 rows of one to four 5.4 with 64, 7 with 256
     const dim3 all(pairs * a.tiles, min(rows, most_rows));
     if (int64_t(all.x) * all.y <= 256) cache_join_kernel<1024><<<all, 1024, 0, stream>>>(a, rows);
     else if (int64_t(all.x) * all.y < 2048) cache_join_kernel<256><<<all, 256, 0, stream>>>(a, rows);

@@ -56,7 +56,8 @@ struct CacheAttnArgs {
   float* stats;                    // [n_tokens][n_q_heads][2]: reference exponent and 1 / denominator, for the weights
 };
 
-// Shares of an attention launch at most: of up to 16 rows every wave's own, of more a workgroup's; and rows of partial results, two tiles a share.
+// Shares of an attention launch at most: of up to 16 rows every wave's own, of more a workgroup's; and rows of partial results,
+// two tiles a share.
 constexpr int kCacheMaxWorkers = 2048;
 constexpr int64_t kCacheSlotRows = int64_t(2) * kCacheMaxWorkers * 16;
 static_assert(kCacheSlotRows >= int64_t(2) * (kCacheMaxWorkers / 4) * 32, "those of 32 rows, too");
@@ -129,9 +130,9 @@ __device__ __forceinline__ uint32_t larger_scale(uint32_t a, uint32_t b) {
   return max(int32_t(a), int32_t(b));
 }
 
-// The codes of four values times f, the inverse of their page's scale, to nearest, ties to even: the product is exact, the one rounding is
-// that of the conversion, in int8 that of adding 1.5 * 2^23.  `last`: the page has the largest scale there is, at which codes stay at those whose
-// values are finite (240 * 2^120 and 63 * 2^122; one step more is 2^128).
+// The codes of four values times f, the inverse of their page's scale, to nearest, ties to even: the product is exact, the one
+// rounding is that of the conversion, in int8 that of adding 1.5 * 2^23.  `last`: the page has the largest scale there is, at
+// which codes stay at those whose values are finite (240 * 2^120 and 63 * 2^122; one step more is 2^128).
 template <int FMT>
 __device__ __forceinline__ bool last_scale(uint32_t scale) { return scale >= (FMT == SHPLB_CACHE_E4M3 ? 247u : 249u) << 23; }
 template <int FMT>
@@ -204,7 +205,8 @@ __device__ __forceinline__ uint32_t half_codes(uint32_t w, float scale = 1.0f) {
 }
 template <int FMT>
 __device__ __forceinline__ uint32_t turned(uint32_t w) { return FMT == SHPLB_CACHE_E4M3 ? w : w ^ 0x80808080u; }
-// Whether all codes times this scale are fp16 numbers (in e4m3 448 * 2^7 and 2^-9 * 2^-15; in int8 so that the scale and 1152 times it are, too).
+// Whether all codes times this scale are fp16 numbers (in e4m3 448 * 2^7 and 2^-9 * 2^-15; in int8 so that the scale and 1152
+// times it are, too).
 template <int FMT>
 __device__ __forceinline__ bool fp16_scale(float scale) {
   const uint32_t b = __float_as_uint(scale), lowest = FMT == SHPLB_CACHE_E4M3 ? 127 - 15 : 127 - 14, most = FMT == SHPLB_CACHE_E4M3 ? 127 + 7 : 127 + 5;

@@ -1,9 +1,10 @@
 // Tokens into the pages of the 8-bit cache and out of them.
 //
-// All three kernels move bytes: a workgroup takes the keys or the values of one page, a page is one run of 8 or 16 KB.
-// append reads 256 and writes 128 bytes per token and head (twice, for K and V), load the other way round, evict (the gather of
-// the tokens that stay) reads and writes 128.  What is read or written once in a step, the 16-bit rows and what is evicted, leaves no trace in
-// the caches (32768 x 8 heads written 54 -> 42 us, 65536 x 2 read back 23 -> 17, the gather of an eviction of 131072 x 8 to a fifth 38 -> 32).
+// All three kernels move bytes: a workgroup takes the keys or the values of one page, a page is one run of 8 or 16 KB.  append
+// reads 256 and writes 128 bytes per token and head (twice, for K and V), load the other way round, evict (the gather of the
+// tokens that stay) reads and writes 128.  What is read or written once in a step, the 16-bit rows and what is evicted, leaves no
+// trace in the caches (32768 x 8 heads written 54 -> 42 us, 65536 x 2 read back 23 -> 17, the gather of an eviction of 131072 x 8
+// to a fifth 38 -> 32).
 #include "cache_common.h"
 
 namespace shplb {
@@ -24,9 +25,10 @@ __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // Workgroup: of a sequence's pages that the step touches one, a head, K or V.  A thread has eight dims of every sixteenth token.
-// SIDE_BY_SIDE: the heads of the same tokens, which lie side by side in the step's tensors, are neighbours (append, 32768 tokens x 8 heads
-// of a fused projection 86 -> 51 us, this and fewer registers).  Neighbours are on different dies, so a head is then always on the same two; load, whose heads
-// may have different lengths after an eviction, goes head after head (131072 tokens, one head whole, 62 -> 31 us).
+// SIDE_BY_SIDE: the heads of the same tokens, which lie side by side in the step's tensors, are neighbours (append, 32768 tokens
+// x 8 heads of a fused projection 86 -> 51 us, this and fewer registers).  Neighbours are on different dies, so a head is then
+// always on the same two; load, whose heads may have different lengths after an eviction, goes head after head (131072 tokens,
+// one head whole, 62 -> 31 us).
 struct PageOf {
   int pair, s, h, nth, which;      // nth page that the step touches
 };
@@ -156,13 +158,13 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 
-// Which tokens of a head stay: the want-th largest key among the tokens that may go is found eleven, eleven and ten bits at a time by counting
-// keys in bins; the tokens' places follow from how many keys in front of them lie above it or at it.
+// Which tokens of a head stay: the want-th largest key among the tokens that may go is found eleven, eleven and ten bits at a
+// time by counting keys in bins; the tokens' places follow from how many keys in front of them lie above it or at it.
 //
-// Of caches of up to 2 kRun positions a head is one workgroup's, from the first count to the last token written.  Longer
-// heads are cut into parts of up to kRun positions, and counting, counting, counting and writing are launches of their own: each begins by adding
-// up what the parts of its head counted in the launch before.  (8 heads of 13269 tokens: 15 us by one workgroup each, 25 and what lies
-// between launches in two parts; of 32525 53, with more weights than registers, and 26 in four; of 131072 28.)
+// Of caches of up to 2 kRun positions a head is one workgroup's, from the first count to the last token written.  Longer heads
+// are cut into parts of up to kRun positions, and counting, counting, counting and writing are launches of their own: each begins
+// by adding up what the parts of its head counted in the launch before.  (8 heads of 13269 tokens: 15 us by one workgroup each,
+// 25 and what lies between launches in two parts; of 32525 53, with more weights than registers, and 26 in four; of 131072 28.)
 constexpr int kBins = 2048, kEach = 8;                           // bins of a count, weights that a thread holds (of one workgroup's heads up to kMostEach)
 constexpr int kSelectThreads = 1024, kFewThreads = 256, kMostEach = 16, kRun = kSelectThreads * kEach;
 static_assert((int64_t(SHPLB_MAX_BLOCKS) * 128 + kRun - 1) / kRun * SHPLB_MAX_SEQ_HEADS * kSelectThreads <= int64_t(UINT32_MAX), "a grid for all parts");
@@ -498,7 +500,8 @@ int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int3
   const SelectArgs a{src, dst, weight, keep, n_sink, n_recent, parts, weight_out, kept, bins, bins + pairs * parts * 3 * kBins};
   const dim3 all(uint32_t(pairs * parts));
   if (parts == 1) {
-    // as few threads and weights of each as there can be (48 sequences x 4 heads of up to 2000 tokens: 7.8 us with 1024 threads, 7.3 with 256)
+    // as few threads and weights of each as there can be (48 sequences x 4 heads of up to 2000 tokens: 7.8 us with 1024 threads,
+    // 7.3 with 256)
     const int64_t capacity = int64_t(src.max_pages) << src.block_log2;
     if (capacity <= kFewThreads * kEach) evict_select_kernel<-1, kFewThreads, kEach><<<all, kFewThreads, 0, stream>>>(a);
     else if (capacity <= kRun) evict_select_kernel<-1, kSelectThreads, kEach><<<all, kSelectThreads, 0, stream>>>(a);
