@@ -8,6 +8,7 @@
  *   shplb_select_topk_per_head  per-head top-k key-block selection
  *   shplb_sparse_attn_prefill   block-sparse causal attention over the selection,
  *                               work items dealt to compute units by descending cost
+ *   shplb_window_attn_prefill   causal attention with a sliding window and first tokens that stay visible
  *   shplb_balance_heads         greedy head-to-partition assignment (host)
  *   shplb_shift_budgets         max-min budget shifting: the producer of the budgets (host)
  *   shplb_block_mass            offline recovery profile: attention weight per block pair
@@ -220,6 +221,22 @@ SHPLB_API int32_t shplb_sparse_attn_prefill_split(const shplb_problem* p, const 
                                         const void* v, const int64_t* sel_ptr, const int32_t* sel_idx,
                                         void* out, float* lse_out, void* sched_stats_out,
                                         void* workspace, int32_t split_slots, void* stream);
+
+/* Causal attention (Eq. 1) in which every token sees the last `window` tokens up to itself and the first n_sink
+ * of its sequence (the sink + recent pattern of Section 2.3, by tokens instead of blocks): position p sees
+ * the positions t <= p with t > p - window or t < n_sink.  Any window >= 1 and n_sink >= 0; a window that
+ * no sequence is longer than gives full causal attention.
+ *   - A step beside shplb_sparse_attn_prefill for layers whose heads all have this pattern; it needs neither scores
+ *     nor a selection nor a workspace.  The problem's `block` only limits the sequences' length.
+ *   - bf16 products, sums in fp32; probabilities are rounded to bf16 before they meet the values, not
+ *     before they are added up.  Results are bit-identical from run to run; in calls of at most as many
+ *     rows (of 128 queries) as there are compute units a sum may be taken in another order than in larger ones.
+ *   - A key or value that is infinite or NaN reaches the tokens that see it, and no others.
+ *   q, k, v: device bf16; out: device bf16, strides as Q, in other memory than q, k and v;
+ *   lse_out: device fp32 [n_q_heads, T], natural logarithm of the softmax denominators, or NULL.
+ * Errors: SHPLB_E_NULL, SHPLB_E_SHAPE, SHPLB_E_UNSUPPORTED as above; SHPLB_E_BUDGET (window < 1 or n_sink < 0). */
+SHPLB_API int32_t shplb_window_attn_prefill(const shplb_problem* p, int32_t n_sink, int32_t window, const void* q, const void* k,
+                                  const void* v, void* out, float* lse_out, void* stream);
 
 /* ---- offline profile ------------------------------------------------------- */
 

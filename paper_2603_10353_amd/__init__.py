@@ -40,5 +40,6 @@ from .binding import (  # noqa: F401
     shplb_strerror,
     shplb_token_recovery,
     shplb_token_recovery_heads,
+    shplb_window_attn_prefill,
     shplb_workspace_bytes,
 )

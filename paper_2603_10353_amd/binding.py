@@ -14,6 +14,7 @@ EXPORTS = [
     "shplb_num_rows", "shplb_max_blocks", "shplb_workspace_bytes", "shplb_score_layout", "shplb_sel_row_ptr",
     "shplb_sched_num_workgroups", "shplb_block_scores", "shplb_select_topk_per_head",
     "shplb_sparse_attn_prefill", "shplb_sparse_attn_prefill_static", "shplb_split_workspace_bytes", "shplb_sparse_attn_prefill_split",
+    "shplb_window_attn_prefill",
     "shplb_balance_heads", "shplb_shift_budgets", "shplb_block_mass",
     "shplb_recovery_curves", "shplb_token_recovery", "shplb_token_recovery_heads", "shplb_probe_mfma_rate",
     "shplb_cache_append", "shplb_cache_load", "shplb_cache_attn_workspace_bytes", "shplb_cache_attn",
@@ -126,6 +127,7 @@ def load_library():
     lib.shplb_sparse_attn_prefill_static.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.shplb_split_workspace_bytes.argtypes = [pp, i32, C.POINTER(i64)]
     lib.shplb_sparse_attn_prefill_split.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]
+    lib.shplb_window_attn_prefill.argtypes = [pp, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.shplb_balance_heads.argtypes = [C.POINTER(i64), i32, i32, i32, C.POINTER(i32), C.POINTER(i64)]
     lib.shplb_probe_mfma_rate.argtypes = [i32, i32, i32, vp, vp]
     lib.shplb_block_mass.argtypes = [pp, vp, vp, vp, vp]
@@ -331,6 +333,11 @@ def shplb_sparse_attn_prefill_split(p: Problem, q, k, v, sel_ptr, sel_idx, out, 
                                                           _dev(sched_stats_out), _dev(workspace),
                                                           int(split_slots), _stream(stream)),
            "shplb_sparse_attn_prefill_split")
+
+
+def shplb_window_attn_prefill(p: Problem, n_sink: int, window: int, q, k, v, out, lse_out=None, stream=None) -> None:
+    _check(load_library().shplb_window_attn_prefill(p.ref(), int(n_sink), int(window), _dev(q), _dev(k), _dev(v), _dev(out),
+                                                    _dev(lse_out), _stream(stream)), "shplb_window_attn_prefill")
 
 
 def shplb_balance_heads(costs, n_parts: int, max_per_part: int = 0):

@@ -305,6 +305,22 @@ int32_t shplb_sparse_attn_prefill_split(const shplb_problem* p, const void* q, c
                          stream);
 }
 
+int32_t shplb_window_attn_prefill(const shplb_problem* p, int32_t n_sink, int32_t window, const void* q, const void* k, const void* v,
+                                  void* out, float* lse_out, void* stream) {
+  if (!p || !q || !k || !v || !out) return SHPLB_E_NULL;
+  if (n_sink < 0 || window < 1) return SHPLB_E_BUDGET;
+  if (p->q_stride_h >= int64_t(1) << 24 || p->kv_stride_h >= int64_t(1) << 24) return SHPLB_E_UNSUPPORTED;
+  Geometry g;
+  if (int32_t st = make_geometry(p, &g)) return st;
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(out)) & 15)
+    return SHPLB_E_SHAPE;
+  if (reinterpret_cast<uintptr_t>(lse_out) & 3) return SHPLB_E_SHAPE;
+  if (out == q || out == k || out == v) return SHPLB_E_SHAPE;     // they are read again after the first outputs are written
+  const int32_t n_wg = persistent_workgroups();
+  if (n_wg < 0) return n_wg;
+  return launch_window_attn(g, n_sink, window, q, k, v, out, lse_out, n_wg / 2, static_cast<hipStream_t>(stream));
+}
+
 // Offline recovery profile of Section 2.4 at block granularity: a dense causal pass.
 int32_t shplb_block_mass(const shplb_problem* p, const void* q, const void* k, float* mass_out, void* stream) {
   if (!q || !k || !mass_out) return SHPLB_E_NULL;

@@ -78,6 +78,8 @@ int32_t launch_select(const Geometry& g, const float* scores, const int64_t* sel
 int32_t launch_order(const Geometry& g, const int64_t* sel_ptr, const int32_t* sel_idx, const WorkspaceLayout& w,
                      char* workspace, int32_t n_wg, int32_t grid, bool halves, hipStream_t stream);
 int32_t launch_mfma_rate(int random_operands, int iters, int n_workgroups, void* scratch, hipStream_t stream);
+int32_t launch_window_attn(const Geometry& g, int32_t n_sink, int32_t window, const void* q, const void* k, const void* v, void* out, float* lse,
+                           int32_t compute_units, hipStream_t stream);
 int32_t launch_block_mass(const Geometry& g, const void* q, const void* k, float* mass, hipStream_t stream);
 int32_t launch_token_recovery(const Geometry& g, const void* q, const void* k, const int32_t* budgets,
                               int32_t n_budgets, float* recovery, hipStream_t stream);

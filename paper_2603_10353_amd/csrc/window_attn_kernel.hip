@@ -1,0 +1,434 @@
+// Causal attention with a sliding window and first tokens that stay visible (gfx950).
+//
+// For a query at position p of its sequence, over the positions t <= p with t > p - window or t < n_sink:
+//
+//   s_t = (q . k_t) * scale * log2(e),  m a reference near max s,  l = sum 2^(s_t - m),  out = sum 2^(s_t - m) v_t / l,  lse = (m + log2 l) ln 2,
+//
+// in one pass over the keys.  Bound by the products: 512 FLOP for every query head and visible pair, 2 window / (1 + 2 / G) and more
+// of them for a byte of K and V.
+//
+// Split.  A work item is a tile of 64 QG queries of one head; it goes through the 64-key tiles that any of its queries sees: those
+// of the first tokens, then those of the window (tile u of the item is key tile u below `sinks`, u + skip from there on).  Items cost
+// about the same, so they are dealt out in rounds, without queues: workgroup b of a grid of 8 n takes place (b % 8) n + b / 8 of
+// every round, so that a die has a run of neighbouring items, which share heads and most of a window in its L2.
+//
+// Tile.  That of attn_pipe_kernel.hip: four waves of 16 QG queries, S^T = K Q^T and O^T = V^T P^T in 16x16x32 products, K and V copied
+// from memory to two LDS stages each, softmax of a tile in front of the next tile's first product and its own second one.  Beside it:
+//  - tiles that all queries see whole have no masks; a wave leaves out those of which its own queries see nothing;
+//  - a query may see nothing of the first tiles: its reference is -infinity until it does, and is then raised at once;
+//  - denominators are sums of the fp32 probabilities (products use them rounded to bf16, as V is), so that lse keeps fp32's precision;
+//  - a value that is infinite or NaN must not reach queries that do not see it, to which a product would carry it as 0 * NaN.  Tiles
+//    with masks are therefore looked through for such values, and where there are some, the products are taken one by one.
+#include "attn_common.h"
+
+namespace shplb {
+namespace {
+
+struct WindowArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  float* lse;                                // or null
+  Strides st;
+  int64_t total_tokens;
+  float scale_log2;
+  int32_t window, n_sink;                    // at most 2^30 each
+  int32_t n_seq, n_q_heads, items;
+  int32_t group;                             // query heads per KV head; 0: kv_of names them
+  int32_t tok_begin[SHPLB_MAX_SEQ + 1];
+  int32_t tile_begin[SHPLB_MAX_SEQ + 1];     // tiles of queries in front of each sequence
+  uint32_t kv_of[SHPLB_MAX_MAPPED_HEADS / 4];
+};
+
+constexpr int kKeys = 64, kTileBytes = kKeys * kRowBytes, kWaves = 4, kThreads = 64 * kWaves;
+
+struct WindowItem {                          // all the same in all lanes
+  int head, kv_head, seq_begin, len, q0;
+  int sinks, skip, tiles;                    // key tiles: see above; at least two (one behind all that is visible does no harm)
+  __device__ __forceinline__ int key0(int u) const { return kKeys * (u < sinks ? u : u + skip); }
+};
+
+template <int BQ>
+__device__ __forceinline__ WindowItem window_item(const WindowArgs& a, int place) {
+  WindowItem it;
+  const auto scalar = [](int x) { return int(__builtin_amdgcn_readfirstlane(x)); };
+  int s = 0;
+  if (a.n_seq > 1) {
+    const int lane = threadIdx.x & 63;
+    s = __builtin_popcountll(__ballot(lane < a.n_seq - 1 && place >= a.tile_begin[lane + 1] * a.n_q_heads));
+  }
+  const int t0 = scalar(a.tile_begin[s]), nt = scalar(a.tile_begin[s + 1]) - t0, local = place - t0 * a.n_q_heads;
+  const int group = a.group > 0 ? a.group : 1;
+  const int run = scalar(uint32_t(local) / uint32_t(nt * group)), rest = local - run * nt * group;     // heads that share keys, tile by tile
+  const int tile = scalar(uint32_t(rest) / uint32_t(group));
+  it.head = run * group + rest - tile * group;
+  it.kv_head = a.group > 0 ? run : scalar(int(a.kv_of[it.head >> 2] >> (8 * (it.head & 3)) & 0xff));
+  it.seq_begin = scalar(a.tok_begin[s]);
+  it.len = scalar(a.tok_begin[s + 1]) - it.seq_begin;
+  it.q0 = tile * BQ;
+  const int hi = min(it.q0 + BQ, it.len), lo = max(it.q0 - a.window + 1, 0);
+  const int end = (hi + kKeys - 1) / kKeys, first = lo / kKeys;
+  it.sinks = min((min(a.n_sink, hi) + kKeys - 1) / kKeys, end);
+  it.skip = max(first - it.sinks, 0);
+  it.tiles = max(end - it.skip, 2);
+  return it;
+}
+
+// A pointer that is the same in all lanes, said explicitly: in scalar registers.
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const char*>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x)))) |
+                                       uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32)))) << 32);
+}
+
+// QG: groups of 16 queries of a wave.
+template <int QG>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_attn_kernel(WindowArgs a) {
+  constexpr int BQ = 64 * QG, MT = kKeys / 16, kQK = 4 * MT, kPV = 8 * (kKeys / 32);
+  constexpr int kLook = 8;                   // LDS operands are fetched so far ahead
+  // a lane's 16 probabilities of a query and tile can only sum to more if one of them exceeds 2^8
+  constexpr float kSumLimit = 4.0f * MT * 256.0f;
+  constexpr int kStores = 4 * QG;            // 16-byte stores of a lane
+
+  __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];         // two stages of K, two of V
+  __shared__ int s_bad;                      // the last step whose values are not all finite
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, hi = lane >> 4, q_wave = 16 * QG * wave;
+  const int64_t row_bytes = a.st.kv_t * 2;
+
+  // copies: a wave moves four rows at a time, row 16 r + cp_row of the tile in round r, 16-byte chunk c of it to slot c ^ swz(row)
+  const int cp_row = 4 * wave + (lane >> 4);
+  const uint32_t cp_chunk = ((lane & 15) ^ swz(cp_row)) << 4, cp_off = uint32_t(cp_row) * uint32_t(row_bytes) + cp_chunk;
+  // K operands: lane (n, hi) reads row 16 mt + n, chunk 4 ks + hi; V's by transpose reads (see attn_pipe_kernel.hip)
+  const int k_rd0 = n * kRowBytes + ((hi ^ swz(n)) << 4);
+  const int tr_row = 4 * hi + ((lane >> 2) & 3), tr_a = lane & 3;
+  const int v_rd0 = tr_row * kRowBytes + (((tr_a >> 1) ^ swz(tr_row)) << 4) + 8 * (tr_a & 1);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_offset_of(lds) + 4 * wave * kRowBytes);
+  if (tid == 0) s_bad = -1;
+
+  const int per_die = int(gridDim.x) / kXcds;
+  int place = int(blockIdx.x) % kXcds * per_die + int(blockIdx.x) / kXcds;
+  if (place >= a.items) return;
+  WindowItem it = window_item<BQ>(a, place);
+  bf16x8 qf[QG][4];
+
+  const auto copy_tile = [&](const uint16_t* base, const WindowItem& w, int u, uint32_t dst) {
+    const int at = min(w.key0(u), w.len - 1), last = w.len - 1 - at;
+    const char* tile = uniform(reinterpret_cast<const char*>(base + int64_t(w.kv_head) * a.st.kv_h) + (int64_t(w.seq_begin) + at) * row_bytes);
+    if (last >= kKeys - 1) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) copy_g2l_16(tile + int64_t(16 * r) * row_bytes, cp_off, dst + 16 * r * kRowBytes);
+    } else {                                 // rows behind the end: the last token again (masked)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) copy_g2l_16(tile, uint32_t(min(16 * r + cp_row, last)) * uint32_t(row_bytes) + cp_chunk, dst + 16 * r * kRowBytes);
+    }
+  };
+  const auto copy_k = [&](const WindowItem& w, int u, int stage) { copy_tile(a.k, w, u, lds0 + stage * kTileBytes); };
+  const auto copy_v = [&](const WindowItem& w, int u, int stage) { copy_tile(a.v, w, u, lds0 + (2 + stage) * kTileBytes); };
+  // what an item begins with, into stages that are free: its first tiles and its queries (operand B: dims 32 ks + 8 hi and on of
+  // query 16 qg + n)
+  const auto start_item = [&](const WindowItem& w, int stage) {
+    copy_k(w, 0, stage);
+#pragma unroll
+    for (int qg = 0; qg < QG; ++qg) {
+      const int tok = w.seq_begin + min(w.q0 + q_wave + 16 * qg + n, w.len - 1);
+      const uint16_t* src = a.q + int64_t(tok) * a.st.q_t + int64_t(w.head) * a.st.q_h + 8 * hi;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) qf[qg][ks] = *reinterpret_cast<const bf16x8*>(src + 32 * ks);
+    }
+    copy_v(w, 0, stage);
+    copy_k(w, 1, stage ^ 1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  int stage = 0, step_no = 0;                // tile u of an item is in stage (its first one's + u) mod 2
+  start_item(it, 0);
+  wait_vmem_all();
+  for (;;) {
+#pragma unroll
+    for (int qg = 0; qg < QG; ++qg) asm volatile("" : "+v"(qf[qg][0]), "+v"(qf[qg][1]), "+v"(qf[qg][2]), "+v"(qf[qg][3]));
+    f32x4 sc[QG][MT], acc[QG][8];
+    float m_ref[QG], l_run[QG];
+    int q_pos[QG];                           // (queries behind the end of the sequence: the last one again)
+#pragma unroll
+    for (int qg = 0; qg < QG; ++qg) {
+      q_pos[qg] = min(it.q0 + q_wave + 16 * qg + n, it.len - 1);
+      m_ref[qg] = -INFINITY;
+      l_run[qg] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) acc[qg][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // positions of the tile's first and last query, and of the wave's
+    const int first = it.q0, last = min(it.q0 + BQ, it.len) - 1;
+    const int w_first = min(first + q_wave, last), w_last = min(first + q_wave + 16 * QG - 1, last);
+    const auto masked = [&](int key0, int lo, int up) { return key0 + kKeys - 1 > lo || (key0 <= up - a.window && key0 + kKeys > a.n_sink); };
+    const auto hidden = [&](int key0) { return key0 > w_last || (key0 + kKeys - 1 <= w_first - a.window && key0 >= a.n_sink); };
+
+    const auto read_k = [&](const char* kt, int gi) {
+      const int ks = gi / MT, mt = gi % MT;
+      return *reinterpret_cast<const bf16x8*>(kt + (k_rd0 ^ (ks << 6)) + mt * 16 * kRowBytes);
+    };
+    const auto read_v = [&](const char* vt, int gi) {
+      const int gq = gi >> 3, dt = gi & 7;
+      const char* at = vt + (v_rd0 ^ (dt << 5)) + gq * 32 * kRowBytes;
+      const s16x4 lo = lds_read_tr16(at), up = lds_read_tr16(at + 16 * kRowBytes);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const auto tile_max = [&](int qg) {
+      float mx = sc[qg][0][0];
+#pragma unroll
+      for (int x = 1; x < 4 * MT; ++x) mx = fmaxf(mx, sc[qg][x >> 2][x & 3]);
+      return mx;
+    };
+    // scores of the tile at key0 from its stage, with masks
+    const auto scores = [&](const char* kt, int key0) {
+      bf16x8 kf[kQK];
+#pragma unroll
+      for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sc[qg][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int gi = 0; gi < kLook; ++gi) kf[gi] = read_k(kt, gi);
+#pragma unroll
+      for (int gi = 0; gi < kQK; ++gi) {
+        if (gi + kLook < kQK) kf[gi + kLook] = read_k(kt, gi + kLook);
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg)
+          sc[qg][gi % MT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[gi], qf[qg][gi / MT], sc[qg][gi % MT], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (masked(key0, w_first, w_last)) {
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg) {
+          int d = key0 + 4 * hi - q_pos[qg], e = key0 + 4 * hi - a.n_sink;
+          asm volatile("" : "+v"(d), "+v"(e));
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int rel = d + (16 * mt + r);
+              if (rel > 0 || (rel <= -a.window && e + (16 * mt + r) >= 0)) sc[qg][mt][r] = -INFINITY;
+            }
+            asm volatile("" : "+v"(sc[qg][mt]));
+          }
+        }
+      }
+    };
+
+    // ---- S(0).  (The item's copies have landed in this wave: see the end of the loop.)
+    __syncthreads();
+    if (!hidden(it.key0(0))) scores(lds + stage * kTileBytes, it.key0(0));
+
+    const int next_place = place + int(gridDim.x);
+    const bool more = next_place < a.items;
+    WindowItem next = it;
+#pragma unroll 1
+    for (int u = 0; u < it.tiles; ++u) {
+      const int key0 = it.key0(u), key1 = it.key0(u + 1);
+      const bool ends = u + 1 == it.tiles, mine = !hidden(key0), checked = masked(key0, first, last);
+      const char* const vt = lds + (2 + stage) * kTileBytes;
+      __builtin_amdgcn_s_setprio(0);
+      wait_vmem_all();                       // own copies of K(u + 1), V(u) have landed ...
+      __syncthreads();                       // ... and everyone's; the stages of K(u) and V(u - 1) are free
+      if (!ends) {
+        copy_v(it, u + 1, stage ^ 1);
+        if (u + 2 < it.tiles) copy_k(it, u + 2, stage);
+      } else if (more) {
+        next = window_item<BQ>(a, next_place);
+        start_item(next, stage ^ 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (checked) {
+        // whether all values are finite, a quarter of them looked at by each wave
+        u32x4 top = {0, 0, 0, 0};
+#pragma unroll
+        for (int x = 0; x < kTileBytes / (16 * kThreads); ++x) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(vt + (x * kThreads + tid) * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top[e] = max(max(top[e], w[e] << 16 & 0x7fff0000u), w[e] & 0x7fff0000u);
+        }
+        const uint32_t most = max(max(top[0], top[1]), max(top[2], top[3]));
+        if (__ballot(most >= 0x7f800000u) != 0 && lane == 0) s_bad = step_no;
+      }
+
+      // ---- probabilities of tile u
+      uint32_t pk[QG][MT][2];
+      float rs[QG];
+      const auto probabilities = [&]() {
+        float sum[QG][2];
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg) sum[qg][0] = sum[qg][1] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < 2 * QG * MT; ++x) {       // two probabilities of a query group, the groups in turn
+          const int qg = x % QG, mt = x / (2 * QG), c = x / QG % 2;
+          const float m_use = m_ref[qg] == -INFINITY ? 0.0f : m_ref[qg];
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qg][mt][2 * c], a.scale_log2, -m_use));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qg][mt][2 * c + 1], a.scale_log2, -m_use));
+          pk[qg][mt][c] = pack_bf16(p0, p1);
+          sum[qg][0] += p0;
+          sum[qg][1] += p1;
+        }
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg) rs[qg] = sum[qg][0] + sum[qg][1];
+      };
+      if (mine) {
+        probabilities();
+        // The reference was fixed by earlier tiles: it is too low for this one where a probability, and with it the sum, came out
+        // large, or where there was none.  Then it is raised to the tile's maximum.
+        const auto too_low = [&](int qg) { return !(rs[qg] <= kSumLimit) || m_ref[qg] == -INFINITY; };
+        if (__any(too_low(0) || too_low(QG - 1))) {
+#pragma unroll
+          for (int qg = 0; qg < QG; ++qg) {
+            const float m_tile = quad_max(tile_max(qg)) * a.scale_log2;
+            const float m_new = fmaxf(m_ref[qg], m_tile);
+            const float alpha = m_new == m_ref[qg] ? 1.0f : __builtin_amdgcn_exp2f(m_ref[qg] - m_new);
+            m_ref[qg] = m_new;
+            l_run[qg] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) acc[qg][dt] *= alpha;
+          }
+          probabilities();
+        }
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg) l_run[qg] += rs[qg];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+
+      // ---- S(u + 1)
+      __builtin_amdgcn_s_setprio(1);
+      if (!ends && !hidden(key1)) scores(lds + (stage ^ 1) * kTileBytes, key1);
+
+      // ---- O^T += V(u)^T P(u)^T
+      bool bad = false;
+      if (checked) {
+        __syncthreads();
+        bad = s_bad == step_no;
+      }
+      if (mine && !bad) {
+        bf16x8 vf[kPV];
+#pragma unroll
+        for (int gi = 0; gi < kLook; ++gi) vf[gi] = read_v(vt, gi);
+#pragma unroll
+        for (int gi = 0; gi < kPV; ++gi) {
+          if (gi + kLook < kPV) vf[gi + kLook] = read_v(vt, gi + kLook);
+          const int gq = gi >> 3, dt = gi & 7;
+#pragma unroll
+          for (int qg = 0; qg < QG; ++qg) {
+            const u32x4 w = {pk[qg][2 * gq][0], pk[qg][2 * gq][1], pk[qg][2 * gq + 1][0], pk[qg][2 * gq + 1][1]};
+            acc[qg][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[gi], __builtin_bit_cast(bf16x8, w), acc[qg][dt], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else if (mine) {
+        // one by one, of visible keys only: the probabilities of key 16 mt + 4 x + 2 c + y are with the lanes hi = x
+#pragma unroll 1
+        for (int kk = 0; kk < kKeys; ++kk) {
+          float p[QG];
+          bool seen[QG];
+#pragma unroll
+          for (int qg = 0; qg < QG; ++qg) {
+            uint32_t w = pk[qg][0][0];
+#pragma unroll
+            for (int x = 1; x < 2 * MT; ++x) w = (kk >> 4) * 2 + (kk >> 1 & 1) == x ? pk[qg][x >> 1][x & 1] : w;
+            w = kk & 1 ? w & 0xffff0000u : w << 16;
+            p[qg] = __uint_as_float(__shfl(int(w), n + 16 * (kk >> 2 & 3)));
+            const int rel = key0 + kk - q_pos[qg];
+            seen[qg] = rel <= 0 && (rel > -a.window || key0 + kk < a.n_sink);
+          }
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(vt + kk * kRowBytes + (((2 * dt + (hi >> 1)) ^ swz(kk & 15)) << 4) + 8 * (hi & 1));
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float x = __uint_as_float(r & 1 ? w[r >> 1] & 0xffff0000u : w[r >> 1] << 16);
+                acc[qg][dt][r] += seen[qg] ? p[qg] * x : 0.0f;
+              }
+          }
+        }
+      }
+      stage ^= 1;
+      ++step_no;
+    }
+    __builtin_amdgcn_s_setprio(0);
+
+    // ---- out: a lane has dims 16 dt + 4 hi + r of its queries; neighbours trade, and a lane stores eight dims at a time
+    const int n_valid = it.len - it.q0;
+    const auto store_rows = [&](bool all) {
+#pragma unroll
+      for (int qg = 0; qg < QG; ++qg) {
+        const int q_at = q_wave + 16 * qg + n;
+        const bool valid = all || q_at < n_valid;
+        const float l = quad_sum(l_run[qg]), inv = 1.0f / l;
+        const int64_t tok = int64_t(it.seq_begin) + it.q0 + min(q_at, n_valid - 1);
+        if (a.lse != nullptr && hi == 0 && valid) a.lse[int64_t(it.head) * a.total_tokens + tok] = (m_ref[qg] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        uint16_t* dst = a.out + tok * a.st.q_t + int64_t(it.head) * a.st.q_h + 16 * (hi & 1) + 8 * (hi >> 1);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const f32x4 &x = acc[qg][2 * p], &y = acc[qg][2 * p + 1];
+          uint32_t e0 = pack_bf16(x[0] * inv, x[1] * inv), e1 = pack_bf16(x[2] * inv, x[3] * inv);
+          uint32_t o0 = pack_bf16(y[0] * inv, y[1] * inv), o1 = pack_bf16(y[2] * inv, y[3] * inv);
+          swap_rows(e0, o0);
+          swap_rows(e1, o1);
+          if (valid) *reinterpret_cast<u32x4*>(dst + 32 * p) = u32x4{e0, e1, o0, o1};
+        }
+      }
+    };
+    // The next item's copies and queries were asked for before these stores, and a wave's vector memory operations complete in
+    // order: with no more than the stores under way they are there.
+    if (q_wave + 16 * QG <= n_valid) {
+      store_rows(true);
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::: "memory");
+      wait_vmem_but(std::integral_constant<int, kStores>{});
+    } else {
+      store_rows(false);
+      wait_vmem_all();
+    }
+    if (!more) break;
+    place = next_place;
+    it = next;
+  }
+}
+
+}  // namespace
+
+int32_t launch_window_attn(const Geometry& g, int32_t n_sink, int32_t window, const void* q, const void* k, const void* v, void* out, float* lse, int32_t compute_units,
+                           hipStream_t stream) {
+  WindowArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.st = g.st;
+  a.total_tokens = g.total_tokens;
+  a.scale_log2 = g.scale * 1.4426950408889634f;
+  a.window = window < 1 << 30 ? window : 1 << 30;
+  a.n_sink = n_sink < 1 << 30 ? n_sink : 1 << 30;
+  a.n_seq = g.meta.n_seq;
+  a.n_q_heads = g.meta.n_q_heads;
+  a.group = g.meta.kv_map ? 0 : g.meta.n_q_heads / g.meta.n_kv_heads;
+  for (int x = 0; x < SHPLB_MAX_MAPPED_HEADS / 4; ++x) a.kv_of[x] = g.meta.kv_of[x];
+  const auto deal = [&](int rows) {
+    int64_t tiles = 0;
+    for (int s = 0; s < a.n_seq; ++s) {
+      a.tok_begin[s] = g.meta.tok_begin[s];
+      a.tile_begin[s] = int32_t(tiles);
+      tiles += (int64_t(g.meta.tok_begin[s + 1]) - g.meta.tok_begin[s] + rows - 1) / rows;
+    }
+    a.tok_begin[a.n_seq] = g.meta.tok_begin[a.n_seq];
+    a.tile_begin[a.n_seq] = int32_t(tiles);
+    return tiles * a.n_q_heads;
+  };
+  int64_t items = deal(128);
+  const bool half = items <= compute_units;
+  if (half) items = deal(64);
+  a.items = int32_t(items);                                      // (at most 2^30: make_geometry())
+  const int grid = int((min(items, int64_t(2) * compute_units) + kXcds - 1) / kXcds * kXcds);
+  if (half) window_attn_kernel<1><<<grid, kThreads, 0, stream>>>(a);
+  else window_attn_kernel<2><<<grid, kThreads, 0, stream>>>(a);
+  return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
+}
+
+}  // namespace shplb

@@ -1,0 +1,30 @@
+"""What the tests of windows and shared prefixes have in common: the comparison with the oracle."""
+from __future__ import annotations
+
+import numpy as np
+
+
+def check(want, got_out, got_lse, rows, keys, half_probability, lift=0.0):
+    """Against the oracle's Result on these rows.  Tolerances, each a sum of what rounds: a score is a sum of 128 exact products in
+    fp32, in an order and with intermediate roundings of the matrix pipe's own (two halves of a step each): 2 * 130 * 2^-24 of the
+    sum of their magnitudes, and as much as 2^-23 of itself for each of three multiplications; a probability moves by as much as its
+    score and the denominator's logarithm do, 2^-22 for each exponential, the additions of the denominator, `keys` of them at most
+    taken 64 apart, and eight times the output is scaled, 2^-22 each; probabilities are rounded before they meet the values, by
+    half_probability of themselves or lift of the reference; the result in bf16, 2^-8."""
+    dz = want.reach * (2 * 130 * 2.0 ** -24 + 3 * 2.0 ** -23)
+    dp = 2 * dz + 2.0 ** -21 + (keys / 64 + 80) * 2.0 ** -24 + 8 * 2.0 ** -22
+    out, lse = want.out[rows], want.lse[:, rows]
+    a = got_out[rows]
+    assert (np.isnan(a) == np.isnan(out)).all(), "NaN where there is none, or none where there is"
+    infinite = np.isinf(out)
+    assert (a[infinite] == out[infinite]).all()
+    fine = np.isfinite(out)
+    tol = 2.0 ** -8 * np.abs(out) + (half_probability + dp) * want.size[rows] * (1 + 2.0 ** -8) + lift * want.all_v[rows] + 1e-30
+    worst = float((np.abs(a - out)[fine] / tol[fine]).max(initial=0.0))
+    assert worst <= 1.0, "output off by %.3g of the tolerance" % worst
+    if got_lse is not None:
+        b = got_lse[:, rows]
+        assert (np.isnan(b) == np.isnan(lse)).all() and (np.isneginf(b) == np.isneginf(lse)).all()
+        fine = np.isfinite(lse)
+        assert (np.abs(b[fine] - lse[fine]) <= dz + dp + 2.0 ** -22 * (np.abs(lse[fine]) + 16)).all()
+    return worst
