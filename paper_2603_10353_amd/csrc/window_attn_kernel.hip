@@ -18,7 +18,7 @@
 //  - a query may see nothing of the first tiles: its reference is -infinity until it does, and is then raised at once;
 //  - denominators are sums of the fp32 probabilities (products use them rounded to bf16, as V is), so that lse keeps fp32's precision;
 //  - a value that is infinite or NaN must not reach queries that do not see it, to which a product would carry it as 0 * NaN.  Tiles
-//    with masks are therefore looked through for such values, and where there are some, the products are taken one by one.
+//    with masks are therefore looked through for such values, and where there are some, they are counted apart.
 #include "attn_common.h"
 
 namespace shplb {
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int rel = d + (16 * mt + r);
-              if (rel > 0 || (rel <= -a.window && e + (16 * mt + r) >= 0)) sc[qg][mt][r] = -INFINITY;
+              sc[qg][mt][r] = (rel > 0) | ((rel <= -a.window) & (e + (16 * mt + r) >= 0)) ? -INFINITY : sc[qg][mt][r];
             }
             asm volatile("" : "+v"(sc[qg][mt]));
           }
@@ -298,12 +298,67 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       if (!ends && !hidden(key1)) scores(lds + (stage ^ 1) * kTileBytes, key1);
 
       // ---- O^T += V(u)^T P(u)^T
-      bool bad = false;
       if (checked) {
         __syncthreads();
-        bad = s_bad == step_no;
+        if (s_bad == step_no) {
+          // Values that are not finite are counted for each query among the keys that it sees, those that are +infinity or NaN and those
+          // that are -infinity or NaN, and are zeros for the products.
+          if (mine) {
+            u32x4 seen[QG][2];
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) {
+              int d = key0 + 4 * hi - q_pos[qg], e = key0 + 4 * hi - a.n_sink;
+              asm volatile("" : "+v"(d), "+v"(e));
+#pragma unroll
+              for (int x = 0; x < 2 * MT; ++x) {
+                const auto one = [&](int key) { return (d + key <= 0) & ((d + key > -a.window) | (e + key < 0)) ? 0x3f80u : 0u; };
+                const int key = 16 * (x >> 1) + 2 * (x & 1);
+                seen[qg][x >> 2][x & 3] = one(key) | one(key + 1) << 16;
+              }
+            }
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+              f32x4 up[QG], down[QG];
+#pragma unroll
+              for (int qg = 0; qg < QG; ++qg) up[qg] = down[qg] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+              for (int gq = 0; gq < 2; ++gq) {
+                const u32x4 w = __builtin_bit_cast(u32x4, read_v(vt, 8 * gq + dt));
+                u32x4 pos, neg;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t lo = w[e] & 0xffffu, hi16 = w[e] >> 16;
+                  const bool lo_bad = (lo & 0x7f80u) == 0x7f80u, hi_bad = (hi16 & 0x7f80u) == 0x7f80u;
+                  pos[e] = (lo_bad & (lo != 0xff80u) ? 0x3f80u : 0u) | (hi_bad & (hi16 != 0xff80u) ? 0x3f800000u : 0u);
+                  neg[e] = (lo_bad & (lo != 0x7f80u) ? 0x3f80u : 0u) | (hi_bad & (hi16 != 0x7f80u) ? 0x3f800000u : 0u);
+                }
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg) {
+                  up[qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pos), __builtin_bit_cast(bf16x8, seen[qg][gq]), up[qg], 0, 0, 0);
+                  down[qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, neg), __builtin_bit_cast(bf16x8, seen[qg][gq]), down[qg], 0, 0, 0);
+                }
+              }
+#pragma unroll
+              for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  const float x = up[qg][r] > 0.0f ? INFINITY : 0.0f;
+                  acc[qg][dt][r] += down[qg][r] > 0.0f ? x - INFINITY : x;
+                }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+          __syncthreads();
+#pragma unroll
+          for (int x = 0; x < kTileBytes / (4 * kThreads); ++x) {
+            uint32_t* const at = reinterpret_cast<uint32_t*>(lds + (2 + stage) * kTileBytes) + x * kThreads + threadIdx.x;
+            const uint32_t w = *at, lo = (w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu, up = (w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u;
+            *at = lo | up;
+          }
+          __syncthreads();
+        }
       }
-      if (mine && !bad) {
+      if (mine) {
         bf16x8 vf[kPV];
 #pragma unroll
         for (int gi = 0; gi < kLook; ++gi) vf[gi] = read_v(vt, gi);
@@ -317,34 +372,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             acc[qg][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[gi], __builtin_bit_cast(bf16x8, w), acc[qg][dt], 0, 0, 0);
           }
           __builtin_amdgcn_sched_barrier(0);
-        }
-      } else if (mine) {
-        // one by one, of visible keys only: the probabilities of key 16 mt + 4 x + 2 c + y are with the lanes hi = x
-#pragma unroll 1
-        for (int kk = 0; kk < kKeys; ++kk) {
-          float p[QG];
-          bool seen[QG];
-#pragma unroll
-          for (int qg = 0; qg < QG; ++qg) {
-            uint32_t w = pk[qg][0][0];
-#pragma unroll
-            for (int x = 1; x < 2 * MT; ++x) w = (kk >> 4) * 2 + (kk >> 1 & 1) == x ? pk[qg][x >> 1][x & 1] : w;
-            w = kk & 1 ? w & 0xffff0000u : w << 16;
-            p[qg] = __uint_as_float(__shfl(int(w), n + 16 * (kk >> 2 & 3)));
-            const int rel = key0 + kk - q_pos[qg];
-            seen[qg] = rel <= 0 && (rel > -a.window || key0 + kk < a.n_sink);
-          }
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(vt + kk * kRowBytes + (((2 * dt + (hi >> 1)) ^ swz(kk & 15)) << 4) + 8 * (hi & 1));
-#pragma unroll
-            for (int qg = 0; qg < QG; ++qg)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float x = __uint_as_float(r & 1 ? w[r >> 1] & 0xffff0000u : w[r >> 1] << 16);
-                acc[qg][dt][r] += seen[qg] ? p[qg] * x : 0.0f;
-              }
-          }
         }
       }
       stage ^= 1;
