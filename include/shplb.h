@@ -18,6 +18,8 @@
  *   shplb_cache_append          the prompt's and later tokens' keys and values into an 8-bit cache
  *   shplb_cache_load            tokens of the cache back in 16 bits
  *   shplb_cache_attn            attention of the next tokens over the cache, and the weight every cached token gets
+ *   shplb_cache_attn_window     the same with a sliding window and first tokens that stay visible
+ *   shplb_cache_attn_shared     the same for sequences that share prefixes, each of which is read once for all of them
  *   shplb_cache_evict           a smaller cache of the tokens with the most accumulated weight, budgets per head
  *
  * Conventions
@@ -406,6 +408,43 @@ SHPLB_API int32_t shplb_cache_attn_workspace_bytes(const shplb_cache* cache, con
                                          int64_t* bytes_out /*host*/);
 SHPLB_API int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const void* q, void* out,
                          float* lse_out, const float* weight_in, float* weight_out, void* workspace, void* stream);
+
+/* Attention of the step's queries over the cache with a sliding window and first tokens that stay visible: a
+ * query that sees the head's first c tokens in shplb_cache_attn sees of them here the last `window` and the
+ * first n_sink (what shplb_window_attn_prefill does in a prompt).  No more of the cache is read than that: table entries of pages
+ * without a token that some query of the step sees are not used, whatever they are, so that a program may give such pages
+ * back, or use a few of them in turn.
+ *   - What the call costs follows from the window, not from the context or the table's room.
+ *   - Otherwise as shplb_cache_attn: numerics, errors, arguments, the queries that see no token.  No weights: those of
+ *     shplb_cache_attn are of all tokens.
+ *   workspace: device, shplb_cache_attn_window_workspace_bytes() for any window, 256-byte aligned; needs no
+ *     clearing; must not be shared with a call in flight on another stream.
+ * Errors: also SHPLB_E_BUDGET (window < 1 or n_sink < 0). */
+SHPLB_API int32_t shplb_cache_attn_window_workspace_bytes(const shplb_cache* cache, const shplb_step* step, int32_t n_sink,
+                                                int32_t window, int64_t* bytes_out /*host*/);
+SHPLB_API int32_t shplb_cache_attn_window(const shplb_cache* cache, const shplb_step* step, int32_t n_sink, int32_t window,
+                                const void* q, void* out, float* lse_out, void* workspace, void* stream);
+
+/* Attention of the step's queries of sequences that share prefixes (a system prompt, samples of one prompt):
+ * sequences cu_prefix[g] .. cu_prefix[g+1]-1 of `cache` come behind sequence g of `prefix`.  A query sees all
+ * tokens of its prefix (of its KV head there) and, of its own sequence, what it sees in shplb_cache_attn; one of a sequence
+ * that is in no such run has no prefix.  A prefix is read once for every 32 rows that it has, not once for every
+ * sequence as with a table in which its pages stand.
+ *   prefix: a cache of one sequence for each prefix, with as many KV heads; its pages may be of another pool,
+ *     format and block, and its heads of different lengths.
+ *   cu_prefix: device int32 [prefix->n_seq+1], not decreasing; offsets outside 0 .. cache->n_seq are taken as those.
+ *   - The rows of a prefix are those between the cu_tokens of its first sequence and of the one behind its last.
+ *   - A damaged length or page of a prefix makes NaN of what all its rows get, as one of a sequence does for its own.
+ *   - Otherwise as shplb_cache_attn: numerics, errors, arguments, queries that see no token (now: neither of their prefix nor of their
+ *     own).  Softmax is over prefix and own tokens together, and so is lse_out.  No weights.
+ *   workspace: device, shplb_cache_attn_shared_workspace_bytes(), 256-byte aligned; needs no clearing;
+ *     must not be shared with a call in flight on another stream.
+ * Errors: also SHPLB_E_SHAPE (other numbers of KV heads); SHPLB_E_UNSUPPORTED for more than 2^24 rows of a KV head in all, or the limits on tiles
+ * and units of shplb_cache_attn, for prefixes with all rows of the step together. */
+SHPLB_API int32_t shplb_cache_attn_shared_workspace_bytes(const shplb_cache* prefix, const shplb_cache* cache,
+                                                const shplb_step* step, int64_t* bytes_out /*host*/);
+SHPLB_API int32_t shplb_cache_attn_shared(const shplb_cache* prefix, const int32_t* cu_prefix, const shplb_cache* cache,
+                                const shplb_step* step, const void* q, void* out, float* lse_out, void* workspace, void* stream);
 
 /* Evicts every head to its budget: of its tokens stay the first n_sink, the last
  * n_recent and, of the others, those of the largest weight (equal weights: the lower

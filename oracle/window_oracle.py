@@ -8,6 +8,8 @@ import math
 
 import numpy as np
 
+from oracle.cache_oracle import decode
+
 D = 128
 
 
@@ -61,20 +63,15 @@ def window_attention(q, k, v, cu, n_sink, window, kv_of, scale=None):
 
 def _values_at(c, s, h, at):
     """Keys and values of a head of a cache at these positions; NaN in pages that are not in the pool."""
+    at = np.asarray(at, np.int64)
+    page = c.table[s, h, at // c.block]
+    there = (page >= 0) & (page < c.n_pages)
+    page = np.where(there, page, 0)
     got = []
     for pages, scales in ((c.k_pages, c.k_scale), (c.v_pages, c.v_scale)):
-        x = np.full((len(at), D), np.nan)
-        for i in range(len(at)):
-            page = int(c.table[s, h, at[i] // c.block])
-            if 0 <= page < c.n_pages:
-                x[i] = _decode(pages[page, at[i] % c.block], c.fmt) * scales[page]
-        got.append(x)
+        x = decode(pages[page, at % c.block], c.fmt) * scales[page][:, None]
+        got.append(np.where(there[:, None], x, np.nan))
     return got
-
-
-def _decode(codes, fmt):
-    from oracle.cache_oracle import decode
-    return decode(codes, fmt)
 
 
 def _rows(q, cu, kv_of, h):

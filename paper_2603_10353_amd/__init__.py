@@ -20,6 +20,10 @@ from .binding import (  # noqa: F401
     shplb_block_scores,
     shplb_cache_append,
     shplb_cache_attn,
+    shplb_cache_attn_shared,
+    shplb_cache_attn_shared_workspace_bytes,
+    shplb_cache_attn_window,
+    shplb_cache_attn_window_workspace_bytes,
     shplb_cache_attn_workspace_bytes,
     shplb_cache_evict,
     shplb_cache_evict_workspace_bytes,

@@ -18,6 +18,7 @@ EXPORTS = [
     "shplb_balance_heads", "shplb_shift_budgets", "shplb_block_mass",
     "shplb_recovery_curves", "shplb_token_recovery", "shplb_token_recovery_heads", "shplb_probe_mfma_rate",
     "shplb_cache_append", "shplb_cache_load", "shplb_cache_attn_workspace_bytes", "shplb_cache_attn",
+    "shplb_cache_attn_window_workspace_bytes", "shplb_cache_attn_window", "shplb_cache_attn_shared_workspace_bytes", "shplb_cache_attn_shared",
     "shplb_cache_evict_workspace_bytes", "shplb_cache_evict",
     "shplb_strerror",
 ]
@@ -141,6 +142,10 @@ def load_library():
     lib.shplb_cache_load.argtypes = [cc, cs, vp, vp, vp]
     lib.shplb_cache_attn_workspace_bytes.argtypes = [cc, cs, C.POINTER(i64)]
     lib.shplb_cache_attn.argtypes = [cc, cs, vp, vp, vp, vp, vp, vp, vp]
+    lib.shplb_cache_attn_window_workspace_bytes.argtypes = [cc, cs, i32, i32, C.POINTER(i64)]
+    lib.shplb_cache_attn_window.argtypes = [cc, cs, i32, i32, vp, vp, vp, vp, vp]
+    lib.shplb_cache_attn_shared_workspace_bytes.argtypes = [cc, cc, cs, C.POINTER(i64)]
+    lib.shplb_cache_attn_shared.argtypes = [cc, vp, cc, cs, vp, vp, vp, vp, vp]
     lib.shplb_cache_evict_workspace_bytes.argtypes = [cc, C.POINTER(i64)]
     lib.shplb_cache_evict.argtypes = [cc, vp, vp, i32, i32, cc, vp, vp, vp, vp]
     for name in EXPORTS[:-1]:
@@ -430,6 +435,31 @@ def shplb_cache_attn(cache: Cache, step: Step, q, out, lse_out=None, weight_in=N
                      stream=None) -> None:
     _check(load_library().shplb_cache_attn(cache.ref(), step.ref(), _dev(q), _dev(out), _dev(lse_out), _dev(weight_in),
                                            _dev(weight_out), _dev(workspace), _stream(stream)), "shplb_cache_attn")
+
+
+def shplb_cache_attn_window_workspace_bytes(cache: Cache, step: Step, n_sink: int, window: int) -> int:
+    out = C.c_int64()
+    _check(load_library().shplb_cache_attn_window_workspace_bytes(cache.ref(), step.ref(), int(n_sink), int(window), C.byref(out)),
+           "shplb_cache_attn_window_workspace_bytes")
+    return out.value
+
+
+def shplb_cache_attn_window(cache: Cache, step: Step, n_sink: int, window: int, q, out, lse_out=None, workspace=None, stream=None) -> None:
+    _check(load_library().shplb_cache_attn_window(cache.ref(), step.ref(), int(n_sink), int(window), _dev(q), _dev(out), _dev(lse_out),
+                                                  _dev(workspace), _stream(stream)), "shplb_cache_attn_window")
+
+
+def shplb_cache_attn_shared_workspace_bytes(prefix: Cache, cache: Cache, step: Step) -> int:
+    out = C.c_int64()
+    _check(load_library().shplb_cache_attn_shared_workspace_bytes(prefix.ref(), cache.ref(), step.ref(), C.byref(out)),
+           "shplb_cache_attn_shared_workspace_bytes")
+    return out.value
+
+
+def shplb_cache_attn_shared(prefix: Cache, cu_prefix, cache: Cache, step: Step, q, out, lse_out=None, workspace=None, stream=None) -> None:
+    """cu_prefix: device int32 [prefix.n_seq + 1]."""
+    _check(load_library().shplb_cache_attn_shared(prefix.ref(), _dev(cu_prefix), cache.ref(), step.ref(), _dev(q), _dev(out), _dev(lse_out),
+                                                  _dev(workspace), _stream(stream)), "shplb_cache_attn_shared")
 
 
 def shplb_cache_evict_workspace_bytes(cache: Cache) -> int:

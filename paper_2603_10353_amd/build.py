@@ -13,7 +13,7 @@ BUILD = os.path.join(PKG_DIR, "_build")
 LIB = os.path.join(PKG_DIR, "libshplb.so")
 SOURCES = ["api.hip", "score_kernels.hip", "select_kernel.hip", "sched_kernels.hip",
            "attn_pipe_kernel.hip", "profile_kernel.hip", "probe_kernels.hip", "cache_api.hip", "cache_pages_kernels.hip",
-           "cache_attn_kernel.hip", "window_attn_kernel.hip"]
+           "cache_attn_kernel.hip", "cache_view_kernels.hip", "window_attn_kernel.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HONOR_NANS = ("cache_", "window_")            # sources whose kernels compute with NaN where the inputs have it
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-fno-honor-nans",

@@ -86,6 +86,78 @@ AttnLayout attn_layout(const shplb_cache* c, const shplb_step* t, int64_t most_r
   return w;
 }
 
+// Tensors and workspace of an attention call that has rows.
+struct AttnPlace {
+  const void* q;
+  void* out;
+  float* lse;
+  void* workspace;
+};
+int32_t place_attn(const AttnPlace& at, const shplb_step* step, const AttnLayout& w, CacheAttnArgs* a) {
+  if (!at.q || !at.out || !at.workspace) return SHPLB_E_NULL;
+  if (at.q == at.out || misaligned(at.q, 16) || misaligned(at.out, 16) || misaligned(at.workspace, 256) || misaligned(at.lse, 4)) return SHPLB_E_SHAPE;
+  char* ws = static_cast<char*>(at.workspace);
+  a->tiles = int32_t(w.tiles);
+  a->n_q_heads = step->n_q_heads;
+  a->scale_log2 = (step->softmax_scale > 0.0f ? step->softmax_scale : 1.0f / std::sqrt(float(kHeadDim))) * 1.4426950408889634f;
+  a->q = static_cast<const uint16_t*>(at.q);
+  a->out = static_cast<uint16_t*>(at.out);
+  a->lse = at.lse;
+  a->part_o = reinterpret_cast<float*>(ws + w.part_o);
+  a->part_ml = reinterpret_cast<float*>(ws + w.part_ml);
+  a->begun = reinterpret_cast<int32_t*>(ws + w.begun);
+  a->stats = reinterpret_cast<float*>(ws + w.stats);
+  return SHPLB_OK;
+}
+
+// What windows add to the arguments: sizes that no position reaches are as good as 2^30.
+int32_t check_window(const shplb_cache* c, int32_t max_tokens, int32_t n_sink, int32_t window, int64_t most_rows, CacheView* v) {
+  if (n_sink < 0 || window < 1) return SHPLB_E_BUDGET;
+  constexpr int32_t kMost = 1 << 30;
+  *v = CacheView{};
+  v->window = window < kMost ? window : kMost;
+  v->n_sink = n_sink < kMost ? n_sink : kMost;
+  // a tile has the rows of cache_attn_rows() tokens at most, and sees window + tokens - 1 positions beside the first ones
+  const int64_t tokens = max_tokens < cache_attn_rows(most_rows) ? max_tokens : cache_attn_rows(most_rows), most = int64_t(v->window) + (tokens > 0 ? tokens : 1) - 1;
+  const int64_t units = (int64_t(v->n_sink) + 63) / 64 + (most + 62) / 64 + 1, all = int64_t(c->max_pages) * c->block / 64;
+  v->most_units = int32_t(units < all ? units : all);
+  return SHPLB_OK;
+}
+
+// A call on sequences with prefixes: its arguments, without the tensors.
+struct SharedArgs {
+  CacheAttnArgs own, pre;
+  int64_t most_rows;
+  int32_t rows_pre;                // rows of an item of the prefixes' list
+  AttnLayout w;                    // of the own tokens' part; the prefixes' one lies behind it
+  int64_t part_o, part_ml, begun, whole_o[2], whole_ml[2], total;
+};
+int32_t check_shared(const shplb_cache* prefix, const shplb_cache* cache, const shplb_step* step, SharedArgs* x) {
+  if (int32_t st = check_cache(prefix, &x->pre.c)) return st;
+  if (int32_t st = check_cache(cache, &x->own.c)) return st;
+  if (prefix->n_kv_heads != cache->n_kv_heads) return SHPLB_E_SHAPE;
+  if (int32_t st = check_queries(cache, step, &x->own.groups, &x->most_rows)) return st;
+  if (int32_t st = check_step(cache, step, step->n_q_heads, step->q_stride_t, step->q_stride_h, &x->own.t)) return st;
+  // the rows of a KV head, all of which may have the same prefix
+  const int64_t most_heads = step->max_tokens > 0 ? x->most_rows / step->max_tokens : 1, rows = int64_t(step->n_tokens) * most_heads;
+  if (rows > 1 << 24) return SHPLB_E_UNSUPPORTED;
+  x->rows_pre = prefix_attn_rows(rows / prefix->n_seq);
+  const int64_t items = (rows / x->rows_pre + prefix->n_seq) * prefix->n_kv_heads;
+  if (items >= int64_t(1) << 24 || items * (int64_t(prefix->max_pages) * prefix->block / 64 + kCacheMostStart) >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
+  x->w = attn_layout(cache, step, x->most_rows);
+  int64_t off = x->w.total;
+  x->part_o = off; off += align256(prefix_slot_rows(x->rows_pre) * kHeadDim * 4);
+  x->part_ml = off; off += align256(prefix_slot_rows(x->rows_pre) * 2 * 4);
+  const int64_t all = int64_t(step->n_tokens) * step->n_q_heads;
+  x->begun = off; off += align256(all * 8);
+  for (int y = 0; y < 2; ++y) {
+    x->whole_o[y] = off; off += align256(all * kHeadDim * 4);
+    x->whole_ml[y] = off; off += align256(all * 8);
+  }
+  x->total = off;
+  return SHPLB_OK;
+}
+
 }  // namespace
 }  // namespace shplb
 
@@ -159,6 +231,63 @@ int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const
   a.begun = reinterpret_cast<int32_t*>(ws + w.begun);
   a.stats = reinterpret_cast<float*>(ws + w.stats);
   return launch_cache_attn(a, int32_t(most_rows), n_wg / 2, static_cast<hipStream_t>(stream));
+}
+
+int32_t shplb_cache_attn_window_workspace_bytes(const shplb_cache* cache, const shplb_step* step, int32_t n_sink, int32_t window, int64_t* bytes_out) {
+  if (n_sink < 0 || window < 1) return SHPLB_E_BUDGET;
+  return shplb_cache_attn_workspace_bytes(cache, step, bytes_out);
+}
+
+int32_t shplb_cache_attn_window(const shplb_cache* cache, const shplb_step* step, int32_t n_sink, int32_t window, const void* q, void* out,
+                                float* lse_out, void* workspace, void* stream) {
+  CacheAttnArgs a{};
+  int64_t most_rows;
+  if (int32_t st = check_cache(cache, &a.c)) return st;
+  if (int32_t st = check_queries(cache, step, &a.groups, &most_rows)) return st;
+  if (int32_t st = check_step(cache, step, step->n_q_heads, step->q_stride_t, step->q_stride_h, &a.t)) return st;
+  if (int32_t st = check_window(cache, step->max_tokens, n_sink, window, most_rows, &a.view)) return st;
+  if (a.t.n_tokens == 0 || a.t.max_tokens == 0) return SHPLB_OK;
+  AttnPlace at{q, out, lse_out, workspace};
+  if (int32_t st = place_attn(at, step, attn_layout(cache, step, most_rows), &a)) return st;
+  const int32_t n_wg = persistent_workgroups();
+  if (n_wg < 0) return n_wg;
+  return launch_cache_attn_window(a, int32_t(most_rows), n_wg / 2, static_cast<hipStream_t>(stream));
+}
+
+int32_t shplb_cache_attn_shared_workspace_bytes(const shplb_cache* prefix, const shplb_cache* cache, const shplb_step* step, int64_t* bytes_out) {
+  if (!bytes_out) return SHPLB_E_NULL;
+  SharedArgs x{};
+  if (int32_t st = check_shared(prefix, cache, step, &x)) return st;
+  *bytes_out = x.total;
+  return SHPLB_OK;
+}
+
+int32_t shplb_cache_attn_shared(const shplb_cache* prefix, const int32_t* cu_prefix, const shplb_cache* cache, const shplb_step* step, const void* q,
+                                void* out, float* lse_out, void* workspace, void* stream) {
+  SharedArgs x{};
+  if (int32_t st = check_shared(prefix, cache, step, &x)) return st;
+  if (x.own.t.n_tokens == 0 || x.own.t.max_tokens == 0) return SHPLB_OK;
+  if (!cu_prefix) return SHPLB_E_NULL;
+  if (misaligned(cu_prefix, 4)) return SHPLB_E_SHAPE;
+  AttnPlace at{q, out, lse_out, workspace};
+  if (int32_t st = place_attn(at, step, x.w, &x.own)) return st;
+  const int32_t n_wg = persistent_workgroups();
+  if (n_wg < 0) return n_wg;
+  const CacheArgs prefixes = x.pre.c;
+  x.pre = x.own;
+  x.pre.c = prefixes;
+  x.pre.view.groups = cu_prefix;
+  x.pre.view.members = cache->n_seq;
+  char* ws = static_cast<char*>(workspace);
+  x.pre.part_o = reinterpret_cast<float*>(ws + x.part_o);
+  x.pre.part_ml = reinterpret_cast<float*>(ws + x.part_ml);
+  x.pre.begun = reinterpret_cast<int32_t*>(ws + x.begun);
+  for (int y = 0; y < 2; ++y) {
+    CacheView& v = y == 0 ? x.own.view : x.pre.view;
+    v.whole_o = reinterpret_cast<float*>(ws + x.whole_o[y]);
+    v.whole_ml = reinterpret_cast<float*>(ws + x.whole_ml[y]);
+  }
+  return launch_cache_attn_shared(x.own, x.pre, int32_t(x.most_rows), x.rows_pre, n_wg / 2, static_cast<hipStream_t>(stream));
 }
 
 int32_t shplb_cache_evict_workspace_bytes(const shplb_cache* cache, int64_t* bytes_out) {

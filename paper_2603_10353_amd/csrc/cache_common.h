@@ -38,6 +38,15 @@ struct HeadGroups {
   uint8_t head[SHPLB_MAX_MAPPED_HEADS];
 };
 
+// Which tokens rows see, where that is not all up to their own (see cache_attn.h).
+struct CacheView {
+  int32_t window, n_sink;          // at most 2^30 each
+  int32_t most_units;              // of 64 tokens, that a tile of rows sees at most, and one more
+  const int32_t* groups;           // [sequences of the cache + 1]
+  int32_t members;                 // sequences of the step
+  float *whole_o, *whole_ml;       // workspace: partial results of rows, [n_tokens][n_q_heads][128] and [2]
+};
+
 struct CacheAttnArgs {
   CacheArgs c;
   StepArgs t;                      // strides of Q and the output
@@ -54,6 +63,7 @@ struct CacheAttnArgs {
   float *part_o, *part_ml;         // partial results: [2 shares][rows][128], [2 shares][rows][2]
   int32_t* begun;                  // [sequences x KV heads][tiles][2]: the share that a tile of rows begins in, its pieces (0: it is whole)
   float* stats;                    // [n_tokens][n_q_heads][2]: reference exponent and 1 / denominator, for the weights
+  CacheView view;
 };
 
 // Shares of an attention launch at most: of up to 16 rows every wave's own, of more a workgroup's; and rows of partial results,
@@ -72,6 +82,12 @@ int32_t launch_cache_evict(const CacheArgs& src, const float* weight, const int3
 int64_t cache_evict_workspace(const CacheArgs& c);
 // Rows (query token, head of the group) of an item of the list that the work is divided from.
 int32_t cache_attn_rows(int64_t most_rows);
+int32_t launch_cache_attn_window(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
+// Rows of an item of the list that the work on prefixes is divided from, where a prefix and KV head has so many on average.
+int32_t prefix_attn_rows(int64_t rows);
+// ... and rows of partial results of such items.
+int64_t prefix_slot_rows(int32_t rows);
+int32_t launch_cache_attn_shared(const CacheAttnArgs& own, const CacheAttnArgs& pre, int32_t most_rows, int32_t rows_pre, int32_t compute_units, hipStream_t stream);
 int32_t launch_cache_attn(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
 
 // A load of what no kernel of the launch writes, at an address that is the same in all lanes: by way of the scalar cache, which leaves

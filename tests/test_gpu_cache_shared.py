@@ -1,0 +1,203 @@
+"""GPU parity of attention behind shared prefixes in the 8-bit cache, through the C ABI against the oracle."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_10353_amd as S
+from cache_harness import D, DEV, Device, bf16, filled, step_of, strided
+from oracle import cache_oracle, window_oracle as orc
+from window_harness import check
+
+pytestmark = pytest.mark.gpu
+E4M3, INT8 = cache_oracle.E4M3, cache_oracle.INT8
+FORMATS = pytest.mark.parametrize("fmt", [E4M3, INT8], ids=["e4m3", "int8"])
+HALF, LIFT = 2.0 ** -11, 2.0 ** -32
+
+
+def stream():
+    return torch.cuda.current_stream()
+
+
+def workspace(pre, dev, step):
+    return torch.empty(S.shplb_cache_attn_shared_workspace_bytes(pre.cache, dev.cache, step), dtype=torch.uint8, device=DEV).fill_(0xff)
+
+
+def cu_of(groups):
+    return torch.tensor(groups, dtype=torch.int32, device=DEV)
+
+
+def call(pre, groups, dev, step, q, ws=None):
+    out, lse = torch.full_like(q, 7.0), torch.full((q.shape[1], q.shape[0]), 7.0, device=DEV)
+    S.shplb_cache_attn_shared(pre.cache, groups if torch.is_tensor(groups) else cu_of(groups), dev.cache, step, q, out, lse,
+                              workspace(pre, dev, step) if ws is None else ws, stream())
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy(), lse.double().cpu().numpy()
+
+
+CASES = {  # lengths of prefixes, cu_prefix, own lengths, new tokens, query heads, KV heads
+    "one_sequence": ([[100]], [0, 1], [[5]], [1], 4, 1),
+    "one_key": ([[1]], [0, 2], [[1], [2]], [1, 1], 1, 1),
+    "samples": ([[300, 200]], [0, 4], [[1, 1], [40, 70], [129, 64], [65, 300]], [1] * 4, 4, 2),
+    "edges": ([[n] for n in (1, 63, 64, 65, 127, 128, 129)], list(range(8)), [[n] for n in (64, 1, 65, 63, 128, 2, 200)], [1] * 7, 2, 1),
+    "empty_prefixes": ([[0, 100], [77, 0], [0, 0]], [0, 2, 4, 5], [[3, 9]] * 6, [1] * 6, 4, 2),
+    "nothing_at_all": ([[0]], [0, 2], [[0], [3], [0]], [1, 1, 1], 2, 1),
+    "some_without": ([[90], [130]], [1, 3, 4], [[20]] * 6, [1, 2, 0, 3, 1, 2], 3, 1),
+    "runs_of_none": ([[90], [130], [64], [40]], [0, 0, 3, 3, 5], [[20]] * 5, [1] * 5, 4, 1),
+    "more_tokens_than_held": ([[70]], [0, 3], [[1], [0], [2]], [4, 3, 2], 2, 1),
+    "rows_17": ([[300]], [0, 17], [[30]] * 17, [1] * 17, 1, 1),
+    "rows_64": ([[500, 77]], [0, 16], [[30, 7]] * 16, [1] * 16, 8, 2),
+    "rows_100": ([[500, 200]], [0, 25], [[30, 65]] * 25, [1] * 25, 8, 2),
+    "rows_128": ([[700]], [0, 32], [[30]] * 32, [1] * 32, 4, 1),
+    "rows_129": ([[700], [300]], [0, 129, 131], [[3]] * 131, [1] * 131, 1, 1),
+    "rows_400_uneven": ([[700, 1, 333], [64, 900, 128]], [2, 30, 55], [[9, 20, 30]] * 57, [2] * 57, 12, 3),
+    "long": ([[6000, 2500]], [0, 70], [[80, 90]] * 70, [1] * 70, 8, 2),
+    "long_few": ([[9000, 70]], [0, 3], [[300, 5000]] * 3, [1] * 3, 4, 2),
+    "many_heads": ([[100] * 4, [30] * 4], [0, 290, 300], [[5, 70, 1, 20]] * 310, [1] * 310, 4, 4),
+    "many_prefixes": ([[70, 5]] * 300, list(range(301)), [[5, 70]] * 300, [1] * 300, 4, 2),
+    "many_prefixes_rows": ([[70]] * 40, [20 * x for x in range(41)], [[9]] * 800, [1] * 800, 1, 1),
+    "draft": ([[400]], [0, 9], [[40]] * 9, [3, 1, 4, 1, 5, 0, 2, 6, 5], 7, 1),
+    "pieces_of_prompts": ([[200]], [0, 2], [[64], [150]], [64, 100], 4, 1),
+}
+
+
+@FORMATS
+@pytest.mark.parametrize("block", [128, 64])
+@pytest.mark.parametrize("name", CASES)
+def test_sizes(name, block, fmt):
+    plens, groups, lens, new, hq, hkv = CASES[name]
+    rng = np.random.default_rng([fmt, block, len(name)])
+    prefix, c = filled(rng, plens, block, fmt), filled(rng, lens, block, fmt)
+    pre, dev = Device(prefix), Device(c)
+    new = np.array(new)
+    T = int(new.sum())
+    q, q64 = bf16(rng.standard_normal((T, hq, D)))
+    step, cu = step_of(dev, new, hq, len(set(new.tolist())) > 1)
+    out, lse = call(pre, groups, dev, step, q.to(DEV))
+    kv_of = np.arange(hq) * hkv // hq
+    want = orc.cache_shared(prefix, groups, c, q64, cu, kv_of)
+    check(want, out, lse, slice(0, T), int(np.max(plens) + np.max(lens)), HALF, LIFT)
+
+
+def test_formats_blocks_strides_mapped_heads_scale_rows_behind():
+    rng = np.random.default_rng(4)
+    kv_of = [2, 0, 0, 2, 0]                    # one KV head without query heads
+    prefix = filled(rng, [[300, 50, 77]], 64, INT8)
+    c = filled(rng, [[100, 50, 300], [80, 1, 129], [9, 9, 9]], 128, E4M3)
+    pre, dev = Device(prefix), Device(c)
+    q, q64 = bf16(rng.standard_normal((8, 5, D)))
+    qd, wide = strided(q, 4)
+    step, cu = step_of(dev, [2, 3, 1], 5, True, behind=2, q_stride_t=wide.shape[1] * D, softmax_scale=0.2, kv_head_of=kv_of)
+    out = torch.full_like(wide, 5.0)
+    S.shplb_cache_attn_shared(pre.cache, cu_of([0, 2]), dev.cache, step, qd, out[:, 2:7], None, workspace(pre, dev, step), stream())
+    want = orc.cache_shared(prefix, [0, 2], c, q64, cu, kv_of, 0.2)
+    check(want, out[:, 2:7].double().cpu().numpy(), None, slice(0, 6), 600, HALF, LIFT)
+    assert (out[6:] == 5).all() and (out[:, :2] == 5).all() and (out[:, 7:] == 5).all()
+
+
+@FORMATS
+@pytest.mark.parametrize("each", [1, 40])
+def test_damage_reaches_those_who_see_it(fmt, each):
+    """Lengths that cannot be, pages that are not there or have a scale of NaN, in prefixes and in own tokens."""
+    rng = np.random.default_rng(5)
+    plens = [[300], [-1], [1000], [300], [300], [300]]
+    prefix = filled(rng, np.clip(plens, 0, 384), 64, fmt, max_pages=6)
+    prefix.lens[:] = plens
+    prefix.table[3, 0, 2] = -1
+    prefix.k_scale[prefix.table[4, 0, 0]] = np.nan
+    prefix.v_scale[prefix.table[5, 0, 4]] = np.nan
+    n = 6 * each + 1
+    c = filled(rng, [[70]] * n, 64, fmt)
+    c.lens[0, 0] = -5
+    c.table[each - 1, 0, 1] = 10 ** 6
+    pre, dev = Device(prefix), Device(c)
+    q, q64 = bf16(rng.standard_normal((n, 2, D)))
+    step, cu = step_of(dev, [1] * n, 2, False)
+    groups = [each * x for x in range(7)]
+    want = orc.cache_shared(prefix, groups, c, q64, cu, [0, 0])
+    assert np.isfinite(want.out[-1]).all() and np.isnan(want.out[each:6 * each]).all()
+    check(want, *call(pre, groups, dev, step, q.to(DEV)), slice(0, n), 400, HALF, LIFT)
+
+
+def test_offsets_out_of_range():
+    """cu_prefix outside the sequences is taken as their ends; cu_tokens that go backwards read and write nothing outside."""
+    rng = np.random.default_rng(6)
+    prefix, c = filled(rng, [[90], [64]], 64, E4M3), filled(rng, [[20]] * 4, 64, E4M3)
+    pre, dev = Device(prefix), Device(c)
+    q, q64 = bf16(rng.standard_normal((4, 2, D)))
+    step, cu = step_of(dev, [1] * 4, 2, False)
+    got = call(pre, [-5, 3, 99], dev, step, q.to(DEV))
+    check(orc.cache_shared(prefix, [0, 3, 4], c, q64, cu, [0, 0]), *got, slice(0, 4), 110, HALF, LIFT)
+    step = S.Step(4, 2, 1, 4, 2, torch.tensor([0, 3, 1, -7, 99], dtype=torch.int32, device=DEV))
+    call(pre, [0, 2, 4], dev, step, q.to(DEV))
+    call(pre, [3, 1, 2], dev, step, q.to(DEV))
+
+
+def test_large_scales_and_queries():
+    rng = np.random.default_rng(7)
+    for size, qsize, other in ((2.0 ** 40, 2.0 ** -40, 2.0 ** 40), (2.0 ** -60, 2.0 ** 60, 2.0 ** -60), (1.0, 300.0, 1.0), (2.0 ** -100, 1.0, 1.0),
+                               (2.0 ** 12, 1e-3, 2.0 ** -12)):
+        for n in (3, 50):
+            prefix, c = filled(rng, [[500, 1000]], 128, E4M3, size=size), filled(rng, [[100, 30]] * n, 128, E4M3, size=other)
+            pre, dev = Device(prefix), Device(c)
+            q, q64 = bf16(rng.standard_normal((n, 8, D)) * qsize)
+            step, cu = step_of(dev, [1] * n, 8, False)
+            want = orc.cache_shared(prefix, [0, n], c, q64, cu, np.arange(8) // 4)
+            check(want, *call(pre, [0, n], dev, step, q.to(DEV)), slice(0, n), 1100, HALF, LIFT)
+
+
+def test_as_one_sequence():
+    """A prefix and one sequence behind it give what the cache gives of both in one table."""
+    rng = np.random.default_rng(8)
+    c = filled(rng, [[900, 900]], 64, E4M3)
+    both = Device(c)
+    prefix = cache_oracle.CacheState(c.k_pages, c.v_pages, c.k_scale, c.v_scale, c.table[:, :, :10].copy(), np.full((1, 2), 640, np.int32), E4M3)
+    own = cache_oracle.CacheState(c.k_pages, c.v_pages, c.k_scale, c.v_scale, c.table[:, :, 10:].copy(), np.full((1, 2), 260, np.int32), E4M3)
+    pre, dev = Device(prefix), Device(own)
+    q, q64 = bf16(rng.standard_normal((3, 8, D)))
+    step, cu = step_of(dev, [3], 8, False)
+    got = call(pre, [0, 1], dev, step, q.to(DEV))
+    want = orc.cache_shared(prefix, [0, 1], own, q64, cu, np.arange(8) // 4)
+    check(want, *got, slice(0, 3), 900, HALF, LIFT)
+    out, lse = torch.zeros_like(q, device=DEV), torch.zeros((8, 3), device=DEV)
+    ws = torch.empty(S.shplb_cache_attn_workspace_bytes(both.cache, step), dtype=torch.uint8, device=DEV)
+    S.shplb_cache_attn(both.cache, step, q.to(DEV), out, lse, None, None, ws, stream())
+    check(want, out.double().cpu().numpy(), lse.double().cpu().numpy(), slice(0, 3), 900, HALF, LIFT)
+
+
+def test_samples_of_a_prompt_token_after_token():
+    """As it is used: the prompt is appended once, samples go on from it, append and attention in one captured step."""
+    rng = np.random.default_rng(9)
+    P, n, hq, hkv, steps = 333, 20, 8, 2, 5
+    (pk, pk64), (pv, pv64) = (bf16(rng.standard_normal((P, hkv, D))) for _ in "kv")
+    z = lambda m: np.zeros((m, 128, D), np.uint8)
+    prefix = cache_oracle.CacheState(z(6), z(6), np.ones(6), np.ones(6), np.arange(6, dtype=np.int32).reshape(1, 2, 3), np.full((1, 2), P, np.int32), E4M3)
+    c = cache_oracle.CacheState(z(40), z(40), np.ones(40), np.ones(40), np.arange(40, dtype=np.int32).reshape(20, 2, 1), np.zeros((20, 2), np.int32), E4M3)
+    pre, dev = Device(prefix), Device(c)
+    S.shplb_cache_append(pre.cache, S.Step(1, hq, hkv, max_tokens=P), pk.to(DEV), pv.to(DEV), stream())
+    cache_oracle.append(prefix, pk64, pv64, [0, P])
+    pre.check_same(prefix)
+    step, cu = step_of(dev, [1] * n, hq, False)
+    ws, groups = workspace(pre, dev, step), cu_of([0, n])
+    q, k, v = (torch.zeros((n, h, D), dtype=torch.bfloat16, device=DEV) for h in (hq, hkv, hkv))
+    out, lse = torch.zeros_like(q), torch.zeros((hq, n), device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        S.shplb_cache_append(dev.cache, step, k, v, stream())
+        S.shplb_cache_attn_shared(pre.cache, groups, dev.cache, step, q, out, lse, ws, stream())
+    for t in range(steps):
+        (a, a64), (b, b64), (x, x64) = (bf16(rng.standard_normal((n, h, D))) for h in (hkv, hkv, hq))
+        k.copy_(a); v.copy_(b); q.copy_(x)
+        dev.lens += 1
+        c.lens += 1
+        graph.replay()
+        torch.cuda.synchronize()
+        cache_oracle.append(c, a64, b64, cu)
+        got = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        check(orc.cache_shared(prefix, [0, n], c, x64, cu, np.arange(hq) // 4), *got, slice(0, n), P + steps, HALF, LIFT)
+        other = torch.cuda.Stream()
+        other.wait_stream(stream())
+        again, again_lse = torch.zeros_like(q), torch.zeros_like(lse)
+        S.shplb_cache_attn_shared(pre.cache, groups, dev.cache, step, q, again, again_lse, workspace(pre, dev, step), other)
+        torch.cuda.synchronize()
+        assert (again == out).all() and (again_lse == lse).all()
+    dev.check_same(c)
