@@ -428,10 +428,10 @@ SHPLB_API int32_t shplb_cache_attn_window(const shplb_cache* cache, const shplb_
 /* Attention of the step's queries of sequences that share prefixes (a system prompt, samples of one prompt):
  * sequences cu_prefix[g] .. cu_prefix[g+1]-1 of `cache` come behind sequence g of `prefix`.  A query sees all
  * tokens of its prefix (of its KV head there) and, of its own sequence, what it sees in shplb_cache_attn; one of a sequence
- * that is in no such run has no prefix.  A prefix is read once for every 32 rows that it has, not once for every
+ * that is in no such run has no prefix.  A prefix is read once for every 128 rows that it has, not once for every
  * sequence as with a table in which its pages stand.
- *   prefix: a cache of one sequence for each prefix, with as many KV heads; its pages may be of another pool,
- *     format and block, and its heads of different lengths.
+ *   prefix: a cache of one sequence for each prefix, with as many KV heads and of the same format; its pages may
+ *     be of another pool and block, and its heads of different lengths.
  *   cu_prefix: device int32 [prefix->n_seq+1], not decreasing; offsets outside 0 .. cache->n_seq are taken as those.
  *   - The rows of a prefix are those between the cu_tokens of its first sequence and of the one behind its last.
  *   - A damaged length or page of a prefix makes NaN of what all its rows get, as one of a sequence does for its own.
@@ -439,7 +439,7 @@ SHPLB_API int32_t shplb_cache_attn_window(const shplb_cache* cache, const shplb_
  *     own).  Softmax is over prefix and own tokens together, and so is lse_out.  No weights.
  *   workspace: device, shplb_cache_attn_shared_workspace_bytes(), 256-byte aligned; needs no clearing;
  *     must not be shared with a call in flight on another stream.
- * Errors: also SHPLB_E_SHAPE (other numbers of KV heads); SHPLB_E_UNSUPPORTED for more than 2^24 rows of a KV head in all, or the limits on tiles
+ * Errors: also SHPLB_E_SHAPE (another number of KV heads or format); SHPLB_E_UNSUPPORTED for more than 2^24 rows of a KV head in all, or the limits on tiles
  * and units of shplb_cache_attn, for prefixes with all rows of the step together. */
 SHPLB_API int32_t shplb_cache_attn_shared_workspace_bytes(const shplb_cache* prefix, const shplb_cache* cache,
                                                 const shplb_step* step, int64_t* bytes_out /*host*/);

@@ -135,7 +135,7 @@ struct SharedArgs {
 int32_t check_shared(const shplb_cache* prefix, const shplb_cache* cache, const shplb_step* step, SharedArgs* x) {
   if (int32_t st = check_cache(prefix, &x->pre.c)) return st;
   if (int32_t st = check_cache(cache, &x->own.c)) return st;
-  if (prefix->n_kv_heads != cache->n_kv_heads) return SHPLB_E_SHAPE;
+  if (prefix->n_kv_heads != cache->n_kv_heads || prefix->format != cache->format) return SHPLB_E_SHAPE;
   if (int32_t st = check_queries(cache, step, &x->own.groups, &x->most_rows)) return st;
   if (int32_t st = check_step(cache, step, step->n_q_heads, step->q_stride_t, step->q_stride_h, &x->own.t)) return st;
   // the rows of a KV head, all of which may have the same prefix

@@ -650,6 +650,13 @@ __device__ __forceinline__ int64_t begun_row(const CacheAttnArgs& a, int row0, i
   return (int64_t(row0) + j) * a.n_q_heads + group_head(a.groups, h, row - j * group);
 }
 
+// Where a group's rows first_row .. first_row + rows - 1, a tile of it, have their results: for each of them the share that the tile begins in,
+// its pieces (0: it is whole) times 256, and the row's place in the tile.
+__device__ __forceinline__ void note_rows(const CacheAttnArgs& a, int row0, int n, int h, int group, int first_row, int rows, int me, int worker, int pieces) {
+  if (me < rows && first_row + me < n * group)
+    *reinterpret_cast<int2*>(a.begun + 2 * begun_row(a, row0, first_row + me, h, group)) = int2{worker, pieces << 8 | me};
+}
+
 // 1 / denominator of a row: 0 of one that sees nothing, so that its output is; of a head whose length cannot be, NaN.  A row that
 // sees tokens and whose products are all -inf (a query that is not finite) has 1 / 0, which makes NaN of its output, its weights
 // and its logarithm.
@@ -660,32 +667,39 @@ __device__ __forceinline__ float row_lse(float top, float sum, float inv) {
   return (top + __builtin_amdgcn_logf(sum) - kLift) * 0.6931471805599453f + 0.0f * inv;
 }
 
+// What a workgroup of it has in LDS.
+template <int NT, int WAVES>
+struct AttnLds {
+  RowsLds<NT> rows[WAVES == 1 ? kWaves : 1];
+  float o[WAVES][16][kLdsRow];
+  float m[WAVES][16 * NT], l[WAVES][16 * NT];
+  int i[kWaves + kThreads];
+};
 // Up to 16 rows (WAVES = 1) every wave has a share of its own.  More rows are worked on 32 at a time, by all WAVES = 4 of a
 // workgroup, which take turns at its share's units; their results meet in LDS, or there would be four times as many partial ones.
 // (For 128 rows x 8 heads x 32768 int8 tokens 41 us, VALU work for the most part: turning the codes into fp16 for every 32 rows.
 // Tiles side by side in a workgroup, to read the codes from memory once, bring nothing.)  ITEMS: no shares, a workgroup an item,
 // for short caches.  PARTS: results are partial ones in any case, for a join with others.
 template <int NT, int WAVES, bool ITEMS, int FMT, int VIEW = kAll, bool PARTS = false>
-__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a, int least) {
+__device__ __forceinline__ void attend_shares(const CacheAttnArgs& a, int least, int block, int blocks, AttnLds<NT, WAVES>& lds) {
   static_assert((VIEW != kGroups || PARTS) && !(PARTS && ITEMS), "a row of a group has tokens of its own, too");
   constexpr bool kOwn = WAVES == 1;
   constexpr int kRows = 16 * NT, kStart = start_units(WAVES);
   static_assert(kOwn || WAVES == kWaves, "one, or all of a workgroup");
-  __shared__ RowsLds<NT> lds_rows[kOwn ? kWaves : 1];
-  __shared__ float lds_o[WAVES][16][kLdsRow];
-  __shared__ float lds_m[WAVES][kRows], lds_l[WAVES][kRows];
-  __shared__ int lds_i[kWaves + kThreads];
+  auto& lds_rows = lds.rows;
+  auto& lds_o = lds.o;
+  auto &lds_m = lds.m, &lds_l = lds.l;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   int at = 0, end = 1 << 30;
   Shares<!kOwn> shares;
   // neighbouring shares in different workgroups, on different compute units
-  const int worker = kOwn ? int(blockIdx.x) + wave * int(gridDim.x) : int(blockIdx.x);
+  const int worker = kOwn ? block + wave * blocks : block;
   Item it;
   if constexpr (ITEMS) {
     const int pair = worker / uint32_t(a.tiles);
     it = {pair, scalar_load(a.c.lens + pair), worker - pair * a.tiles, 0};
   } else {
-    it = locate<false, kRows, kStart, VIEW>(a, worker, int(gridDim.x) * (kOwn ? kWaves : 1), least, kOwn ? int(gridDim.x) : 1, lds_i, at, end, shares);
+    it = locate<false, kRows, kStart, VIEW>(a, worker, blocks * (kOwn ? kWaves : 1), least, kOwn ? blocks : 1, lds.i, at, end, shares);
   }
   while (at < end) {
     // (the lane as a number of which the compiler knows nothing: what follows from it is worked out here and again at the item's end, and
@@ -821,15 +835,22 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a
       __syncthreads();
     }
     if (ITEMS) break;
-    if (u0 == 0 && (kOwn ? (tid & 63) == 0 : tid == 0)) {       // for the joining kernel: pieces of the item, if it ends in another share
-      // (a group's tiles are noted at their first rows: how many there are is not known beforehand)
-      const int64_t note = VIEW == kGroups ? begun_row(a, row0, first_row, h, group) : int64_t(pair) * a.tiles + it.tile;
-      *reinterpret_cast<int2*>(a.begun + 2 * note) = int2{worker, whole ? 0 : shares.of(at - it.unit + units - 1) - worker + 1};
+    // for the joining kernel: pieces of the item, if it ends in another share
+    if (VIEW == kGroups) {
+      if (u0 == 0) note_rows(a, row0, n, h, group, first_row, kRows, kOwn ? tid & 63 : tid, worker, whole ? 0 : shares.of(at - it.unit + units - 1) - worker + 1);
+    } else if (u0 == 0 && (kOwn ? (tid & 63) == 0 : tid == 0)) {
+      *reinterpret_cast<int2*>(a.begun + 2 * (int64_t(pair) * a.tiles + it.tile)) = int2{worker, whole ? 0 : shares.of(at - it.unit + units - 1) - worker + 1};
     }
     at += u1 - it.unit;
     it.unit = -kStart;
     if (++it.tile == tiles) it = next_pair<kStart>(a, pair);
   }
+}
+
+template <int NT, int WAVES, bool ITEMS, int FMT, int VIEW = kAll, bool PARTS = false>
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CacheAttnArgs a, int least) {
+  __shared__ AttnLds<NT, WAVES> lds;
+  attend_shares<NT, WAVES, ITEMS, FMT, VIEW, PARTS>(a, least, int(blockIdx.x), int(gridDim.x), lds);
 }
 
 // Joins the pieces of one row of an item: with M the largest m, out = sum 2^(m - M) O / sum 2^(m - M) l.  A workgroup a row (y)

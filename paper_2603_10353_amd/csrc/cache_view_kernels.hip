@@ -25,104 +25,476 @@ int32_t launch_window(const CacheAttnArgs& a, int rows, int most_rows, int compu
   return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
 }
 
-// ---- shared prefixes.  The rows of all sequences that share a prefix are rows of one item: its keys are read once for 32 of
-// them (16 where there are no more).  A second launch attends to the sequences' own tokens; both leave partial results.
+// ---- shared prefixes.  The rows of all sequences that share a prefix are rows of one item: its keys are read once for many of them.
+// One launch attends to the prefixes and to the sequences' own tokens, either divided like the cache of cache_attn_kernel.hip; all results are partial ones, which a second launch joins.
+
+// Rows of a prefix's item.  Up to 48 of them are worked on like those of a cache, 16 or 32 at a time: codes come from memory
+// into registers, and are turned to fp16 for each tile by itself.  More rows: 128 at a time, 32 of each wave, whose workgroup turns the
+// codes of 64 keys to fp16 once, in LDS, while the products of the last ones are done; the tile is that of window_attn_kernel.hip, in
+// fp16.
+constexpr int kPrefixRows = 128, kPrefixStart = 4;
+
+struct PrefixLds {
+  char k[2][kUnit * kRowBytes], v[2][kUnit * kRowBytes];        // keys and values of two units in fp16: chunk c of row r in slot c ^ swz(r)
+  int i[kWaves + kThreads];
+};
+
 template <int FMT>
-void launch_prefix(const CacheAttnArgs& a, int grid, int rows, hipStream_t stream) {
-  if (rows == 16) cache_attn_kernel<1, 1, false, FMT, kGroups, true><<<grid, kThreads, 0, stream>>>(a, 3);
-  else cache_attn_kernel<2, kWaves, false, FMT, kGroups, true><<<grid, kThreads, 0, stream>>>(a, kWaves);
+__device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least, int block, int blocks, PrefixLds& lds) {
+  constexpr int NT = 2, MT = kUnit / 16, kQK = 4 * MT, kPV = 8 * (kUnit / 32), kLook = 8;
+  // a lane has sixteen probabilities of a row and unit: with this sum none is more than fp16 holds
+  constexpr float kSumLimit = 60000.0f;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, hi = lane >> 4;
+  int at, end;
+  Shares<true> shares;
+  Item it = locate<false, kPrefixRows, kPrefixStart, kGroups>(a, block, blocks, least, 1, lds.i, at, end, shares);
+  // operands in LDS, as in window_attn_kernel.hip; a thread brings eight codes of rows tid / 16 + 16 x, one chunk each
+  const int k_rd0 = n16 * kRowBytes + ((hi ^ swz(n16)) << 4);
+  const int tr_row = 4 * hi + ((lane >> 2) & 3), tr_a = lane & 3;
+  const int v_rd0 = tr_row * kRowBytes + (((tr_a >> 1) ^ swz(tr_row)) << 4) + 8 * (tr_a & 1);
+  const int wr = (tid >> 4) * kRowBytes + (((tid & 15) ^ swz(tid >> 4)) << 4);
+  struct Codes {
+    u32x2 x[4];
+  };
+  while (at < end) {
+    const int pair = it.pair, s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads;
+    int row0, n, tiles, units;
+    view_tokens<kGroups, true>(a, s, row0, n);
+    const int len = it.len, group = group_size(a.groups, h), rows = n * group;
+    pair_units<false, kPrefixRows, kGroups>(a, rows, len, tiles, units);
+    if (tiles == 0) {
+      if (n > 0) it = next_pair<kPrefixStart>(a, pair);
+      else if (!next_sequence<kPrefixStart, kGroups>(a, s, lane, it)) break;
+      continue;
+    }
+    const int u0 = max(it.unit, 0), u1 = min(units, it.unit + (end - at));
+    if (u1 <= u0) break;
+    const int u_end = good_length(a.c, len) && len > 0 ? u1 : u0, first_row = it.tile * kPrefixRows, my_row = first_row + wave * 32;
+    const bool mine = my_row < rows;                             // whether the wave has rows
+
+    // The pages of 64 places of the table on, a lane each: looked up one by one by scalar loads, which the waits for LDS operands are waits for,
+    // too, every unit would wait for two of them that wait for one another (128 sequences behind 32768 tokens x 8 heads: 144 us).
+    int looked_up = 0, page_here = 0;
+    float k_here = 0.0f, v_here = 0.0f;
+    const auto look_up = [&](int first) {
+      looked_up = first;
+      const int place = min(first + lane, (u1 - 1) * kUnit >> a.c.block_log2);
+      const int page = a.c.table[int64_t(pair) * a.c.max_pages + place];
+      const bool bad = page < 0 || page >= a.c.n_pages;
+      page_here = bad ? -1 : page;
+      k_here = bad ? __uint_as_float(kNanBits) : a.c.k_scale[max(page_here, 0)];
+      v_here = bad ? __uint_as_float(kNanBits) : a.c.v_scale[max(page_here, 0)];
+    };
+    const auto page_of = [&](int u) {
+      const int place = min(u, u1 - 1) * kUnit >> a.c.block_log2;
+      if (place - looked_up >= 64) look_up(place);
+      const int x = place - looked_up, page = __builtin_amdgcn_readlane(page_here, x);
+      const auto scale = [&](float y) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(y), x)); };
+      return Page{((int64_t(max(page, 0)) << a.c.block_log2) + (min(u, u1 - 1) * kUnit & ((1 << a.c.block_log2) - 1))) * kHeadDim, page < 0, scale(k_here), scale(v_here)};
+    };
+    look_up(u0 * kUnit >> a.c.block_log2);
+    const auto ask = [&](const uint8_t* base, const Page& page, bool there, Codes& c) {
+      const SlotBuffer b = unit_buffer(base, page.byte, there && !page.bad);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) c.x[x] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, tid * 8, x * 16 * kHeadDim, 0));
+    };
+    const auto put_keys = [&](const Codes& c, int stage) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) *reinterpret_cast<f16x8*>(lds.k[stage] + wr + x * 16 * kRowBytes) = key_operand<FMT>(c.x[x][0], c.x[x][1]);
+    };
+    // values with their scale, where that leaves fp16 numbers of them
+    const auto put_values = [&](Codes& c, int key0, float scale, int stage) {
+      if (key0 + kUnit > len) {                                  // codes behind the last token may be anything
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (key0 + (tid >> 4) + 16 * x >= len) c.x[x] = u32x2{0, 0};
+      }
+      const float f = fp16_scale<FMT>(scale) ? scale : 1.0f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t p = turned<FMT>(c.x[x][0]), q = turned<FMT>(c.x[x][1]);
+        *reinterpret_cast<u32x4*>(lds.v[stage] + wr + x * 16 * kRowBytes) =
+            u32x4{half_codes<FMT, false>(p, f), half_codes<FMT, true>(p, f), half_codes<FMT, false>(q, f), half_codes<FMT, true>(q, f)};
+      }
+    };
+
+    // ---- the first units and the queries
+    Page p0 = page_of(u0), p1 = page_of(u0 + 1), p2 = page_of(u0 + 2);      // of units u, u + 1 and u + 2
+    Codes kc, vc, k_first;
+    ask(a.c.k, p0, u0 < u_end, k_first);
+    ask(a.c.k, p1, u0 + 1 < u_end, kc);
+    ask(a.c.v, p0, u0 < u_end, vc);
+    f16x8 qf[NT][4];
+    float to_log2[NT], m[NT], l[NT];
+    f32x4 acc[NT][8], sc[NT][MT];
+    bool far_lane = false;
+    {
+      Query q[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int row = my_row + nt * 16 + n16;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) q[nt].part[x] = u32x4{0, 0, 0, 0};
+        if (row < rows) {
+          const int j = row / group, head = group_head(a.groups, h, row - j * group);
+          const uint16_t* src = a.q + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + 8 * hi;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) q[nt].part[x] = *reinterpret_cast<const u32x4*>(src + 32 * x);
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        to_log2[nt] = query_operands(a, q[nt], qf[nt]);
+        far_lane |= far_row(to_log2[nt]);
+        m[nt] = -INFINITY;
+        l[nt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) acc[nt][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+    bool far = __ballot(far_lane) != 0;
+
+    const auto read_k = [&](const char* kt, int gi) {
+      const int ks = gi / MT, mt = gi % MT;
+      return *reinterpret_cast<const f16x8*>(kt + (k_rd0 ^ (ks << 6)) + mt * 16 * kRowBytes);
+    };
+    const auto read_v = [&](const char* vt, int gi) {
+      const int gq = gi >> 3, dt = gi & 7;
+      const char* from = vt + (v_rd0 ^ (dt << 5)) + gq * 32 * kRowBytes;
+      const s16x4 lo = lds_read_tr16(from), up = lds_read_tr16(from + 16 * kRowBytes);
+      return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const auto next_scores = [&](const char* kt) {
+      f16x8 kf[kQK];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sc[nt][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int gi = 0; gi < kLook; ++gi) kf[gi] = read_k(kt, gi);
+#pragma unroll
+      for (int gi = 0; gi < kQK; ++gi) {
+        if (gi + kLook < kQK) kf[gi + kLook] = read_k(kt, gi + kLook);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sc[nt][gi % MT] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[gi], qf[nt][gi / MT], sc[nt][gi % MT], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+
+    __syncthreads();                                             // the stages are free
+    put_keys(k_first, 0);
+    __syncthreads();
+    if (mine && u0 < u_end) next_scores(lds.k[0]);
+    put_keys(kc, 1);
+    put_values(vc, u0 * kUnit, p0.v_scale, 0);
+    ask(a.c.k, p2, u0 + 2 < u_end, kc);
+    ask(a.c.v, p1, u0 + 1 < u_end, vc);
+    int stage = 0;                                               // of unit u
+    int u = u0;
+    // One unit.  scaled: its values are codes, and what they add is multiplied by the page's scale.
+    const auto step = [&](auto scaled_c) __attribute__((always_inline)) {
+      constexpr bool kScaled = decltype(scaled_c)::value;
+      const int key0 = u * kUnit;
+      const float k_scale = p0.k_scale, v_scale = p0.v_scale;
+      const Page p3 = page_of(u + 3);
+      __builtin_amdgcn_s_setprio(0);
+      __syncthreads();                       // keys of u + 1 and values of u are there; the stages of keys of u and values of u - 1 are free
+      f16x2 pk[NT][MT][2];
+      if (mine) {
+        float to[NT], rs[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) to[nt] = to_log2[nt] * k_scale;
+        if (far || key0 + kUnit > len) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const bool apart = far && to[nt] == INFINITY;
+            const float first = apart ? to_log2[nt] : to[nt], second = apart ? k_scale : 1.0f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) sc[nt][mt][r] = key0 + 16 * mt + 4 * hi + r < len ? sc[nt][mt][r] * first * second : -INFINITY;
+            to[nt] = 1.0f;
+          }
+        }
+        const auto probabilities = [&]() {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float off = kLift - (m[nt] == -INFINITY ? 0.0f : m[nt]);
+            float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int x = 0; x < 2 * MT; ++x) {
+              const int mt = x >> 1, c = x & 1;
+              const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][mt][2 * c], to[nt], off));
+              const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][mt][2 * c + 1], to[nt], off));
+              pk[nt][mt][c] = f16x2{(_Float16)e0, (_Float16)e1};
+              sum[0] += e0;
+              sum[1] += e1;
+            }
+            rs[nt] = sum[0] + sum[1];
+          }
+        };
+        probabilities();
+        // the reference is raised where a probability may be too large, or where there is none yet
+        const auto too_low = [&](int nt) { return !(rs[nt] <= kSumLimit) || m[nt] == -INFINITY; };
+        if (__any(too_low(0) || too_low(NT - 1))) {
+          bool raised_far = false;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float top = sc[nt][0][0];
+#pragma unroll
+            for (int x = 1; x < 4 * MT; ++x) top = fmaxf(top, sc[nt][x >> 2][x & 3]);
+            top = quad_max(top * to[nt]);
+            const float m_new = fmaxf(m[nt], top), alpha = m_new == m[nt] ? 1.0f : __builtin_amdgcn_exp2f(m[nt] - m_new);
+            m[nt] = m_new;
+            l[nt] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) acc[nt][dt] *= alpha;
+            raised_far |= far_reference(m_new);
+          }
+          if (!far && __ballot(raised_far)) {
+            far = true;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) sc[nt][mt] *= to[nt];
+              to[nt] = 1.0f;
+            }
+          }
+          probabilities();
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) l[nt] += rs[nt];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // the codes that are there go into the free stages, and the next ones are asked for
+      put_keys(kc, stage);
+      put_values(vc, key0 + kUnit, p1.v_scale, stage ^ 1);
+      ask(a.c.k, p3, u + 3 < u_end, kc);
+      ask(a.c.v, p2, u + 2 < u_end, vc);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      if (mine) {
+        if (u + 1 < u_end) next_scores(lds.k[stage ^ 1]);
+        const char* const vt = lds.v[stage];
+        const auto p_of = [&](int nt, int gq) {
+          return __builtin_bit_cast(f16x8, u32x4{__builtin_bit_cast(uint32_t, pk[nt][2 * gq][0]), __builtin_bit_cast(uint32_t, pk[nt][2 * gq][1]),
+                                                 __builtin_bit_cast(uint32_t, pk[nt][2 * gq + 1][0]), __builtin_bit_cast(uint32_t, pk[nt][2 * gq + 1][1])});
+        };
+        if constexpr (!kScaled) {
+          f16x8 vf[kPV];
+#pragma unroll
+          for (int gi = 0; gi < kLook; ++gi) vf[gi] = read_v(vt, gi);
+#pragma unroll
+          for (int gi = 0; gi < kPV; ++gi) {
+            if (gi + kLook < kPV) vf[gi + kLook] = read_v(vt, gi + kLook);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) acc[nt][gi & 7] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[gi], p_of(nt, gi >> 3), acc[nt][gi & 7], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        } else {
+          const float scale = fp16_scale<FMT>(v_scale) ? 1.0f : v_scale;
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+              for (int gq = 0; gq < 2; ++gq) x = __builtin_amdgcn_mfma_f32_16x16x32_f16(read_v(vt, 8 * gq + dt), p_of(nt, gq), x, 0, 0, 0);
+              acc[nt][dt] += x * scale;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      stage ^= 1;
+      p0 = p1;
+      p1 = p2;
+      p2 = p3;
+      ++u;
+    };
+    // From the first page on whose scale does not leave fp16 numbers of its values, units go by a loop of their own: in one with the other's
+    // products the output's registers would be moved.
+    while (u < u_end && fp16_scale<FMT>(p0.v_scale)) step(std::false_type{});
+#pragma unroll 1
+    while (u < u_end) step(std::true_type{});
+    __builtin_amdgcn_s_setprio(0);
+
+    // ---- partial results: a lane has dims 16 dt + 4 hi and on of its rows
+    const bool whole = u0 == 0 && u1 == units;
+    if (mine) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int row = my_row + nt * 16 + n16;
+        const float sum = quad_sum(l[nt]);
+        if (row >= rows) continue;
+        const int64_t slot = whole ? begun_row(a, row0, row, h, group) : (2 * int64_t(block) + (u0 == 0)) * kPrefixRows + (row - first_row);
+        float* o = (whole ? a.view.whole_o : a.part_o) + slot * kHeadDim + 4 * hi;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(o + 16 * dt) = acc[nt][dt];
+        if (hi == 0) *reinterpret_cast<f32x2*>((whole ? a.view.whole_ml : a.part_ml) + 2 * slot) = f32x2{m[nt], sum};
+      }
+    }
+    if (u0 == 0) note_rows(a, row0, n, h, group, first_row, kPrefixRows, tid, block, whole ? 0 : shares.of(at - it.unit + units - 1) - block + 1);
+    at += u1 - it.unit;
+    it.unit = -kPrefixStart;
+    if (++it.tile == tiles) it = next_pair<kPrefixStart>(a, pair);
+  }
 }
+
 template <int FMT>
-void launch_own(const CacheAttnArgs& a, int grid, int rows, hipStream_t stream) {
-  if (rows == 16) cache_attn_kernel<1, 1, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(a, 3);
-  else cache_attn_kernel<2, kWaves, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(a, kWaves);
+__global__ __launch_bounds__(kThreads, 2) void prefix_kernel(CacheAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) PrefixLds lds;
+  prefix_shares<FMT>(a, 4, int(blockIdx.x), int(gridDim.x), lds);
+}
+
+// Both in one launch: every other workgroup of a die attends to the prefixes.  Workgroup b goes to die b % 8, there to shader engine
+// (b / 8) % 4 in turn, whether it is free or not, and there to the eight compute units in turn: of two neighbours on a die there is one of
+// either kind, every engine has the kinds in turn, and so has every compute unit.
+template <int ROWS, int FMT, int VIEW>
+__device__ __forceinline__ void attend_rows(const CacheAttnArgs& a, int block, int blocks, AttnLds<ROWS / 16, ROWS == 16 ? 1 : kWaves>& lds) {
+  attend_shares<ROWS / 16, ROWS == 16 ? 1 : kWaves, false, FMT, VIEW, true>(a, ROWS == 16 ? 3 : kWaves, block, blocks, lds);
+}
+template <int ROWS, int OWN, int FMT>
+__global__ __launch_bounds__(kThreads, 2) void shared_attn_kernel(CacheAttnArgs a, CacheAttnArgs pre) {
+  __shared__ union {
+    AttnLds<OWN / 16, OWN == 16 ? 1 : kWaves> own;
+    AttnLds<ROWS / 16, ROWS == 16 ? 1 : kWaves> pre;
+  } lds;
+  const int b = int(blockIdx.x), blocks = int(gridDim.x) / 2, block = b / (2 * kXcds) * kXcds + b % kXcds, on_die = b / kXcds;
+  if ((on_die + on_die / 4 + on_die / 32) % 2 == 0) attend_rows<ROWS, FMT, kGroups>(pre, block, blocks, lds.pre);
+  else attend_rows<OWN, FMT, kAll>(a, block, blocks, lds.own);
 }
 
 // Joins a row's pieces, those of its prefix and those of its own tokens: with M the largest m, out = sum 2^(m - M) O / sum 2^(m -
-// M) l.  A wave a row; its halves take turns at the pieces, a lane four dims.
-__global__ __launch_bounds__(kThreads) void shared_join_kernel(CacheAttnArgs a, CacheAttnArgs pre, int rows_own, int rows_pre) {
-  const int lane = threadIdx.x & 63, d4 = lane & 31, half = lane >> 5;
+// M) l.  A workgroup a row (y) of an item (x) of own tokens, or, where there are many, a wave (THREADS = 64, four of them in a
+// workgroup); groups of 32 lanes take turns at the pieces, a lane four dims, and what they have is added up in order.  Where the
+// pieces are is noted by rows, so that all that has to be known of them comes in one go.
+template <int THREADS>
+__global__ __launch_bounds__(join_threads(THREADS)) void shared_join_kernel(CacheAttnArgs a, CacheAttnArgs pre, int rows_own, int rows_pre) {
+  constexpr int kParts = THREADS / 32, kMost = 2 * kCacheMaxWorkers;
+  constexpr bool kShared = THREADS > 64;       // each piece's statistics are read by one thread and shared
+  __shared__ float lds_m[kShared ? kMost : 1], lds_l[kShared ? kMost : 1];
+  __shared__ f32x4 lds_o[kShared ? kParts : 1][32];
+  const int tid = kShared ? threadIdx.x : threadIdx.x & 63, lane = tid & 63, d4 = tid & 31, part = tid >> 5;
   const int pair = blockIdx.x / uint32_t(a.tiles), tile = blockIdx.x - pair * a.tiles;
-  const int in_tile = int(blockIdx.y) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = tile * rows_own + in_tile;
+  const int in_tile = kShared ? int(blockIdx.y) : int(blockIdx.y) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = tile * rows_own + in_tile;
   const int s = pair / a.c.n_kv_heads, h = pair - s * a.c.n_kv_heads, group = group_size(a.groups, h);
   int row0, n;
   step_tokens<true>(a.t, s, row0, n);
-  if (in_tile >= rows_own || row >= n * group) return;
-  const int j = row / group, i = row - j * group, head = group_head(a.groups, h, i), len = scalar_load(a.c.lens + pair);
   const int2 own = *reinterpret_cast<const int2*>(a.begun + 2 * int64_t(blockIdx.x));
+  const int len = scalar_load(a.c.lens + pair);
+  const auto holds = [&](int x) { return x < pre.c.n_seq && pre.view.groups[min(x, pre.c.n_seq - 1)] <= s && s < pre.view.groups[min(x, pre.c.n_seq - 1) + 1]; };
+  const bool some = holds(lane);
+  if (in_tile >= rows_own || row >= n * group) return;           // (the item may not be one: nothing was written for it then)
+  const int j = row / group, i = row - j * group, head = group_head(a.groups, h, i);
+  const int64_t by_row = (int64_t(row0) + j) * a.n_q_heads + head;
+  const int2 front = *reinterpret_cast<const int2*>(pre.begun + 2 * by_row);
   // the prefix: the first one whose run of sequences holds this one
-  int g = -1;
-  for (int g0 = 0; g0 < pre.c.n_seq && g < 0; g0 += 64) {
-    const int at = min(g0 + lane, pre.c.n_seq - 1);
-    const uint64_t here = __ballot(g0 + lane < pre.c.n_seq && pre.view.groups[at] <= s && s < pre.view.groups[at + 1]);
+  uint64_t here = __ballot(some);
+  int g = here ? int(__builtin_ctzll(here)) : -1;
+  for (int g0 = 64; g0 < pre.c.n_seq && g < 0; g0 += 64) {
+    here = __ballot(holds(g0 + lane));
     if (here) g = g0 + int(__builtin_ctzll(here));
   }
-  int2 front = {0, 0};
-  int front_row = 0, prefix_len = 0;
+  // (What a row notes that is outside of its prefix's rows, as offsets that go backwards have it, is nothing that was written for it: it
+  // is not followed out of the slots, and the row is NaN.)
+  const int front_pieces = min(max(front.y >> 8, 0), kCacheMaxWorkers), front_begin = min(max(front.x, 0), kCacheMaxWorkers - front_pieces);
+  const int64_t front_row = min(front.y & 255, rows_pre - 1);
+  const int n_own = max(own.y, 1), pieces = n_own + (g >= 0 ? max(front_pieces, 1) : 0);
+  const auto place = [&](int x, const float*& o, const float*& ml) {
+    const int y = x - n_own;
+    const bool mine = y < 0, whole = mine ? own.y == 0 : front_pieces == 0;
+    const int64_t slot = mine ? (2 * int64_t(own.x + x) + (x == 0)) * rows_own + in_tile : (2 * int64_t(front_begin + y) + (y == 0)) * rows_pre + front_row;
+    const int64_t at = whole ? by_row : slot;
+    o = (mine ? whole ? a.view.whole_o : a.part_o : whole ? pre.view.whole_o : pre.part_o) + at * kHeadDim;
+    ml = (mine ? whole ? a.view.whole_ml : a.part_ml : whole ? pre.view.whole_ml : pre.part_ml) + 2 * at;
+  };
+  const auto stats = [&](int x) {
+    const float *o, *ml;
+    place(x, o, ml);
+    return *reinterpret_cast<const f32x2*>(ml);
+  };
+  const auto values = [&](int x) {
+    const float *o, *ml;
+    place(x, o, ml);
+    return *reinterpret_cast<const f32x4*>(o + d4 * 4);
+  };
+  constexpr int kEarly = kShared ? 4 : 8;
+  f32x4 early[kEarly];
+#pragma unroll
+  for (int x = 0; x < kEarly; ++x) early[x] = part + kParts * x < pieces ? values(part + kParts * x) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  f32x2 mine = {-INFINITY, 0.0f};
+  if (!kShared) {
+    if (lane < pieces) mine = stats(lane);
+  } else {
+    for (int x = tid; x < pieces; x += THREADS) {
+      const f32x2 ml = stats(x);
+      lds_m[x] = ml.x;
+      lds_l[x] = ml.y;
+    }
+  }
   bool good = good_length(a.c, len);
+  int prefix_len = 0;
   if (g >= 0) {
     int first, tokens;
     view_tokens<kGroups, true>(pre, g, first, tokens);
     prefix_len = scalar_load(pre.c.lens + int64_t(g) * pre.c.n_kv_heads + h);
     const int t = row0 + j - first;
-    good = good && good_length(pre.c, prefix_len) && t >= 0 && t < tokens;      // (offsets that go backwards: rows outside of their prefix's)
-    if (good) {
-      const int at = t * group + i, tile_row = at / rows_pre * rows_pre;
-      front = *reinterpret_cast<const int2*>(pre.begun + 2 * begun_row(pre, first, tile_row, h, group));
-      front_row = at - tile_row;
-    }
+    good = good && good_length(pre.c, prefix_len) && t >= 0 && t < tokens;
   }
-  // what was whole lies by rows, the pieces of the others in their shares' slots
-  const int64_t by_row = begun_row(a, row0, row, h, group);
-  const int n_own = good ? max(own.y, 1) : 0, pieces = n_own + (good && g >= 0 ? max(front.y, 1) : 0);
-  const auto stats = [&](int x) {
-    const int y = x - n_own;
-    const float* at = y < 0 ? (own.y == 0 ? a.view.whole_ml + 2 * by_row : a.part_ml + 2 * ((2 * int64_t(own.x + x) + (x == 0)) * rows_own + in_tile))
-                            : (front.y == 0 ? pre.view.whole_ml + 2 * by_row : pre.part_ml + 2 * ((2 * int64_t(front.x + y) + (y == 0)) * rows_pre + front_row));
-    return *reinterpret_cast<const f32x2*>(at);
-  };
-  const auto values = [&](int x) {
-    const int y = x - n_own;
-    const float* at = y < 0 ? (own.y == 0 ? a.view.whole_o + by_row * kHeadDim : a.part_o + ((2 * int64_t(own.x + x) + (x == 0)) * rows_own + in_tile) * kHeadDim)
-                            : (front.y == 0 ? pre.view.whole_o + by_row * kHeadDim : pre.part_o + ((2 * int64_t(front.x + y) + (y == 0)) * rows_pre + front_row) * kHeadDim);
-    return *reinterpret_cast<const f32x4*>(at + d4 * 4);
-  };
-  constexpr int kEarly = 4;
-  f32x4 early[kEarly];
-  float early_m[kEarly];
-#pragma unroll
-  for (int x = 0; x < kEarly; ++x) {
-    early[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    early_m[x] = -INFINITY;
-    if (half + 2 * x < pieces) {
-      early[x] = values(half + 2 * x);
-      early_m[x] = stats(half + 2 * x).x;
-    }
+  // every wave by itself, in the same order
+  if (kShared) {
+    __syncthreads();
+    if (lane < pieces) mine = f32x2{lds_m[lane], lds_l[lane]};
   }
-  f32x2 mine = {-INFINITY, 0.0f};
-  if (lane < pieces) mine = stats(lane);
+  const auto again = [&](int x) { return kShared ? f32x2{lds_m[x], lds_l[x]} : stats(x); };
   float top = mine.x;
-  for (int x = lane + 64; x < pieces; x += 64) top = fmaxf(top, stats(x).x);
+  for (int x = lane + 64; x < pieces; x += 64) top = fmaxf(top, again(x).x);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float ref = top == -INFINITY ? 0.0f : top;
-  float sum = __builtin_amdgcn_exp2f(mine.x - ref) * mine.y;
-  for (int x = lane + 64; x < pieces; x += 64) sum += __builtin_amdgcn_exp2f(stats(x).x - ref) * stats(x).y;
+  const float my_factor = __builtin_amdgcn_exp2f(mine.x - ref);
+  float sum = my_factor * mine.y;
+  for (int x = lane + 64; x < pieces; x += 64) {
+    const f32x2 ml = again(x);
+    sum += __builtin_amdgcn_exp2f(ml.x - ref) * ml.y;
+  }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int x = 0; x < kEarly; ++x)
-    if (half + 2 * x < pieces) o += __builtin_amdgcn_exp2f(early_m[x] - ref) * early[x];
+  for (int x = 0; x < kEarly; ++x) {
+    const int at = part + kParts * x;
+    const float f = kShared ? __builtin_amdgcn_exp2f(lds_m[at] - ref) : __shfl(my_factor, at);
+    if (at < pieces) o += f * early[x];
+  }
 #pragma unroll 8
-  for (int x = half + 2 * kEarly; x < pieces; x += 2) o += __builtin_amdgcn_exp2f(stats(x).x - ref) * values(x);
+  for (int x = part + kParts * kEarly; x < pieces; x += kParts) o += __builtin_amdgcn_exp2f(again(x).x - ref) * values(x);
+  if constexpr (!kShared) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], 32);
-  if (half) return;
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], 32);
+  } else {
+    lds_o[part][d4] = o;
+    __syncthreads();
+  }
+  if constexpr (kParts > 8) {
+    if (part < 4) {
+#pragma unroll
+      for (int x = 1; x < kParts / 4; ++x) o += lds_o[part + 4 * x][d4];
+    }
+    __syncthreads();
+    if (part < 4) lds_o[part][d4] = o;
+    __syncthreads();
+  }
+  if (tid >= 32) return;
+  if constexpr (kShared) {
+#pragma unroll
+    for (int x = 1; x < min(kParts, kParts > 8 ? 4 : 8); ++x) o += lds_o[x][d4];
+  }
   const float inv = row_inverse(good, max(len - n + 1 + j, 0) + prefix_len, sum);
   *reinterpret_cast<u32x2*>(a.out + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + d4 * 4) =
       u32x2{pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)};
-  if (lane == 0 && a.lse != nullptr) a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = row_lse(top, sum, inv);
+  if (tid == 0 && a.lse != nullptr) a.lse[int64_t(head) * a.t.n_tokens + row0 + j] = row_lse(top, sum, inv);
 }
 
 }  // namespace
@@ -133,17 +505,31 @@ int32_t launch_cache_attn_window(const CacheAttnArgs& a, int32_t most_rows, int3
                                         : launch_window<SHPLB_CACHE_INT8>(a, rows, most_rows, compute_units, stream);
 }
 
-int32_t prefix_attn_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }
-int64_t prefix_slot_rows(int32_t) { return kCacheSlotRows; }
+int32_t prefix_attn_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 48 ? 32 : kPrefixRows; }
+int64_t prefix_slot_rows(int32_t rows) { return rows == kPrefixRows ? int64_t(2) * (kCacheMaxWorkers / kWaves) * kPrefixRows : kCacheSlotRows; }
 
 int32_t launch_cache_attn_shared(const CacheAttnArgs& own, const CacheAttnArgs& pre, int32_t most_rows, int32_t rows_pre, int32_t compute_units, hipStream_t stream) {
   const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2), rows = cache_attn_rows(most_rows);
-  if (pre.c.format == SHPLB_CACHE_E4M3) launch_prefix<SHPLB_CACHE_E4M3>(pre, grid, rows_pre, stream);
-  else launch_prefix<SHPLB_CACHE_INT8>(pre, grid, rows_pre, stream);
-  if (own.c.format == SHPLB_CACHE_E4M3) launch_own<SHPLB_CACHE_E4M3>(own, grid, rows, stream);
-  else launch_own<SHPLB_CACHE_INT8>(own, grid, rows, stream);
-  const dim3 all(uint32_t(own.c.n_seq * own.c.n_kv_heads) * own.tiles, (min(rows, most_rows) + kWaves - 1) / kWaves);
-  shared_join_kernel<<<all, kThreads, 0, stream>>>(own, pre, rows, rows_pre);
+  const auto launch = [&](auto fmt_c) {
+    constexpr int FMT = decltype(fmt_c)::value;
+    if (rows_pre == kPrefixRows) {
+      prefix_kernel<FMT><<<grid, kThreads, 0, stream>>>(pre);
+      if (rows == 16) cache_attn_kernel<1, 1, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(own, 3);
+      else cache_attn_kernel<2, kWaves, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(own, kWaves);
+    } else if (rows_pre == 16) {
+      if (rows == 16) shared_attn_kernel<16, 16, FMT><<<2 * grid, kThreads, 0, stream>>>(own, pre);
+      else shared_attn_kernel<16, 32, FMT><<<2 * grid, kThreads, 0, stream>>>(own, pre);
+    } else {
+      if (rows == 16) shared_attn_kernel<32, 16, FMT><<<2 * grid, kThreads, 0, stream>>>(own, pre);
+      else shared_attn_kernel<32, 32, FMT><<<2 * grid, kThreads, 0, stream>>>(own, pre);
+    }
+  };
+  if (own.c.format == SHPLB_CACHE_E4M3) launch(std::integral_constant<int, SHPLB_CACHE_E4M3>{});
+  else launch(std::integral_constant<int, SHPLB_CACHE_INT8>{});
+  const dim3 all(uint32_t(own.c.n_seq * own.c.n_kv_heads) * own.tiles, min(rows, most_rows));
+  if (int64_t(all.x) * all.y <= 256) shared_join_kernel<1024><<<all, 1024, 0, stream>>>(own, pre, rows, rows_pre);
+  else if (int64_t(all.x) * all.y < 2048) shared_join_kernel<256><<<all, 256, 0, stream>>>(own, pre, rows, rows_pre);
+  else shared_join_kernel<64><<<dim3(all.x, (all.y + kWaves - 1) / kWaves), kThreads, 0, stream>>>(own, pre, rows, rows_pre);
   return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
 }
 

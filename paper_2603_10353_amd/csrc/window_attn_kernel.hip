@@ -179,39 +179,49 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int x = 1; x < 4 * MT; ++x) mx = fmaxf(mx, sc[qg][x >> 2][x & 3]);
       return mx;
     };
-    // scores of the tile at key0 from its stage, with masks
-    const auto scores = [&](const char* kt, int key0) {
-      bf16x8 kf[kQK];
-#pragma unroll
-      for (int qg = 0; qg < QG; ++qg)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sc[qg][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    typedef bf16x8 Operands[kQK];
+    static_assert(kPV == kQK, "as many for either product");
+    const auto first_k = [&](const char* kt, Operands& kf) {
 #pragma unroll
       for (int gi = 0; gi < kLook; ++gi) kf[gi] = read_k(kt, gi);
+    };
+    const auto first_v = [&](const char* vt, Operands& vf) {
+#pragma unroll
+      for (int gi = 0; gi < kLook; ++gi) vf[gi] = read_v(vt, gi);
+    };
+    // scores of a tile, the first operands being there; vt: the first ones of its values are fetched behind the last, into vf
+    const auto products_k = [&](const char* kt, Operands& kf, const char* vt, Operands* vf) {
 #pragma unroll
       for (int gi = 0; gi < kQK; ++gi) {
         if (gi + kLook < kQK) kf[gi + kLook] = read_k(kt, gi + kLook);
+        else if (vf != nullptr) (*vf)[gi + kLook - kQK] = read_v(vt, gi + kLook - kQK);
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg)
-          sc[qg][gi % MT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[gi], qf[qg][gi / MT], sc[qg][gi % MT], 0, 0, 0);
+          sc[qg][gi % MT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[gi], qf[qg][gi / MT], gi < MT ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[qg][gi % MT], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (masked(key0, w_first, w_last)) {
+    };
+    const auto mask_scores = [&](int key0) {
 #pragma unroll
-        for (int qg = 0; qg < QG; ++qg) {
-          int d = key0 + 4 * hi - q_pos[qg], e = key0 + 4 * hi - a.n_sink;
-          asm volatile("" : "+v"(d), "+v"(e));
+      for (int qg = 0; qg < QG; ++qg) {
+        int d = key0 + 4 * hi - q_pos[qg], e = key0 + 4 * hi - a.n_sink;
+        asm volatile("" : "+v"(d), "+v"(e));
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int rel = d + (16 * mt + r);
-              sc[qg][mt][r] = (rel > 0) | ((rel <= -a.window) & (e + (16 * mt + r) >= 0)) ? -INFINITY : sc[qg][mt][r];
-            }
-            asm volatile("" : "+v"(sc[qg][mt]));
+          for (int r = 0; r < 4; ++r) {
+            const int rel = d + (16 * mt + r);
+            sc[qg][mt][r] = (rel > 0) | ((rel <= -a.window) & (e + (16 * mt + r) >= 0)) ? -INFINITY : sc[qg][mt][r];
           }
+          asm volatile("" : "+v"(sc[qg][mt]));
         }
       }
+    };
+    const auto scores = [&](const char* kt, int key0) {
+      Operands kf;
+      first_k(kt, kf);
+      products_k(kt, kf, nullptr, nullptr);
+      if (masked(key0, w_first, w_last)) mask_scores(key0);
     };
 
     // ---- S(0).  (The item's copies have landed in this wave: see the end of the loop.)
@@ -221,14 +231,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int next_place = place + int(gridDim.x);
     const bool more = next_place < a.items;
     WindowItem next = it;
-#pragma unroll 1
-    for (int u = 0; u < it.tiles; ++u) {
+    int u = 0;
+    // One tile.  plain: all queries see all of it and of the next one.
+    const auto step = [&](auto plain_c) __attribute__((always_inline)) {
+      constexpr bool kPlain = decltype(plain_c)::value;
       const int key0 = it.key0(u), key1 = it.key0(u + 1);
-      const bool ends = u + 1 == it.tiles, mine = !hidden(key0), checked = masked(key0, first, last);
+      const bool ends = !kPlain && u + 1 == it.tiles, mine = kPlain || !hidden(key0), checked = !kPlain && masked(key0, first, last);
       const char* const vt = lds + (2 + stage) * kTileBytes;
+      const char* const kt = lds + (stage ^ 1) * kTileBytes;
+      Operands kf, vf;
       __builtin_amdgcn_s_setprio(0);
       wait_vmem_all();                       // own copies of K(u + 1), V(u) have landed ...
       __syncthreads();                       // ... and everyone's; the stages of K(u) and V(u - 1) are free
+      if constexpr (kPlain) {
+        first_k(kt, kf);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       if (!ends) {
         copy_v(it, u + 1, stage ^ 1);
         if (u + 2 < it.tiles) copy_k(it, u + 2, stage);
@@ -295,7 +313,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
       // ---- S(u + 1)
       __builtin_amdgcn_s_setprio(1);
-      if (!ends && !hidden(key1)) scores(lds + (stage ^ 1) * kTileBytes, key1);
+      if constexpr (kPlain) products_k(kt, kf, vt, &vf);
+      else if (!ends && !hidden(key1)) scores(kt, key1);
 
       // ---- O^T += V(u)^T P(u)^T
       if (checked) {
@@ -359,9 +378,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         }
       }
       if (mine) {
-        bf16x8 vf[kPV];
-#pragma unroll
-        for (int gi = 0; gi < kLook; ++gi) vf[gi] = read_v(vt, gi);
+        if constexpr (!kPlain) first_v(vt, vf);
 #pragma unroll
         for (int gi = 0; gi < kPV; ++gi) {
           if (gi + kLook < kPV) vf[gi + kLook] = read_v(vt, gi + kLook);
@@ -376,6 +393,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       }
       stage ^= 1;
       ++step_no;
+      ++u;
+    };
+    const auto plain = [&]() { return u + 1 < it.tiles && !masked(it.key0(u), first, last) && !masked(it.key0(u + 1), first, last); };
+#pragma unroll 1
+    while (u < it.tiles) {
+#pragma unroll 1
+      while (plain()) step(std::true_type{});
+      step(std::false_type{});               // (the last tile is never plain)
     }
     __builtin_amdgcn_s_setprio(0);
 

@@ -55,6 +55,7 @@ CASES = {  # lengths of prefixes, cu_prefix, own lengths, new tokens, query head
     "many_heads": ([[100] * 4, [30] * 4], [0, 290, 300], [[5, 70, 1, 20]] * 310, [1] * 310, 4, 4),
     "many_prefixes": ([[70, 5]] * 300, list(range(301)), [[5, 70]] * 300, [1] * 300, 4, 2),
     "many_prefixes_rows": ([[70]] * 40, [20 * x for x in range(41)], [[9]] * 800, [1] * 800, 1, 1),
+    "rows_200_short": ([[40, 300], [0, 64]], [0, 25, 50], [[9, 2]] * 50, [1] * 50, 16, 2),
     "draft": ([[400]], [0, 9], [[40]] * 9, [3, 1, 4, 1, 5, 0, 2, 6, 5], 7, 1),
     "pieces_of_prompts": ([[200]], [0, 2], [[64], [150]], [64, 100], 4, 1),
 }
@@ -78,10 +79,10 @@ def test_sizes(name, block, fmt):
     check(want, out, lse, slice(0, T), int(np.max(plens) + np.max(lens)), HALF, LIFT)
 
 
-def test_formats_blocks_strides_mapped_heads_scale_rows_behind():
+def test_blocks_strides_mapped_heads_scale_rows_behind():
     rng = np.random.default_rng(4)
     kv_of = [2, 0, 0, 2, 0]                    # one KV head without query heads
-    prefix = filled(rng, [[300, 50, 77]], 64, INT8)
+    prefix = filled(rng, [[300, 50, 77]], 64, E4M3)
     c = filled(rng, [[100, 50, 300], [80, 1, 129], [9, 9, 9]], 128, E4M3)
     pre, dev = Device(prefix), Device(c)
     q, q64 = bf16(rng.standard_normal((8, 5, D)))

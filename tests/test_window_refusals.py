@@ -151,8 +151,10 @@ def test_prefixes():
         assert status(call) == -2
     lib = S.load_library()
     assert lib.shplb_cache_attn_shared_workspace_bytes(cache().ref(), cache().ref(), step().ref(), None) == -1
-    # other formats, blocks and numbers of sequences than the prefixes' are fine
-    other = cache(format=S.SHPLB_CACHE_INT8, block=64, n_seq=7)
+    for call in shared_calls(cache(format=S.SHPLB_CACHE_INT8), cache(), step()):
+        assert status(call) == -2
+    # other blocks and numbers of sequences than the prefixes' are fine
+    other = cache(block=64, n_seq=7)
     assert S.shplb_cache_attn_shared_workspace_bytes(other, cache(), step()) > 0
 
 
@@ -162,7 +164,7 @@ def test_limits():
     for call in shared_calls(cache(), cache(), many):
         assert status(call) == -5
     long = cache(max_pages=4096, n_seq=1)
-    for tokens, fits in ((1 << 12, True), (1 << 18, False)):
+    for tokens, fits in ((1 << 12, True), (1 << 19, False)):
         s = step(n_tokens=2 * tokens, max_tokens=tokens)
         if fits:
             assert S.shplb_cache_attn_shared_workspace_bytes(long, cache(), s) > 0
