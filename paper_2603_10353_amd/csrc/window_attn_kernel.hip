@@ -114,6 +114,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const auto copy_tile = [&](const uint16_t* base, const WindowItem& w, int u, uint32_t dst) {
     const int at = min(w.key0(u), w.len - 1), last = w.len - 1 - at;
     const char* tile = uniform(reinterpret_cast<const char*>(base + int64_t(w.kv_head) * a.st.kv_h) + (int64_t(w.seq_begin) + at) * row_bytes);
+    dst = __builtin_amdgcn_readfirstlane(dst);
     if (last >= kKeys - 1) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) copy_g2l_16(tile + int64_t(16 * r) * row_bytes, cp_off, dst + 16 * r * kRowBytes);
@@ -204,16 +205,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const auto mask_scores = [&](int key0) {
 #pragma unroll
       for (int qg = 0; qg < QG; ++qg) {
-        int d = key0 + 4 * hi - q_pos[qg], e = key0 + 4 * hi - a.n_sink;
-        asm volatile("" : "+v"(d), "+v"(e));
+        int back = q_pos[qg] - key0 - 4 * hi, left = a.n_sink - key0 - 4 * hi;         // how far back a key lies; first tokens from it on
+        asm volatile("" : "+v"(back), "+v"(left));
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int rel = d + (16 * mt + r);
-            sc[qg][mt][r] = (rel > 0) | ((rel <= -a.window) & (e + (16 * mt + r) >= 0)) ? -INFINITY : sc[qg][mt][r];
-          }
-          asm volatile("" : "+v"(sc[qg][mt]));
+        for (int x = 0; x < 4 * MT; ++x) {
+          const int at = 16 * (x >> 2) + (x & 3);
+          sc[qg][x >> 2][x & 3] = (uint32_t(back - at) < uint32_t(a.window)) | ((back >= at) & (left > at)) ? sc[qg][x >> 2][x & 3] : -INFINITY;
+          if ((x & 3) == 3) asm volatile("" : "+v"(sc[qg][x >> 2]));
         }
       }
     };
@@ -232,7 +230,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const bool more = next_place < a.items;
     WindowItem next = it;
     int u = 0;
-    // One tile.  plain: all queries see all of it and of the next one.
+    // One tile.  plain: all queries see all of it, and it is not the last one.
     const auto step = [&](auto plain_c) __attribute__((always_inline)) {
       constexpr bool kPlain = decltype(plain_c)::value;
       const int key0 = it.key0(u), key1 = it.key0(u + 1);
@@ -257,15 +255,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       __builtin_amdgcn_sched_barrier(0);
       if (checked) {
         // whether all values are finite, a quarter of them looked at by each wave
-        u32x4 top = {0, 0, 0, 0};
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 top[4] = {};
 #pragma unroll
         for (int x = 0; x < kTileBytes / (16 * kThreads); ++x) {
           const u32x4 w = *reinterpret_cast<const u32x4*>(vt + (x * kThreads + tid) * 16);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top[e] = max(max(top[e], w[e] << 16 & 0x7fff0000u), w[e] & 0x7fff0000u);
+          for (int e = 0; e < 4; ++e) top[e] = __builtin_elementwise_max(top[e], __builtin_bit_cast(u16x2, w[e] & 0x7fff7fffu));
         }
-        const uint32_t most = max(max(top[0], top[1]), max(top[2], top[3]));
-        if (__ballot(most >= 0x7f800000u) != 0 && lane == 0) s_bad = step_no;
+        const u16x2 most = __builtin_elementwise_max(__builtin_elementwise_max(top[0], top[1]), __builtin_elementwise_max(top[2], top[3]));
+        if (__ballot(max(most.x, most.y) >= 0x7f80) != 0 && lane == 0) s_bad = step_no;
       }
 
       // ---- probabilities of tile u
@@ -313,8 +312,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
       // ---- S(u + 1)
       __builtin_amdgcn_s_setprio(1);
-      if constexpr (kPlain) products_k(kt, kf, vt, &vf);
-      else if (!ends && !hidden(key1)) scores(kt, key1);
+      if constexpr (kPlain) {
+        products_k(kt, kf, vt, &vf);
+        if (masked(key1, w_first, w_last)) mask_scores(key1);
+      } else if (!ends && !hidden(key1)) scores(kt, key1);
 
       // ---- O^T += V(u)^T P(u)^T
       if (checked) {
@@ -395,7 +396,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       ++step_no;
       ++u;
     };
-    const auto plain = [&]() { return u + 1 < it.tiles && !masked(it.key0(u), first, last) && !masked(it.key0(u + 1), first, last); };
+    const auto plain = [&]() { return u + 1 < it.tiles && !masked(it.key0(u), first, last); };
 #pragma unroll 1
     while (u < it.tiles) {
 #pragma unroll 1
