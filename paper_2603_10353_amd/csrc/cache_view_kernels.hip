@@ -72,8 +72,22 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
     const int u_end = good_length(a.c, len) && len > 0 ? u1 : u0, first_row = it.tile * kPrefixRows, my_row = first_row + wave * 32;
     const bool mine = my_row < rows;                             // whether the wave has rows
 
-    // The pages of 64 places of the table on, a lane each: looked up one by one by scalar loads, which the waits for LDS operands are waits for,
-    // too, every unit would wait for two of them that wait for one another (128 sequences behind 32768 tokens x 8 heads: 144 us).
+    // The queries are on their way while pages are looked up.
+    Query q[2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = my_row + nt * 16 + n16;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) q[nt].part[x] = u32x4{0, 0, 0, 0};
+      if (row < rows) {
+        const int j = row / group, head = group_head(a.groups, h, row - j * group);
+        const uint16_t* src = a.q + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + 8 * hi;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) q[nt].part[x] = *reinterpret_cast<const u32x4*>(src + 32 * x);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // The pages of 64 places of the table on, a lane each.  (One by one by scalar loads the waits for LDS operands would be waits for them, too.)
     int looked_up = 0, page_here = 0;
     float k_here = 0.0f, v_here = 0.0f;
     const auto look_up = [&](int first) {
@@ -82,18 +96,29 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
       const int page = a.c.table[int64_t(pair) * a.c.max_pages + place];
       const bool bad = page < 0 || page >= a.c.n_pages;
       page_here = bad ? -1 : page;
-      k_here = bad ? __uint_as_float(kNanBits) : a.c.k_scale[max(page_here, 0)];
-      v_here = bad ? __uint_as_float(kNanBits) : a.c.v_scale[max(page_here, 0)];
+      k_here = a.c.k_scale[max(page_here, 0)];
+      v_here = a.c.v_scale[max(page_here, 0)];
+    };
+    const auto place_of = [&](int u) { return (min(u, u1 - 1) * kUnit >> a.c.block_log2) - looked_up; };
+    // where a unit's codes are; its scales are asked for while it is on its way, and are there later
+    struct Codes8 {
+      int64_t byte;
+      bool bad;
     };
     const auto page_of = [&](int u) {
-      const int place = min(u, u1 - 1) * kUnit >> a.c.block_log2;
-      if (place - looked_up >= 64) look_up(place);
-      const int x = place - looked_up, page = __builtin_amdgcn_readlane(page_here, x);
-      const auto scale = [&](float y) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(y), x)); };
-      return Page{((int64_t(max(page, 0)) << a.c.block_log2) + (min(u, u1 - 1) * kUnit & ((1 << a.c.block_log2) - 1))) * kHeadDim, page < 0, scale(k_here), scale(v_here)};
+      if (place_of(u) >= 64) look_up(looked_up + place_of(u));
+      const int page = __builtin_amdgcn_readlane(page_here, place_of(u));
+      return Codes8{((int64_t(max(page, 0)) << a.c.block_log2) + (min(u, u1 - 1) * kUnit & ((1 << a.c.block_log2) - 1))) * kHeadDim, page < 0};
+    };
+    struct Scales {
+      float k, v;
+    };
+    const auto scales_of = [&](int u, bool bad) {                // (of a unit whose page was the last one asked for, or one before it)
+      const auto lane_value = [&](float y) { return bad ? __uint_as_float(kNanBits) : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(y), place_of(u))); };
+      return Scales{lane_value(k_here), lane_value(v_here)};
     };
     look_up(u0 * kUnit >> a.c.block_log2);
-    const auto ask = [&](const uint8_t* base, const Page& page, bool there, Codes& c) {
+    const auto ask = [&](const uint8_t* base, const Codes8& page, bool there, Codes& c) {
       const SlotBuffer b = unit_buffer(base, page.byte, there && !page.bad);
 #pragma unroll
       for (int x = 0; x < 4; ++x) c.x[x] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, tid * 8, x * 16 * kHeadDim, 0));
@@ -118,8 +143,9 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
       }
     };
 
-    // ---- the first units and the queries
-    Page p0 = page_of(u0), p1 = page_of(u0 + 1), p2 = page_of(u0 + 2);      // of units u, u + 1 and u + 2
+    // ---- the first units
+    const Codes8 p0 = page_of(u0);
+    Codes8 p1 = page_of(u0 + 1), p2 = page_of(u0 + 2);           // of units u + 1 and u + 2
     Codes kc, vc, k_first;
     ask(a.c.k, p0, u0 < u_end, k_first);
     ask(a.c.k, p1, u0 + 1 < u_end, kc);
@@ -129,19 +155,6 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
     f32x4 acc[NT][8], sc[NT][MT];
     bool far_lane = false;
     {
-      Query q[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int row = my_row + nt * 16 + n16;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) q[nt].part[x] = u32x4{0, 0, 0, 0};
-        if (row < rows) {
-          const int j = row / group, head = group_head(a.groups, h, row - j * group);
-          const uint16_t* src = a.q + (int64_t(row0) + j) * a.t.stride_t + head * a.t.stride_h + 8 * hi;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) q[nt].part[x] = *reinterpret_cast<const u32x4*>(src + 32 * x);
-        }
-      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         to_log2[nt] = query_operands(a, q[nt], qf[nt]);
@@ -186,7 +199,8 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
     __syncthreads();
     if (mine && u0 < u_end) next_scores(lds.k[0]);
     put_keys(kc, 1);
-    put_values(vc, u0 * kUnit, p0.v_scale, 0);
+    Scales s0 = scales_of(u0, p0.bad), s1 = scales_of(u0 + 1, p1.bad);         // of units u and u + 1
+    put_values(vc, u0 * kUnit, s0.v, 0);
     ask(a.c.k, p2, u0 + 2 < u_end, kc);
     ask(a.c.v, p1, u0 + 1 < u_end, vc);
     int stage = 0;                                               // of unit u
@@ -195,8 +209,9 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
     const auto step = [&](auto scaled_c) __attribute__((always_inline)) {
       constexpr bool kScaled = decltype(scaled_c)::value;
       const int key0 = u * kUnit;
-      const float k_scale = p0.k_scale, v_scale = p0.v_scale;
-      const Page p3 = page_of(u + 3);
+      const float k_scale = s0.k, v_scale = s0.v;
+      const Scales s2 = scales_of(u + 2, p2.bad);
+      const Codes8 p3 = page_of(u + 3);
       __builtin_amdgcn_s_setprio(0);
       __syncthreads();                       // keys of u + 1 and values of u are there; the stages of keys of u and values of u - 1 are free
       f16x2 pk[NT][MT][2];
@@ -268,7 +283,7 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
       __builtin_amdgcn_sched_barrier(0);
       // the codes that are there go into the free stages, and the next ones are asked for
       put_keys(kc, stage);
-      put_values(vc, key0 + kUnit, p1.v_scale, stage ^ 1);
+      put_values(vc, key0 + kUnit, s1.v, stage ^ 1);
       ask(a.c.k, p3, u + 3 < u_end, kc);
       ask(a.c.v, p2, u + 2 < u_end, vc);
       __builtin_amdgcn_sched_barrier(0);
@@ -307,14 +322,15 @@ __device__ __forceinline__ void prefix_shares(const CacheAttnArgs& a, int least,
         }
       }
       stage ^= 1;
-      p0 = p1;
+      s0 = s1;
+      s1 = s2;
       p1 = p2;
       p2 = p3;
       ++u;
     };
     // From the first page on whose scale does not leave fp16 numbers of its values, units go by a loop of their own: in one with the other's
     // products the output's registers would be moved.
-    while (u < u_end && fp16_scale<FMT>(p0.v_scale)) step(std::false_type{});
+    while (u < u_end && fp16_scale<FMT>(s0.v)) step(std::false_type{});
 #pragma unroll 1
     while (u < u_end) step(std::true_type{});
     __builtin_amdgcn_s_setprio(0);
