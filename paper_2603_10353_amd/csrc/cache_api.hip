@@ -141,7 +141,7 @@ int32_t check_shared(const shplb_cache* prefix, const shplb_cache* cache, const 
   // the rows of a KV head, all of which may have the same prefix
   const int64_t most_heads = step->max_tokens > 0 ? x->most_rows / step->max_tokens : 1, rows = int64_t(step->n_tokens) * most_heads;
   if (rows > 1 << 24) return SHPLB_E_UNSUPPORTED;
-  x->rows_pre = prefix_attn_rows(rows / prefix->n_seq);
+  x->rows_pre = prefix_attn_rows(rows / prefix->n_seq, int64_t(prefix->n_seq) * prefix->n_kv_heads, int64_t(prefix->max_pages) * prefix->block);
   const int64_t items = (rows / x->rows_pre + prefix->n_seq) * prefix->n_kv_heads;
   if (items >= int64_t(1) << 24 || items * (int64_t(prefix->max_pages) * prefix->block / 64 + kCacheMostStart) >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
   x->w = attn_layout(cache, step, x->most_rows);

@@ -83,8 +83,9 @@ int64_t cache_evict_workspace(const CacheArgs& c);
 // Rows (query token, head of the group) of an item of the list that the work is divided from.
 int32_t cache_attn_rows(int64_t most_rows);
 int32_t launch_cache_attn_window(const CacheAttnArgs& a, int32_t most_rows, int32_t compute_units, hipStream_t stream);
-// Rows of an item of the list that the work on prefixes is divided from, where a prefix and KV head has so many on average.
-int32_t prefix_attn_rows(int64_t rows);
+// Rows of an item of the list that the work on prefixes is divided from: of `pairs` prefixes and KV heads with so many rows on average and
+// room for so many tokens.
+int32_t prefix_attn_rows(int64_t rows, int64_t pairs, int64_t room);
 // ... and rows of partial results of such items.
 int64_t prefix_slot_rows(int32_t rows);
 int32_t launch_cache_attn_shared(const CacheAttnArgs& own, const CacheAttnArgs& pre, int32_t most_rows, int32_t rows_pre, int32_t compute_units, hipStream_t stream);

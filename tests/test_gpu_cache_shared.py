@@ -79,6 +79,70 @@ def test_sizes(name, block, fmt):
     check(want, out, lse, slice(0, T), int(np.max(plens) + np.max(lens)), HALF, LIFT)
 
 
+# By what the tables have room for, more rows are worked on 128 at a time, and prefixes and own tokens in two launches.
+ROOMY = {  # ..., pages that tables have room for: of the prefixes, of the own tokens
+    "rows_128": ([[250, 70]] * 3, [0, 30, 41, 70], [[9, 70]] * 72, [1] * 72, 8, 2, 4096, 4),
+    "rows_128_uneven": ([[1, 0, 333], [64, 900, 128]], [2, 30, 55], [[9, 20, 30]] * 57, [2] * 57, 12, 3, 2000, 4),
+    "rows_128_of_many": ([[130]] * 20, [15 * x for x in range(21)], [[20]] * 300, [1] * 300, 4, 1, 4000, 2),
+    "rows_128_pieces": ([[200]], [0, 2], [[64], [150]], [64, 100], 4, 1, 4096, 4),
+    "rows_16": ([[100, 30]] * 30, [2 * x for x in range(31)], [[30, 200]] * 62, [1] * 62, 8, 2, 600, 100),
+    "rows_32": ([[100, 30]] * 10, [7 * x for x in range(11)], [[30, 200]] * 70, [1] * 70, 8, 2, 1500, 5),
+    "rows_32_own_too": ([[100, 30]] * 5, [2 * x for x in range(6)], [[30, 200]] * 10, [5] * 10, 8, 2, 1500, 1500),
+}
+
+
+@FORMATS
+@pytest.mark.parametrize("block", [128, 64])
+@pytest.mark.parametrize("name", ROOMY)
+def test_tables_with_room(name, block, fmt):
+    plens, groups, lens, new, hq, hkv, prefix_pages, own_pages = ROOMY[name]
+    rng = np.random.default_rng([fmt, block, len(name)])
+    if name == "rows_128_uneven":
+        prefix_pages *= 2
+    prefix, c = filled(rng, plens, block, fmt, max_pages=prefix_pages, extra_pages=1), filled(rng, lens, block, fmt, max_pages=max(own_pages, 200 // block + 1))
+    pre, dev = Device(prefix), Device(c)
+    T = int(np.sum(new))
+    q, q64 = bf16(rng.standard_normal((T, hq, D)))
+    step, cu = step_of(dev, new, hq, len(set(new)) > 1)
+    out, lse = call(pre, groups, dev, step, q.to(DEV))
+    want = orc.cache_shared(prefix, groups, c, q64, cu, np.arange(hq) * hkv // hq)
+    check(want, out, lse, slice(0, T), int(np.max(plens) + np.max(lens)), HALF, LIFT)
+
+
+@FORMATS
+def test_shares_of_many_pages(fmt):
+    """A prefix so long that a workgroup's share has more pages than are looked up at once, some of scales that fp16 does not hold; a few
+    rows against their products in 64 bits."""
+    gen = torch.Generator(device=DEV).manual_seed(fmt)
+    n, P, hq, hkv, block = 512, 100001, 8, 2, 64
+    pages = -(-P // block)
+    codes = lambda: (torch.randint(0, 256, (hkv * pages, block, D), device=DEV, generator=gen) % 127
+                     + 128 * torch.randint(0, 2, (hkv * pages, block, D), device=DEV, generator=gen)).to(torch.uint8)
+    k, v = codes(), codes()
+    ks = torch.exp2(torch.randint(-9, -6, (hkv * pages,), device=DEV, generator=gen).float())
+    vs = torch.exp2(torch.randint(-9, -6, (hkv * pages,), device=DEV, generator=gen).float())
+    table = torch.randperm(hkv * pages, device=DEV, generator=gen).to(torch.int32).view(1, hkv, pages)
+    vs[table[0, 1, pages // 2].long()] = 2.0 ** -30
+    lens = torch.full((1, hkv), P, dtype=torch.int32, device=DEV)
+    prefix = S.Cache(k, v, ks, vs, table, lens, 1, hkv, block, pages, hkv * pages, S.SHPLB_CACHE_E4M3 if fmt == E4M3 else S.SHPLB_CACHE_INT8)
+    own = Device(cache_oracle.CacheState(*(np.zeros((1, block, D), np.uint8),) * 2, np.ones(1), np.ones(1), np.full((n, hkv, 1), -1, np.int32), np.zeros((n, hkv), np.int32), fmt))
+    q = torch.randn((n, hq, D), device=DEV, generator=gen).to(torch.bfloat16)
+    step = S.Step(n, hq, hkv)
+    out, lse = torch.zeros_like(q), torch.zeros((hq, n), device=DEV)
+    ws = torch.empty(S.shplb_cache_attn_shared_workspace_bytes(prefix, own.cache, step), dtype=torch.uint8, device=DEV)
+    S.shplb_cache_attn_shared(prefix, cu_of([0, n]), own.cache, step, q, out, lse, ws, stream())
+    value = torch.from_numpy(cache_oracle.decode(np.arange(256), fmt)).to(DEV)
+    rows = [0, 1, 77, 128, 300, 511]
+    want = orc.Result(np.zeros((len(rows), hq, D)))
+    for h in range(hkv):
+        at = table[0, h].long()
+        kh, vh = ((value[x[at].long()] * sc[at].double()[:, None, None]).view(-1, D)[:P] for x, sc in ((k, ks), (v, vs)))
+        for i, r in enumerate(rows):
+            for x in range(4 * h, 4 * h + 4):
+                want.put(i, x, q[r, x].double().cpu().numpy(), kh.cpu().numpy(), vh.cpu().numpy(), D ** -0.5, True)
+    check(want, out[rows].double().cpu().numpy(), lse[:, rows].double().cpu().numpy(), slice(0, len(rows)), P, HALF, LIFT)
+
+
 def test_blocks_strides_mapped_heads_scale_rows_behind():
     rng = np.random.default_rng(4)
     kv_of = [2, 0, 0, 2, 0]                    # one KV head without query heads
