@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_attn_kernel(CacheAttnArgs 
 // workgroup); groups of 32 lanes take turns at the pieces, a lane four dims, and what they have is added up in order.  Where the
 // pieces are is noted by rows, so that all that has to be known of them comes in one go.
 template <int THREADS>
-__global__ __launch_bounds__(join_threads(THREADS)) void shared_join_kernel(CacheAttnArgs a, CacheAttnArgs pre, int rows_own, int rows_pre) {
+__global__ __launch_bounds__(join_threads(THREADS)) void shared_join_kernel(CacheAttnArgs a, CacheAttnArgs pre, int rows_own, int rows_pre, int shares_pre) {
   constexpr int kParts = THREADS / 32, kMost = 2 * kCacheMaxWorkers;
   constexpr bool kShared = THREADS > 64;       // each piece's statistics are read by one thread and shared
   __shared__ float lds_m[kShared ? kMost : 1], lds_l[kShared ? kMost : 1];
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(join_threads(THREADS)) void shared_join_kernel(Cach
   }
   // (What a row notes that is outside of its prefix's rows, as offsets that go backwards have it, is nothing that was written for it: it
   // is not followed out of the slots, and the row is NaN.)
-  const int front_pieces = min(max(front.y >> 8, 0), kCacheMaxWorkers), front_begin = min(max(front.x, 0), kCacheMaxWorkers - front_pieces);
+  const int front_pieces = min(max(front.y >> 8, 0), shares_pre), front_begin = min(max(front.x, 0), shares_pre - front_pieces);
   const int64_t front_row = min(front.y & 255, rows_pre - 1);
   const int n_own = max(own.y, 1), pieces = n_own + (g >= 0 ? max(front_pieces, 1) : 0);
   const auto place = [&](int x, const float*& o, const float*& ml) {
@@ -560,10 +560,11 @@ int32_t launch_cache_attn_shared(const CacheAttnArgs& own, const CacheAttnArgs& 
   };
   if (own.c.format == SHPLB_CACHE_E4M3) launch(std::integral_constant<int, SHPLB_CACHE_E4M3>{});
   else launch(std::integral_constant<int, SHPLB_CACHE_INT8>{});
+  const int shares_pre = int(prefix_slot_rows(rows_pre) / (2 * rows_pre));      // that there are slots for
   const dim3 all(uint32_t(own.c.n_seq * own.c.n_kv_heads) * own.tiles, min(rows, most_rows));
-  if (int64_t(all.x) * all.y <= 256) shared_join_kernel<1024><<<all, 1024, 0, stream>>>(own, pre, rows, rows_pre);
-  else if (int64_t(all.x) * all.y < 2048) shared_join_kernel<256><<<all, 256, 0, stream>>>(own, pre, rows, rows_pre);
-  else shared_join_kernel<64><<<dim3(all.x, (all.y + kWaves - 1) / kWaves), kThreads, 0, stream>>>(own, pre, rows, rows_pre);
+  if (int64_t(all.x) * all.y <= 256) shared_join_kernel<1024><<<all, 1024, 0, stream>>>(own, pre, rows, rows_pre, shares_pre);
+  else if (int64_t(all.x) * all.y < 2048) shared_join_kernel<256><<<all, 256, 0, stream>>>(own, pre, rows, rows_pre, shares_pre);
+  else shared_join_kernel<64><<<dim3(all.x, (all.y + kWaves - 1) / kWaves), kThreads, 0, stream>>>(own, pre, rows, rows_pre, shares_pre);
   return hipGetLastError() == hipSuccess ? SHPLB_OK : SHPLB_E_HIP;
 }
 

@@ -193,8 +193,9 @@ def test_offsets_out_of_range():
     got = call(pre, [-5, 3, 99], dev, step, q.to(DEV))
     check(orc.cache_shared(prefix, [0, 3, 4], c, q64, cu, [0, 0]), *got, slice(0, 4), 110, HALF, LIFT)
     step = S.Step(4, 2, 1, 4, 2, torch.tensor([0, 3, 1, -7, 99], dtype=torch.int32, device=DEV))
-    call(pre, [0, 2, 4], dev, step, q.to(DEV))
-    call(pre, [3, 1, 2], dev, step, q.to(DEV))
+    for groups in ([0, 2, 4], [3, 1, 2]):
+        for left in (0xff, 0x7f, 0x01):
+            call(pre, groups, dev, step, q.to(DEV), workspace(pre, dev, step).fill_(left))
 
 
 def test_large_scales_and_queries():

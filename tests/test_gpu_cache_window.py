@@ -63,6 +63,13 @@ CASES = {  # lengths, new tokens, query heads, KV heads, sinks, window
     "by_shares": ([[5000, 300], [2, 3500]], [1, 1], 4, 2, 130, 2600),
     "by_shares_tokens": ([[4500, 300], [2900, 3500]], [5, 2], 4, 2, 4, 2500),
     "by_shares_rows": ([[4700, 6000]], [20], 4, 2, 64, 4100),
+    "wide": ([[700, 65], [300, 500]], [40, 64], 8, 2, 4, 100),
+    "wide_sinks": ([[700], [90], [64]], [100, 77, 3], 3, 1, 200, 130),
+    "wide_whole_prompts": ([[200], [150], [64]], [200, 150, 64], 2, 1, 0, 31),
+    "wide_long": ([[6000, 9000]], [70], 4, 2, 130, 4100),
+    "wide_more_than_held": ([[30, 200], [0, 1], [100, 100]], [64, 40, 0], 4, 2, 2, 70),
+    "wide_everything": ([[1500]], [60], 4, 1, 0, 2 ** 31 - 1),
+    "wide_uneven_groups": ([[260, 300, 10]], [25], 21, 3, 1, 70),
     "groups_of_seven": ([[260, 300, 10]], [3], 21, 3, 1, 70),
 }
 
@@ -72,6 +79,7 @@ CASES = {  # lengths, new tokens, query heads, KV heads, sinks, window
 @pytest.mark.parametrize("name", CASES)
 def test_sizes(name, block, fmt):
     lens, new, hq, hkv, n_sink, window = CASES[name]
+    assert len(lens[0]) == hkv
     rng = np.random.default_rng([fmt, block, len(name)])
     c = filled(rng, lens, block, fmt, max_pages=60 if name == "small" else None)
     new = np.array(new)
@@ -121,10 +129,12 @@ def test_strides_mapped_heads_scale_rows_behind(fmt):
 
 
 @FORMATS
-def test_damage_reaches_those_who_see_it(fmt):
+@pytest.mark.parametrize("wide", [False, True])
+def test_damage_reaches_those_who_see_it(fmt, wide):
     """Lengths that cannot be, pages that are not there, pages with a scale of NaN: eight tokens, of which the first see the page
     that is damaged, and the last do not."""
     rng = np.random.default_rng(5)
+    group = 12 if wide else 1
     lens = [[300], [-1], [1000], [300], [300], [300]]
     c = filled(rng, np.clip(lens, 0, 384), 64, fmt, max_pages=6)
     c.lens[:] = lens
@@ -134,9 +144,9 @@ def test_damage_reaches_those_who_see_it(fmt):
     for s in (3, 4, 5):
         c.table[s, 0, 1] = 10 ** 6
     dev = Device(c)
-    q, q64 = bf16(rng.standard_normal((48, 1, D)))
-    step, cu = step_of(dev, [8] * 6, 1, False)
-    want = orc.cache_window(c, q64, cu, [0], 4, 105)
+    q, q64 = bf16(rng.standard_normal((48, group, D)))
+    step, cu = step_of(dev, [8] * 6, group, False)
+    want = orc.cache_window(c, q64, cu, [0] * group, 4, 105)
     assert np.isnan(want.out[24:28]).all() and np.isfinite(want.out[28:32]).all() and np.isnan(want.out[8:24]).all()
     check(want, *call(dev, step, 4, 105, q.to(DEV)), slice(0, 48), 384, HALF, LIFT)
 
@@ -147,11 +157,12 @@ def test_large_scales_and_queries():
     for size, qsize in ((2.0 ** 40, 2.0 ** -40), (2.0 ** -60, 2.0 ** 60), (1.0, 300.0), (2.0 ** -100, 1.0)):
         c = filled(rng, [[500, 3000]], 128, cache_oracle.E4M3, size=size)
         dev = Device(c)
-        q, q64 = bf16(rng.standard_normal((3, 2, D)) * qsize)
-        step, cu = step_of(dev, [3], 2, False)
-        for window in (100, 2500):
-            want = orc.cache_window(c, q64, cu, [0, 1], 2, window)
-            check(want, *call(dev, step, 2, window, q.to(DEV)), slice(0, 3), 3000, HALF, LIFT)
+        for n in (3, 60):
+            q, q64 = bf16(rng.standard_normal((n, 2, D)) * qsize)
+            step, cu = step_of(dev, [n], 2, False)
+            for window in (100, 2500):
+                want = orc.cache_window(c, q64, cu, [0, 1], 2, window)
+                check(want, *call(dev, step, 2, window, q.to(DEV)), slice(0, n), 3000, HALF, LIFT)
 
 
 @pytest.mark.parametrize("window", [50, 2500])

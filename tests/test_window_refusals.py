@@ -164,7 +164,7 @@ def test_limits():
     for call in shared_calls(cache(), cache(), many):
         assert status(call) == -5
     long = cache(max_pages=4096, n_seq=1)
-    for tokens, fits in ((1 << 12, True), (1 << 19, False)):
+    for tokens, fits in ((1 << 12, True), (1 << 20, False)):
         s = step(n_tokens=2 * tokens, max_tokens=tokens)
         if fits:
             assert S.shplb_cache_attn_shared_workspace_bytes(long, cache(), s) > 0
