@@ -6,7 +6,7 @@ import torch
 import paper_2603_10353_amd as S
 from cache_harness import D, DEV, Device, bf16, filled, step_of, strided
 from oracle import cache_oracle, window_oracle as orc
-from window_harness import check
+from window_harness import check, in_a_large_pool
 
 pytestmark = pytest.mark.gpu
 E4M3, INT8 = cache_oracle.E4M3, cache_oracle.INT8
@@ -196,6 +196,20 @@ def test_offsets_out_of_range():
     for groups in ([0, 2, 4], [3, 1, 2]):
         for left in (0xff, 0x7f, 0x01):
             call(pre, groups, dev, step, q.to(DEV), workspace(pre, dev, step).fill_(left))
+
+
+@pytest.mark.parametrize("n,room", [(4, 0), (30, 0), (80, 4000)], ids=["rows_8", "rows_60", "rows_160_in_128"])
+def test_a_pool_past_32_bits_and_queries_of_nan(n, room):
+    rng = np.random.default_rng(22)
+    prefix = filled(rng, [[700, 300]], 128, cache_oracle.INT8, max_pages=max(room, 6))
+    c = filled(rng, [[9 + 5 * x % 140, 1 + 7 * x % 90] for x in range(n)], 64, cache_oracle.INT8)
+    pre, dev = in_a_large_pool(prefix), in_a_large_pool(c)
+    q, _ = bf16(rng.standard_normal((n, 4, D)))
+    q[2, 1, 77] = np.nan
+    step, cu = step_of(dev, [1] * n, 4, False)
+    want = orc.cache_shared(prefix, [0, n], c, q.double().numpy(), cu, [0, 0, 1, 1])
+    assert np.isnan(want.out[2, 1]).all() and np.isfinite(want.out[2, 0]).all()
+    check(want, *call(pre, [0, n], dev, step, q.to(DEV)), slice(0, n), 900, HALF, LIFT)
 
 
 def test_large_scales_and_queries():

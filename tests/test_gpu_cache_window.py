@@ -6,7 +6,7 @@ import torch
 import paper_2603_10353_amd as S
 from cache_harness import D, DEV, Device, bf16, filled, step_of, strided
 from oracle import cache_oracle, window_oracle as orc
-from window_harness import check
+from window_harness import check, in_a_large_pool
 
 pytestmark = pytest.mark.gpu
 FORMATS = pytest.mark.parametrize("fmt", [cache_oracle.E4M3, cache_oracle.INT8], ids=["e4m3", "int8"])
@@ -163,6 +163,20 @@ def test_large_scales_and_queries():
             for window in (100, 2500):
                 want = orc.cache_window(c, q64, cu, [0, 1], 2, window)
                 check(want, *call(dev, step, 2, window, q.to(DEV)), slice(0, n), 3000, HALF, LIFT)
+
+
+@pytest.mark.parametrize("new", [1, 12, 50])
+def test_a_pool_past_32_bits_and_queries_of_nan(new):
+    rng = np.random.default_rng(21)
+    lens = [[900, 333], [70, 60], [500, 129]]
+    c = filled(rng, lens, 128, cache_oracle.E4M3)
+    dev = in_a_large_pool(c)
+    q, _ = bf16(rng.standard_normal((3 * new, 4, D)))
+    q[new, 1, 77] = np.nan
+    step, cu = step_of(dev, [new] * 3, 4, False)
+    want = orc.cache_window(c, q.double().numpy(), cu, [0, 0, 1, 1], 5, 200)
+    assert np.isnan(want.out[new, 1]).all() and np.isfinite(want.out[new, 0]).all()
+    check(want, *call(dev, step, 5, 200, q.to(DEV)), slice(0, 3 * new), 900, HALF, LIFT)
 
 
 @pytest.mark.parametrize("window", [50, 2500])

@@ -111,6 +111,36 @@ def test_what_is_not_finite_reaches_those_who_see_it(hq):
     check(want, out[:, heads], lse[heads], slice(0, T), T, HALF)
 
 
+def test_rows_so_far_apart_that_offsets_pass_32_bits():
+    rng = np.random.default_rng(13)
+    T, hq, hkv, stride = 300, 2, 1, 2 ** 24 - 8                  # a token every 32 MB
+    (q, q64), (k, k64), (v, v64) = inputs(rng, T, hq, hkv)
+    room = torch.empty((T - 1) * stride + 6 * D, dtype=torch.bfloat16, device=DEV)
+    assert room.numel() * 2 > 2 ** 33
+    at = lambda first, heads: room.as_strided((T, heads, D), (stride, D, 1), first * D)
+    dq, dk, dv, out = at(0, 2), at(2, 1), at(3, 1), at(4, 2)
+    dq.copy_(q), dk.copy_(k), dv.copy_(v)
+    lse = torch.zeros((hq, T), device=DEV)
+    p = S.Problem([0, T], hq, hkv, 128, q_stride_t=stride, q_stride_h=D, kv_stride_t=stride, kv_stride_h=D)
+    S.shplb_window_attn_prefill(p, 3, 100, dq, dk, dv, out, lse, stream())
+    got = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    check(orc.window_attention(q64, k64, v64, [0, T], 3, 100, [0, 0]), *got, slice(0, T), T, HALF)
+
+
+@pytest.mark.parametrize("hq", [1, 8], ids=["few_rows", "many_rows"])
+def test_as_many_sequences_as_there_may_be(hq):
+    """... some of whose queries are NaN, which is nothing to the others."""
+    rng = np.random.default_rng(14)
+    lens = [1 + 37 * x % 130 for x in range(64)]
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    (q, _), (k, k64), (v, v64) = inputs(rng, int(cu[-1]), hq, 1)
+    q[5::41, 0, 9] = np.nan
+    out, lse = call(S.Problem(cu, hq, 1, 64), 2, 50, *up((q,), (k,), (v,)))
+    want = orc.window_attention(q.double().numpy(), k64, v64, cu, 2, 50, [0] * hq)
+    assert np.isnan(want.out[5, 0]).all() and np.isfinite(want.out[6]).all()
+    check(want, out, lse, slice(0, int(cu[-1])), max(lens), HALF)
+
+
 def test_scores_of_every_size():
     """References that rise late and by far, scores far below the first tile's, queries and keys of large numbers."""
     rng = np.random.default_rng(10)

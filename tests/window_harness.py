@@ -1,7 +1,12 @@
-"""What the tests of windows and shared prefixes have in common: the comparison with the oracle."""
+"""What the tests of windows and shared prefixes have in common: the comparison with the oracle, caches of many pages."""
 from __future__ import annotations
 
 import numpy as np
+import torch
+
+import paper_2603_10353_amd as S
+from cache_harness import D, Device
+from oracle import cache_oracle
 
 
 def check(want, got_out, got_lse, rows, keys, half_probability, lift=0.0):
@@ -28,3 +33,18 @@ def check(want, got_out, got_lse, rows, keys, half_probability, lift=0.0):
         fine = np.isfinite(lse)
         assert (np.abs(b[fine] - lse[fine]) <= dz + dp + 2.0 ** -22 * (np.abs(lse[fine]) + 16)).all()
     return worst
+
+
+def in_a_large_pool(c):
+    """The CacheState on the device, its pages at the end of a pool of more than 2^32 bytes."""
+    behind = -(-2 ** 32 // (c.block * D)) + 3
+    dev = Device(c)
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale"):
+        small = getattr(dev, name)
+        large = torch.empty((behind + c.n_pages, *small.shape[1:]), dtype=small.dtype, device=small.device)
+        large[behind:] = small
+        setattr(dev, name, large)
+    dev.table += behind * (dev.table >= 0).int()
+    dev.cache = S.Cache(dev.k_pages, dev.v_pages, dev.k_scale, dev.v_scale, dev.table, dev.lens, dev.n_seq, dev.n_kv_heads, c.block,
+                        dev.max_pages, behind + c.n_pages, S.SHPLB_CACHE_E4M3 if c.fmt == cache_oracle.E4M3 else S.SHPLB_CACHE_INT8)
+    return dev
