@@ -274,10 +274,9 @@ def test_samples_of_a_prompt_token_after_token():
         cache_oracle.append(c, a64, b64, cu)
         got = out.double().cpu().numpy(), lse.double().cpu().numpy()
         check(orc.cache_shared(prefix, [0, n], c, x64, cu, np.arange(hq) // 4), *got, slice(0, n), P + steps, HALF, LIFT)
-        other = torch.cuda.Stream()
+        other, again, again_lse, mine = torch.cuda.Stream(), torch.zeros_like(q), torch.zeros_like(lse), workspace(pre, dev, step)
         other.wait_stream(stream())
-        again, again_lse = torch.zeros_like(q), torch.zeros_like(lse)
-        S.shplb_cache_attn_shared(pre.cache, groups, dev.cache, step, q, again, again_lse, workspace(pre, dev, step), other)
+        S.shplb_cache_attn_shared(pre.cache, groups, dev.cache, step, q, again, again_lse, mine, other)
         torch.cuda.synchronize()
         assert (again == out).all() and (again_lse == lse).all()
     dev.check_same(c)

@@ -195,9 +195,9 @@ def test_graph_of_a_step_streams_and_workspaces(window):
         S.shplb_cache_attn_window(dev.cache, step, 4, window, q, out, lse, ws[0], stream())
     side = torch.cuda.Stream()
     for x in range(4):
+        other, other_lse = torch.zeros_like(q), torch.zeros((4, 2), device=DEV)
         side.wait_stream(torch.cuda.current_stream())
         graph.replay()
-        other, other_lse = torch.zeros_like(q), torch.zeros((4, 2), device=DEV)
         S.shplb_cache_attn_window(dev.cache, step, 4, window, q, other, other_lse, ws[1], side)
         torch.cuda.synchronize()
         want, want_lse = call(dev, step, 4, window, q, ws[1])
