@@ -66,7 +66,7 @@ extern "C" {
 #define SHPLB_OK              0
 #define SHPLB_E_NULL        (-1)  /* a required pointer is NULL */
 #define SHPLB_E_SHAPE       (-2)  /* bad shape, stride, alignment or cu_seqlens */
-#define SHPLB_E_BUDGET      (-3)  /* negative budget, or partition cannot hold the units */
+#define SHPLB_E_BUDGET      (-3)  /* negative budget, window below 1, or partition cannot hold the units */
 #define SHPLB_E_WORKSPACE   (-4)  /* the problem needs more scratch than shplb_sparse_attn_prefill_static has */
 #define SHPLB_E_UNSUPPORTED (-5)  /* head_dim != 128, block not 64/128, too many sequences/blocks/heads */
 #define SHPLB_E_HIP         (-6)  /* a HIP call or kernel launch failed */
@@ -428,8 +428,8 @@ SHPLB_API int32_t shplb_cache_attn_window(const shplb_cache* cache, const shplb_
 /* Attention of the step's queries of sequences that share prefixes (a system prompt, samples of one prompt):
  * sequences cu_prefix[g] .. cu_prefix[g+1]-1 of `cache` come behind sequence g of `prefix`.  A query sees all
  * tokens of its prefix (of its KV head there) and, of its own sequence, what it sees in shplb_cache_attn; one of a sequence
- * that is in no such run has no prefix.  A prefix is read once for every 128 rows that it has, not once for every
- * sequence as with a table in which its pages stand.
+ * that is in no such run has no prefix.  A prefix is read once for every 128 rows that it has (16 or 32 in smaller calls), not once for
+ * every sequence as with a table in which its pages stand.
  *   prefix: a cache of one sequence for each prefix, with as many KV heads and of the same format; its pages may
  *     be of another pool and block, and its heads of different lengths.
  *   cu_prefix: device int32 [prefix->n_seq+1], not decreasing; offsets outside 0 .. cache->n_seq are taken as those.
@@ -437,8 +437,8 @@ SHPLB_API int32_t shplb_cache_attn_window(const shplb_cache* cache, const shplb_
  *   - A damaged length or page of a prefix makes NaN of what all its rows get, as one of a sequence does for its own.
  *   - Otherwise as shplb_cache_attn: numerics, errors, arguments, queries that see no token (now: neither of their prefix nor of their
  *     own).  Softmax is over prefix and own tokens together, and so is lse_out.  No weights.
- *   workspace: device, shplb_cache_attn_shared_workspace_bytes(), 256-byte aligned; needs no clearing;
- *     must not be shared with a call in flight on another stream.
+ *   workspace: device, shplb_cache_attn_shared_workspace_bytes() (of these caches and this step or one with at least as many n_tokens
+ *     and max_tokens and the same heads), 256-byte aligned; needs no clearing; must not be shared with a call in flight on another stream.
  * Errors: also SHPLB_E_SHAPE (another number of KV heads or format); SHPLB_E_UNSUPPORTED for more than 2^24 rows of a KV head in all, or the limits on tiles
  * and units of shplb_cache_attn, for prefixes with all rows of the step together. */
 SHPLB_API int32_t shplb_cache_attn_shared_workspace_bytes(const shplb_cache* prefix, const shplb_cache* cache,

@@ -7,7 +7,10 @@ namespace shplb {
 namespace {
 
 // ---- windows.  A step's work does not grow with the context: a head has the units of its window and of its first tokens, and how the
-// work is divided follows from them like that of cache_attn_kernel.hip from a table's room.
+// work is divided follows from them like that of cache_attn_kernel.hip from a table's room.  Bound by reading with few rows (128 sequences
+// x 8 heads, a window of 4096: 148 us, 5.7 TB/s of what is seen), by VALU work with many (codes to fp16 for every 32 rows: 8 sequences x 32 tokens x 28/4
+// int8 heads, a window of 2000: 36 us).  128 rows at a time, as prefixes below have them, are 40 there, and 15 to 70% slower in smaller
+// calls: windows are short, and an item of 128 rows has too few of their units to pay for its beginning.
 template <int FMT>
 int32_t launch_window(const CacheAttnArgs& a, int rows, int most_rows, int compute_units, hipStream_t stream) {
   const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2), pairs = a.c.n_seq * a.c.n_kv_heads;
@@ -26,7 +29,9 @@ int32_t launch_window(const CacheAttnArgs& a, int rows, int most_rows, int compu
 }
 
 // ---- shared prefixes.  The rows of all sequences that share a prefix are rows of one item: its keys are read once for many of them.
-// One launch attends to the prefixes and to the sequences' own tokens, either divided like the cache of cache_attn_kernel.hip; all results are partial ones, which a second launch joins.
+// Prefixes and own tokens are attended to in one launch or two, either divided like the cache of cache_attn_kernel.hip; all results are
+// partial ones, which a last launch joins.  Prefixes are bound by the products and what feeds them (of 128 rows x 8 heads x 32768 tokens
+// the units take 65 us, 1.05 PFLOP/s, and 22 go to beginnings, results and the last shares' wait), own tokens by reading.
 
 // Rows of a prefix's item.  Up to 48 of them are worked on like those of a cache, 16 or 32 at a time: codes come from memory
 // into registers, and are turned to fp16 for each tile by itself.  More rows: 128 at a time, 32 of each wave, whose workgroup turns the
@@ -435,7 +440,8 @@ __global__ __launch_bounds__(join_threads(THREADS)) void shared_join_kernel(Cach
     place(x, o, ml);
     return *reinterpret_cast<const f32x4*>(o + d4 * 4);
   };
-  constexpr int kEarly = kShared ? 4 : 8;
+  // (a wave that has a row for itself asks for 32 pieces at once: prefixes of 8192 tokens that 64 sequences share, 20 pieces a row, 73 us, 76 with sixteen)
+  constexpr int kEarly = kShared ? 4 : 16;
   f32x4 early[kEarly];
 #pragma unroll
   for (int x = 0; x < kEarly; ++x) early[x] = part + kParts * x < pieces ? values(part + kParts * x) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};

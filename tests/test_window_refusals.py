@@ -177,3 +177,13 @@ def test_nothing_to_do():
     s = step(n_tokens=0, max_tokens=0)
     S.shplb_cache_attn_window(cache(), s, 0, 1, None, None, None, None)
     S.shplb_cache_attn_shared(cache(), None, cache(), s, None, None, None, None)
+
+
+def test_a_workspace_for_more_tokens_does_for_fewer():
+    sizes = []
+    for n in (1, 2, 3, 5, 8, 9, 16, 17, 33, 60, 100, 257, 600):
+        s = step(n_tokens=2 * n, max_tokens=n)
+        sizes.append((S.shplb_cache_attn_window_workspace_bytes(cache(), s, 4, 100),
+                      *(S.shplb_cache_attn_shared_workspace_bytes(cache(max_pages=m), cache(), s) for m in (1, 100, 4096))))
+    for a, b in zip(sizes, sizes[1:]):
+        assert all(x <= y for x, y in zip(a, b))
