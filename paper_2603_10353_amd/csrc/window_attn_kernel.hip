@@ -87,16 +87,15 @@ __device__ __forceinline__ const char* uniform(const char* p) {
                                        uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32)))) << 32);
 }
 
-// QG: groups of 16 queries of a wave.
-template <int QG>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_attn_kernel(WindowArgs a) {
+// One item; whether a sum came out that is not finite.  CAREFUL: values that are not finite are told apart from zeros by what sees them.
+// lds: two stages of K, two of V; s_bad: -1.
+template <int QG, bool CAREFUL>
+__device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowItem& it, char* lds, int& s_bad) {
   constexpr int BQ = 64 * QG, MT = kKeys / 16, kQK = 4 * MT, kPV = 8 * (kKeys / 32);
   constexpr int kLook = 8;                   // LDS operands are fetched so far ahead
   // a lane's 16 probabilities of a query and tile can only sum to more if one of them exceeds 2^8
   constexpr float kSumLimit = 4.0f * MT * 256.0f;
 
-  __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];         // two stages of K, two of V
-  __shared__ int s_bad;                      // the last step whose values are not all finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, hi = lane >> 4, q_wave = 16 * QG * wave;
   const int64_t row_bytes = a.st.kv_t * 2;
@@ -109,11 +108,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int tr_row = 4 * hi + ((lane >> 2) & 3), tr_a = lane & 3;
   const int v_rd0 = tr_row * kRowBytes + (((tr_a >> 1) ^ swz(tr_row)) << 4) + 8 * (tr_a & 1);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_offset_of(lds) + 4 * wave * kRowBytes);
-  if (tid == 0) s_bad = -1;
-
-  const int in_lap = int(uint32_t(blockIdx.x) % uint32_t(a.lap)), place = int(blockIdx.x) - in_lap + in_lap % kXcds * (a.lap / kXcds) + in_lap / kXcds;
-  if (place >= a.items) return;
-  const WindowItem it = window_item<BQ>(a, place);
 
   const auto copy_tile = [&](const uint16_t* base, int u, uint32_t dst) {
     const int at = min(it.key0(u), it.len - 1), last = it.len - 1 - at;
@@ -225,13 +219,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
   for (int qg = 0; qg < QG; ++qg) asm volatile("" : "+v"(qf[qg][0]), "+v"(qf[qg][1]), "+v"(qf[qg][2]), "+v"(qf[qg][3]));
   __syncthreads();
-  if (!hidden(it.key0(0))) scores(lds, it.key0(0));
+  if (!CAREFUL || !hidden(it.key0(0))) scores(lds, it.key0(0));
 
-  // One tile.  plain: all queries see all of it, and it is not the last one.
+  // One tile.  plain: it is not the last one, and (CAREFUL) all queries see all of it.
   const auto step = [&](auto plain_c) __attribute__((always_inline)) {
     constexpr bool kPlain = decltype(plain_c)::value;
     const int key0 = it.key0(u), key1 = it.key0(u + 1);
-    const bool ends = !kPlain && u + 1 == it.tiles, mine = kPlain || !hidden(key0), checked = !kPlain && masked(key0, first, last);
+    const bool ends = !kPlain && u + 1 == it.tiles, mine = kPlain || !hidden(key0), checked = CAREFUL && !kPlain && masked(key0, first, last);
     const int stage = u & 1;
     const char* const vt = lds + (2 + stage) * kTileBytes;
     const char* const kt = lds + (stage ^ 1) * kTileBytes;
@@ -389,7 +383,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     ++u;
   };
-  const auto plain = [&]() { return u + 1 < it.tiles && !masked(it.key0(u), first, last); };
+  const auto plain = [&]() { return u + 1 < it.tiles && (!CAREFUL || !masked(it.key0(u), first, last)); };
 #pragma unroll 1
   while (u < it.tiles) {
 #pragma unroll 1
@@ -397,6 +391,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     step(std::false_type{});               // (the last tile is never plain)
   }
   __builtin_amdgcn_s_setprio(0);
+  float odd = 0.0f;                          // NaN if there is such a sum
+  if constexpr (!CAREFUL) {
+#pragma unroll
+    for (int x = 0; x < 32 * QG; ++x) odd = __builtin_fmaf(acc[x >> 5][x >> 2 & 7][x & 3], 0.0f, odd);
+  }
 
   // ---- out: a lane has dims 16 dt + 4 hi + r of its queries; neighbours trade, and a lane stores eight dims at a time
   const int n_valid = it.len - it.q0;
@@ -418,6 +417,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       if (valid) *reinterpret_cast<u32x4*>(dst + 32 * p) = u32x4{e0, e1, o0, o1};
     }
   }
+  return __ballot(odd != 0.0f) != 0;
+}
+
+// QG: groups of 16 queries of a wave.
+template <int QG>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_attn_kernel(WindowArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
+  __shared__ int s_bad, s_odd;               // the last step whose values are not all finite; whether some sum is not
+  if (threadIdx.x == 0) {
+    s_bad = -1;
+    s_odd = 0;
+  }
+  const int in_lap = int(uint32_t(blockIdx.x) % uint32_t(a.lap)), place = int(blockIdx.x) - in_lap + in_lap % kXcds * (a.lap / kXcds) + in_lap / kXcds;
+  if (place >= a.items) return;
+  const WindowItem it = window_item<64 * QG>(a, place);
+  if (attend_item<QG, false>(a, it, lds, s_bad) && threadIdx.x % 64 == 0) s_odd = 1;
+  __syncthreads();
+  if (s_odd != 0) attend_item<QG, true>(a, it, lds, s_bad);      // (and writes the outputs again)
 }
 
 }  // namespace
