@@ -195,17 +195,23 @@ __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowIte
     }
   };
   const auto mask_scores = [&](int key0) {
+    const auto mask = [&](auto sinks_c) {
 #pragma unroll
-    for (int qg = 0; qg < QG; ++qg) {
-      int back = q_pos[qg] - key0 - 4 * hi, left = a.n_sink - key0 - 4 * hi;         // how far back a key lies; first tokens from it on
-      asm volatile("" : "+v"(back), "+v"(left));
+      for (int qg = 0; qg < QG; ++qg) {
+        int back = q_pos[qg] - key0 - 4 * hi, left = a.n_sink - key0 - 4 * hi;       // how far back a key lies; first tokens from it on
+        asm volatile("" : "+v"(back), "+v"(left));
 #pragma unroll
-      for (int x = 0; x < 4 * MT; ++x) {
-        const int at = 16 * (x >> 2) + (x & 3);
-        sc[qg][x >> 2][x & 3] = (uint32_t(back - at) < uint32_t(a.window)) | ((back >= at) & (left > at)) ? sc[qg][x >> 2][x & 3] : -INFINITY;
-        if ((x & 3) == 3) asm volatile("" : "+v"(sc[qg][x >> 2]));
+        for (int x = 0; x < 4 * MT; ++x) {
+          const int at = 16 * (x >> 2) + (x & 3);
+          bool sees = uint32_t(back - at) < uint32_t(a.window);
+          if constexpr (decltype(sinks_c)::value) sees = sees | ((back >= at) & (left > at));
+          sc[qg][x >> 2][x & 3] = sees ? sc[qg][x >> 2][x & 3] : -INFINITY;
+          if ((x & 3) == 3) asm volatile("" : "+v"(sc[qg][x >> 2]));
+        }
       }
-    }
+    };
+    if (key0 < a.n_sink) mask(std::true_type{});
+    else mask(std::false_type{});
   };
   const auto scores = [&](const char* kt, int key0) {
     Operands kf;
