@@ -111,6 +111,18 @@ def test_what_is_not_finite_reaches_those_who_see_it(hq):
     check(want, out[:, heads], lse[heads], slice(0, T), T, HALF)
 
 
+@pytest.mark.parametrize("T,window", [(2, 1), (5, 2), (65, 3), (130, 64), (260, 100)])
+def test_what_is_not_finite_in_short_sequences(T, window):
+    """... beside one without: the first token, hidden from all but a few, the last one, which nobody else sees, and one in between."""
+    rng = np.random.default_rng([15, T])
+    (q, q64), (k, k64), (v, _) = inputs(rng, 2 * T, 2, 1)
+    v[0, 0, 3], v[T - 1, 0, 4], v[T // 2, 0, 100] = np.nan, np.inf, -np.inf
+    out, lse = call(S.Problem([0, T, 2 * T], 2, 1, 128), 0, window, *up((q,), (k,), (v,)))
+    want = orc.window_attention(q64, k64, v.double().numpy(), [0, T, 2 * T], 0, window, [0, 0])
+    assert np.isfinite(want.out[T:]).all() and np.isnan(want.out[0, :, 3]).all() and np.isfinite(want.out[:T - 1, :, 4]).all()
+    check(want, out, lse, slice(0, 2 * T), T, HALF)
+
+
 def test_rows_so_far_apart_that_offsets_pass_32_bits():
     rng = np.random.default_rng(13)
     T, hq, hkv, stride = 300, 2, 1, 2 ** 24 - 8                  # a token every 32 MB
