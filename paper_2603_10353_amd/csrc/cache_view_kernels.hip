@@ -9,17 +9,23 @@ namespace {
 // ---- windows.  A step's work does not grow with the context: a head has the units of its window and of its first tokens, and how the
 // work is divided follows from them like that of cache_attn_kernel.hip from a table's room.  Bound by reading with few rows (128 sequences
 // x 8 heads, a window of 4096: 148 us, 5.7 TB/s of what is seen), by VALU work with many (codes to fp16 for every 32 rows: 8 sequences x 32 tokens x 28/4
-// int8 heads, a window of 2000: 36 us).  128 rows at a time, as prefixes below have them, are 40 there, and 15 to 70% slower in smaller
+// int8 heads, a window of 2000: 31 us).  128 rows at a time, as prefixes below have them, are 40 there, and 15 to 70% slower in smaller
 // calls: windows are short, and an item of 128 rows has too few of their units to pay for its beginning.
 template <int FMT>
 int32_t launch_window(const CacheAttnArgs& a, int rows, int most_rows, int compute_units, hipStream_t stream) {
   const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2), pairs = a.c.n_seq * a.c.n_kv_heads;
   const int64_t most = min(int64_t(a.c.max_pages) << a.c.block_log2, int64_t(a.view.most_units) * kUnit);
   constexpr int kShort = kWholeWaves * kWholeUnits * kUnit;
+  // More rows: a workgroup a tile of them, without shares and joining, where a tile's chain of units costs less than that: always up to 2048 tokens; up to
+  // 2560 from a tile for every other compute unit on (a window of 2000, 32 new tokens of a sequence: 256 tiles 28 us, 39 in shares, 128 24 and 26, 32 of
+  // them 23 and 20); up to 4608 from two for every compute unit on (a window of 4000: 512 tiles 84 and 92, 1024 160 and 174; 256 46 and 57, but 38 and 34
+  // if lengths are from 100 on); beyond, shares (of 8000: 512 tiles 165 and 169, 320 128 and 110).
+  const int64_t items = int64_t(pairs) * a.tiles;
+  const bool whole_tiles = most <= kShort || (most <= kShort * 5 / 4 && items >= compute_units / 2) || (most <= kShort * 9 / 4 && items >= 2 * compute_units);
   if (rows == 16 && pairs <= 2 * compute_units && most <= kShort) {
     cache_whole_kernel<false, FMT, kWindow><<<pairs, 64 * kWholeWaves, 0, stream>>>(a);
-  } else if (rows > 16 && (most <= kShort || (most <= 2 * kShort && int64_t(pairs) * a.tiles >= 2 * compute_units))) {
-    cache_attn_kernel<2, kWaves, true, FMT, kWindow><<<uint32_t(pairs) * a.tiles, kThreads, 0, stream>>>(a, 0);
+  } else if (rows > 16 && whole_tiles) {
+    cache_attn_kernel<2, kWaves, true, FMT, kWindow><<<uint32_t(items), kThreads, 0, stream>>>(a, 0);
   } else {
     if (rows == 16) cache_attn_kernel<1, 1, false, FMT, kWindow><<<grid, kThreads, 0, stream>>>(a, 3);
     else cache_attn_kernel<2, kWaves, false, FMT, kWindow><<<grid, kThreads, 0, stream>>>(a, kWaves);
