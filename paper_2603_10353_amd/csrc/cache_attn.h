@@ -682,7 +682,7 @@ struct AttnLds {
 // for short caches.  PARTS: results are partial ones in any case, for a join with others.
 template <int NT, int WAVES, bool ITEMS, int FMT, int VIEW = kAll, bool PARTS = false>
 __device__ __forceinline__ void attend_shares(const CacheAttnArgs& a, int least, int block, int blocks, AttnLds<NT, WAVES>& lds) {
-  static_assert((VIEW != kGroups || PARTS) && !(PARTS && ITEMS), "a row of a group has tokens of its own, too");
+  static_assert(VIEW != kGroups || (PARTS && !ITEMS), "a row of a group has tokens of its own, too");
   constexpr bool kOwn = WAVES == 1;
   constexpr int kRows = 16 * NT, kStart = start_units(WAVES);
   static_assert(kOwn || WAVES == kWaves, "one, or all of a workgroup");
@@ -834,7 +834,10 @@ __device__ __forceinline__ void attend_shares(const CacheAttnArgs& a, int least,
       }
       __syncthreads();
     }
-    if (ITEMS) break;
+    if (ITEMS) {
+      if (PARTS && tid == 0) *reinterpret_cast<int2*>(a.begun + 2 * (int64_t(pair) * a.tiles + it.tile)) = int2{0, 0};       // whole
+      break;
+    }
     // for the joining kernel: pieces of the item, if it ends in another share
     if (VIEW == kGroups) {
       if (u0 == 0) note_rows(a, row0, n, h, group, first_row, kRows, kOwn ? tid & 63 : tid, worker, whole ? 0 : shares.of(at - it.unit + units - 1) - worker + 1);

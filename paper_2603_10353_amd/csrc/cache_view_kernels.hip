@@ -551,6 +551,10 @@ int32_t launch_cache_attn_shared(const CacheAttnArgs& own, const CacheAttnArgs& 
   const auto launch_own = [&](auto fmt_c) {
     constexpr int FMT = decltype(fmt_c)::value;
     if (rows == 16) cache_attn_kernel<1, 1, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(own, 3);
+    // (a workgroup a tile of rows where tables have room for 1024 tokens: 64 sequences x 5 new tokens, up to 700 held, behind 8000 91 us, 98 in shares; 16
+    // with room for 2048 57 and 54)
+    else if (int64_t(own.c.max_pages) << own.c.block_log2 <= kWholeWaves * kWholeUnits * kUnit / 2)
+      cache_attn_kernel<2, kWaves, true, FMT, kAll, true><<<uint32_t(own.c.n_seq * own.c.n_kv_heads) * own.tiles, kThreads, 0, stream>>>(own, 0);
     else cache_attn_kernel<2, kWaves, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(own, kWaves);
   };
   const auto launch = [&](auto fmt_c) {
