@@ -392,6 +392,18 @@ __global__ __launch_bounds__(kThreads, 2) void shared_attn_kernel(CacheAttnArgs 
   else attend_rows<OWN, FMT, kAll>(a, block, blocks, lds.own);
 }
 
+// Prefixes 128 rows at a time, and behind them, where a workgroup has ended, own tokens of drafts: neither waits for the other's last shares.
+template <int FMT>
+__global__ __launch_bounds__(kThreads, 2) void shared_wide_kernel(CacheAttnArgs a, CacheAttnArgs pre) {
+  __shared__ __attribute__((aligned(1024))) union Lds {
+    AttnLds<2, kWaves> own;
+    PrefixLds pre;
+  } lds;
+  const int b = int(blockIdx.x), blocks = int(gridDim.x) / 2;
+  if (b < blocks) prefix_shares<FMT>(pre, 4, b, blocks, lds.pre);
+  else attend_rows<32, FMT, kAll>(a, b - blocks, blocks, lds.own);
+}
+
 // Joins a row's pieces, those of its prefix and those of its own tokens: with M the largest m, out = sum 2^(m - M) O / sum 2^(m -
 // M) l.  A workgroup a row (y) of an item (x) of own tokens, or, where there are many, a wave (THREADS = 64, four of them in a
 // workgroup); groups of 32 lanes take turns at the pieces, a lane four dims, and what they have is added up in order.  Where the
@@ -548,18 +560,24 @@ int32_t launch_cache_attn_shared(const CacheAttnArgs& own, const CacheAttnArgs& 
   const auto units = [](const CacheAttnArgs& a, int64_t tiles) { return a.c.n_kv_heads * tiles * (((int64_t(a.c.max_pages) << a.c.block_log2) + kUnit - 1) / kUnit); };
   const int64_t most_heads = own.t.max_tokens > 0 ? most_rows / own.t.max_tokens : 1;
   const bool apart = units(pre, int64_t(own.t.n_tokens) * most_heads / rows_pre + pre.c.n_seq) + units(own, int64_t(own.c.n_seq) * own.tiles) >= 16384;
+  // Own tokens of more than 16 rows: a workgroup a tile of rows where tables have room for 1024 tokens (64 sequences x 5 new tokens, up to 700 held, behind
+  // 8000 91 us, 98 in shares; 16 with room for 2048 57 and 54); else, behind prefixes of 128 rows, in one launch with these (64 with room for 2048 97 us,
+  // 101 in two, 32 of them 62 and 71; with up to 16 rows, one token each, 75 and 73).
+  const bool own_items = rows > 16 && int64_t(own.c.max_pages) << own.c.block_log2 <= kWholeWaves * kWholeUnits * kUnit / 2;
   const auto launch_own = [&](auto fmt_c) {
     constexpr int FMT = decltype(fmt_c)::value;
     if (rows == 16) cache_attn_kernel<1, 1, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(own, 3);
-    // (a workgroup a tile of rows where tables have room for 1024 tokens: 64 sequences x 5 new tokens, up to 700 held, behind 8000 91 us, 98 in shares; 16
-    // with room for 2048 57 and 54)
-    else if (int64_t(own.c.max_pages) << own.c.block_log2 <= kWholeWaves * kWholeUnits * kUnit / 2)
+    else if (own_items)
       cache_attn_kernel<2, kWaves, true, FMT, kAll, true><<<uint32_t(own.c.n_seq * own.c.n_kv_heads) * own.tiles, kThreads, 0, stream>>>(own, 0);
     else cache_attn_kernel<2, kWaves, false, FMT, kAll, true><<<grid, kThreads, 0, stream>>>(own, kWaves);
   };
   const auto launch = [&](auto fmt_c) {
     constexpr int FMT = decltype(fmt_c)::value;
     if (rows_pre == kPrefixRows) {
+      if (rows > 16 && !own_items) {
+        shared_wide_kernel<FMT><<<2 * grid, kThreads, 0, stream>>>(own, pre);
+        return;
+      }
       prefix_kernel<FMT><<<grid, kThreads, 0, stream>>>(pre);
       launch_own(std::integral_constant<int, FMT>{});
     } else if (apart) {

@@ -87,6 +87,9 @@ ROOMY = {  # ..., pages that tables have room for: of the prefixes, of the own t
     "rows_128_pieces": ([[200]], [0, 2], [[64], [150]], [64, 100], 4, 1, 4096, 4),
     "rows_16": ([[100, 30]] * 30, [2 * x for x in range(31)], [[30, 200]] * 62, [1] * 62, 8, 2, 600, 100),
     "rows_32": ([[100, 30]] * 10, [7 * x for x in range(11)], [[30, 200]] * 70, [1] * 70, 8, 2, 1500, 5),
+    "rows_128_drafts": ([[300, 200], [64, 700]], [1, 9, 20], [[30, 200], [0, 5], [500, 64], [129, 3]] * 6, [5, 6, 7, 2] * 6, 8, 2, 4000, 30),
+    "rows_128_drafts_of_many": ([[130]] * 20, [5 * x for x in range(21)], [[20], [90]] * 60, [20] * 120, 4, 1, 4000, 1100),
+    "rows_128_drafts_in_little": ([[300, 200]], [0, 40], [[30, 200], [0, 5], [250, 64], [129, 3]] * 11, [6, 5, 7, 0] * 11, 8, 2, 4000, 4),
     "rows_32_own_too": ([[100, 30]] * 5, [2 * x for x in range(6)], [[30, 200]] * 10, [5] * 10, 8, 2, 1500, 1500),
 }
 
