@@ -9,7 +9,7 @@ namespace {
 // ---- windows.  A step's work does not grow with the context: a head has the units of its window and of its first tokens, and how the
 // work is divided follows from them like that of cache_attn_kernel.hip from a table's room.  Bound by reading with few rows (128 sequences
 // x 8 heads, a window of 4096: 148 us, 5.7 TB/s of what is seen), by VALU work with many (codes to fp16 for every 32 rows: 8 sequences x 32 tokens x 28/4
-// int8 heads, a window of 2000: 31 us).  128 rows at a time, as prefixes below have them, are 40 there, and 15 to 70% slower in smaller
+// int8 heads, a window of 2000: 28 to 30 us).  128 rows at a time, as prefixes below have them, are 40 there, and 15 to 70% slower in smaller
 // calls: windows are short, and an item of 128 rows has too few of their units to pay for its beginning.
 template <int FMT>
 int32_t launch_window(const CacheAttnArgs& a, int rows, int most_rows, int compute_units, hipStream_t stream) {
