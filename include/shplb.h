@@ -233,7 +233,8 @@ SHPLB_API int32_t shplb_sparse_attn_prefill_split(const shplb_problem* p, const 
  *   - bf16 products, sums in fp32; probabilities are rounded to bf16 before they meet the values, not
  *     before they are added up.  Results are bit-identical from run to run; in calls of at most as many
  *     rows (of 128 queries) as there are compute units a sum may be taken in another order than in larger ones.
- *   - A key or value that is infinite or NaN reaches the tokens that see it, and no others.
+ *   - A key or value that is infinite or NaN reaches the tokens that see it, and no others.  (Where there are such values, rows near
+ *     them are worked on twice.)
  *   q, k, v: device bf16; out: device bf16, strides as Q, in other memory than q, k and v;
  *   lse_out: device fp32 [n_q_heads, T], natural logarithm of the softmax denominators, or NULL.
  * Errors: SHPLB_E_NULL, SHPLB_E_SHAPE, SHPLB_E_UNSUPPORTED as above; SHPLB_E_BUDGET (window < 1 or n_sink < 0). */

@@ -62,19 +62,22 @@ template <int BQ>
 __device__ __forceinline__ WindowItem window_item(const WindowArgs& a, int place) {
   WindowItem it;
   const auto scalar = [](int x) { return int(__builtin_amdgcn_readfirstlane(x)); };
-  int s = 0;
+  int t0 = 0, t1 = a.tile_begin[1];
+  it.seq_begin = a.tok_begin[0];
+  it.len = a.len[0];
   if (a.n_seq > 1) {
-    const int lane = threadIdx.x & 63;
-    s = __builtin_popcountll(__ballot(lane < a.n_seq - 1 && place >= a.tile_begin[lane + 1] * a.n_q_heads));
+    const int lane = threadIdx.x & 63, s = __builtin_popcountll(__ballot(lane < a.n_seq - 1 && place >= a.tile_begin[lane + 1] * a.n_q_heads));
+    t0 = scalar(a.tile_begin[s]);
+    t1 = scalar(a.tile_begin[s + 1]);
+    it.seq_begin = scalar(a.tok_begin[s]);
+    it.len = scalar(a.len[s]);
   }
-  const int t0 = scalar(a.tile_begin[s]), nt = scalar(a.tile_begin[s + 1]) - t0, local = place - t0 * a.n_q_heads;
+  const int nt = t1 - t0, local = place - t0 * a.n_q_heads;
   const int group = a.group > 0 ? a.group : 1;
   const int run = scalar(uint32_t(local) / uint32_t(nt * group)), rest = local - run * nt * group;     // heads that share keys, tile by tile
   const int nth = scalar(uint32_t(rest) / uint32_t(group)), tile = nt - 1 - nth;
   it.head = run * group + rest - nth * group;
   it.kv_head = a.group > 0 ? run : scalar(int(a.kv_of[it.head >> 2] >> (8 * (it.head & 3)) & 0xff));
-  it.seq_begin = scalar(a.tok_begin[s]);
-  it.len = scalar(a.len[s]);
   it.q0 = tile * BQ;
   const int hi = min(it.q0 + BQ, it.len), lo = max(it.q0 - a.window + 1, 0);
   const int end = (hi + kKeys - 1) / kKeys, first = lo / kKeys;
