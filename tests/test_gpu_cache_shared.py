@@ -201,6 +201,33 @@ def test_offsets_out_of_range():
             call(pre, groups, dev, step, q.to(DEV), workspace(pre, dev, step).fill_(left))
 
 
+@FORMATS
+@pytest.mark.parametrize("new,room", [(1, 4), (6, 4), (6, 40)], ids=["tokens", "drafts_in_little", "drafts"])
+def test_damage_where_128_rows_are_taken_together(fmt, new, room):
+    rng = np.random.default_rng(16)
+    plens = [[300], [-1], [10 ** 6], [300], [300], [300]]
+    prefix = filled(rng, np.where(np.array(plens) == 300, 300, 0), 64, fmt, max_pages=4000)
+    prefix.lens[:] = plens
+    prefix.table[3, 0, 2] = -1
+    prefix.k_scale[prefix.table[4, 0, 0]] = np.nan
+    prefix.v_scale[prefix.table[5, 0, 4]] = np.nan
+    n = 6 * 25 + 1
+    c = filled(rng, [[70]] * n, 64, fmt, max_pages=room)
+    c.lens[0, 0], c.lens[1, 0] = -5, 64 * room + 1
+    c.table[24, 0, 1] = 10 ** 6
+    pre, dev = Device(prefix), Device(c)
+    q, q64 = bf16(rng.standard_normal((new * n, 4, D)))
+    step, cu = step_of(dev, [new] * n, 4, False)
+    groups = [25 * x for x in range(7)]
+    want = orc.cache_shared(prefix, groups, c, q64, cu, [0] * 4)
+    assert np.isfinite(want.out[-1]).all() and np.isfinite(want.out[2 * new]).all() and np.isnan(want.out[25 * new:150 * new]).any(-1).all()
+    check(want, *call(pre, groups, dev, step, q.to(DEV)), slice(0, new * n), 400, HALF, LIFT)
+    cut = torch.from_numpy(rng.integers(-9, new * n + 9, n + 1).astype(np.int32)).to(DEV)    # offsets in no order: nothing outside is read or written
+    step = S.Step(n, 4, 1, new * n, 2 * new, cut)
+    for left in (0xff, 0x7f, 0x01):
+        call(pre, groups[::-1] if left == 1 else groups, dev, step, q.to(DEV), workspace(pre, dev, step).fill_(left))
+
+
 @pytest.mark.parametrize("n,room", [(4, 0), (30, 0), (80, 4000)], ids=["rows_8", "rows_60", "rows_160_in_128"])
 def test_a_pool_past_32_bits_and_queries_of_nan(n, room):
     rng = np.random.default_rng(22)
