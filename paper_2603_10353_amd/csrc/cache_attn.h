@@ -30,11 +30,12 @@
 // 6 to join; a sequence of 777 tokens 10 us, of which the launch and three reads that wait for one another are eight.
 #pragma once
 #include "cache_common.h"
+#include "cache_span.h"
 
 namespace shplb {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kUnit = 64;
+constexpr int kThreads = 256, kWaves = 4;
 // What beginning with an item costs, in units of the list of all units (where it is that many empty ones in front of the item's own):
 // the queries, the first keys, the results, all of them waited for.  A wave by itself: for a batch of 128 sequences x 8 heads of lengths
 // between 100 and 16000, where it has one to five items, 102 us without, 97 with two, 100 with five.  Four waves together, which
@@ -48,8 +49,7 @@ constexpr int kLdsRow = kHeadDim + 4;          // floats of a row in LDS: rows f
 // What rows see.
 //  - kAll: their head's tokens up to their own.
 //  - kWindow: of those the last `window` and the first n_sink.  A tile of rows goes through the units that any of its rows
-//    sees: those of the first tokens, then those of the windows (unit u of the tile is unit u of the head below `sinks`, u + skip
-//    from there on).  As many units are reckoned with for every tile as one has at most.
+//    sees: those of the first tokens, then those of the windows (cache_span.h).  As many units are reckoned with for every tile as one has at most.
 //  - kGroups: all of the tokens of a cache whose sequence s is shared by the rows of the step's sequences groups[s] ..
 //    groups[s + 1] - 1.
 enum { kAll, kWindow, kGroups };
@@ -121,26 +121,10 @@ __device__ __forceinline__ void pair_units(const CacheAttnArgs& a, int rows, int
 }
 
 // What the rows first_row .. first_row + ROWS - 1 of n tokens see with windows.
-struct Span {
-  int sinks, skip, count;                      // of units, see above
-  int low_first, low_last;                     // where the windows of the first and of the last row begin
-  __device__ __forceinline__ int unit(int u) const { return u < sinks ? u : u + skip; }
-};
 template <int VIEW, int ROWS>
 __device__ __forceinline__ Span span_of(const CacheAttnArgs& a, int first_row, int n, int group, int len) {
-  if constexpr (VIEW != kWindow) {
-    return {};
-  } else {
-    const int before = len - n + 1, first = first_row / group, last = (min(first_row + ROWS, n * group) - 1) / group;
-    Span x;
-    x.low_first = before + first - a.view.window;
-    x.low_last = before + last - a.view.window;
-    const int hi = max(before + last, 0), end = (hi + kUnit - 1) / kUnit, begin = max(x.low_first, 0) / kUnit;
-    x.sinks = (min(a.view.n_sink, hi) + kUnit - 1) / kUnit;
-    x.skip = max(begin - x.sinks, 0);
-    x.count = end - x.skip;
-    return x;
-  }
+  if constexpr (VIEW != kWindow) return {};
+  else return window_span(a.view.window, a.view.n_sink, first_row, ROWS, n, group, len, a.c.max_pages << a.c.block_log2);
 }
 
 // The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more
@@ -728,7 +712,7 @@ __device__ __forceinline__ void attend_shares(const CacheAttnArgs& a, int least,
     int u_last = u1 - 1;
     if (VIEW == kWindow) {
       u_end = min(u_end, span.count);
-      u_last = max(min(u1, span.count) - 1, 0);
+      u_last = span.last(u1);
     }
     const int seen_before = VIEW == kGroups ? len : len - n + 1, seen_first = VIEW == kGroups ? len : len - n + 1 + first_row / group;
     RowsLds<NT>& rows_lds = lds_rows[kOwn ? wave : 0];           // (waves of one share write the same)
@@ -1001,7 +985,7 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
   if (rows == 0 && !WEIGHTS) return;
   const Span span = span_of<VIEW, 16>(a, 0, n, max(group, 1), len);
   const int units = !good ? 0 : VIEW == kWindow ? span.count : (len + kUnit - 1) / kUnit;
-  const int last = VIEW == kWindow ? max(units - 1, 0) : ((a.c.max_pages << a.c.block_log2) / kUnit) - 1;
+  const int last = VIEW == kWindow ? span.last(units) : ((a.c.max_pages << a.c.block_log2) / kUnit) - 1;
   Flight f;
   Rows<1> r;
   f32x4 kept[kWholeUnits][4];

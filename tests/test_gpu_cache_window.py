@@ -246,3 +246,22 @@ def test_a_prompt_and_the_tokens_behind_it():
         want = orc.cache_window(c, q64[t:t + 1], [0, 1], np.arange(hq) // 2, n_sink, window)
         check(want, out[t:t + 1].double().cpu().numpy(), None, slice(0, 1), total, HALF, LIFT)
     dev.check_same(c)
+
+
+@FORMATS
+@pytest.mark.parametrize("group", [1, 12], ids=["rows_8", "rows_96"])
+@pytest.mark.parametrize("n_sink,window,pages", [(0, 105, 6), (0, 2 ** 31 - 1, 6), (0, 3000, 70), (5, 3000, 70)], ids=["short", "all", "by_shares", "by_shares_with_sinks"])
+def test_lengths_that_cannot_be(fmt, group, n_sink, window, pages):
+    """... without first tokens, too, whose unit is else the one that is looked up; heads beside them stay as they are."""
+    rng = np.random.default_rng(23)
+    lens = np.array([[300], [10 ** 9], [64 * pages + 1], [64 * pages], [2 ** 31 - 1], [-1], [-2 ** 30 - 3], [-2 ** 31], [300]])
+    c = filled(rng, np.where((lens >= 0) & (lens <= 64 * pages), lens, 0), 64, fmt, max_pages=pages)
+    c.lens[:] = lens
+    dev = Device(c)
+    n = 8 * len(lens)
+    q, q64 = bf16(rng.standard_normal((n, group, D)))
+    step, cu = step_of(dev, [8] * len(lens), group, False)
+    want = orc.cache_window(c, q64, cu, [0] * group, n_sink, window)
+    whole = [s for s in range(len(lens)) if np.isfinite(want.out[8 * s:8 * s + 8]).all()]
+    assert whole == [0, 3, 8] and np.isnan(want.out[8:24]).all() and np.isnan(want.out[32:64]).all()
+    check(want, *call(dev, step, n_sink, window, q.to(DEV)), slice(0, n), 64 * pages, HALF, LIFT)
