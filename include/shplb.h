@@ -433,7 +433,8 @@ SHPLB_API int32_t shplb_cache_attn_window(const shplb_cache* cache, const shplb_
  * every sequence as with a table in which its pages stand.
  *   prefix: a cache of one sequence for each prefix, with as many KV heads and of the same format; its pages may
  *     be of another pool and block, and its heads of different lengths.
- *   cu_prefix: device int32 [prefix->n_seq+1], not decreasing; offsets outside 0 .. cache->n_seq are taken as those.
+ *   cu_prefix: device int32 [prefix->n_seq+1], not decreasing; offsets outside 0 .. cache->n_seq are taken as those. (Where they
+ *     decrease, what rows of runs that overlap get is not defined; nothing outside of the buffers is read or written.)
  *   - The rows of a prefix are those between the cu_tokens of its first sequence and of the one behind its last.
  *   - A damaged length or page of a prefix makes NaN of what all its rows get, as one of a sequence does for its own.
  *   - Otherwise as shplb_cache_attn: numerics, errors, arguments, queries that see no token (now: neither of their prefix nor of their

@@ -127,7 +127,7 @@ int32_t check_window(const shplb_cache* c, int32_t max_tokens, int32_t n_sink, i
 // A call on sequences with prefixes: its arguments, without the tensors.
 struct SharedArgs {
   CacheAttnArgs own, pre;
-  int64_t most_rows;
+  int64_t most_rows, most_listed;  // (of units in the prefixes' list)
   int32_t rows_pre;                // rows of an item of the prefixes' list
   AttnLayout w;                    // of the own tokens' part; the prefixes' one lies behind it
   int64_t part_o, part_ml, begun, whole_o[2], whole_ml[2], total;
@@ -143,7 +143,8 @@ int32_t check_shared(const shplb_cache* prefix, const shplb_cache* cache, const 
   if (rows > 1 << 24) return SHPLB_E_UNSUPPORTED;
   x->rows_pre = prefix_attn_rows(rows / prefix->n_seq, int64_t(prefix->n_seq) * prefix->n_kv_heads, int64_t(prefix->max_pages) * prefix->block);
   const int64_t items = (rows / x->rows_pre + prefix->n_seq) * prefix->n_kv_heads;
-  if (items >= int64_t(1) << 24 || items * (int64_t(prefix->max_pages) * prefix->block / 64 + kCacheMostStart) >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
+  x->most_listed = items * (int64_t(prefix->max_pages) * prefix->block / 64 + kCacheMostStart);
+  if (items >= int64_t(1) << 24 || x->most_listed >= int64_t(1) << 30) return SHPLB_E_UNSUPPORTED;
   x->w = attn_layout(cache, step, x->most_rows);
   int64_t off = x->w.total;
   x->part_o = off; off += align256(prefix_slot_rows(x->rows_pre) * kHeadDim * 4);
@@ -278,6 +279,7 @@ int32_t shplb_cache_attn_shared(const shplb_cache* prefix, const int32_t* cu_pre
   x.pre.c = prefixes;
   x.pre.view.groups = cu_prefix;
   x.pre.view.members = cache->n_seq;
+  x.pre.view.most_listed = int32_t(x.most_listed);
   char* ws = static_cast<char*>(workspace);
   x.pre.part_o = reinterpret_cast<float*>(ws + x.part_o);
   x.pre.part_ml = reinterpret_cast<float*>(ws + x.part_ml);

@@ -130,10 +130,16 @@ __device__ __forceinline__ Span span_of(const CacheAttnArgs& a, int first_row, i
 // The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more
 // than `few` of them.  Up to 512 pairs every wave adds them up by itself, a lane a run of them; beyond, the four waves do it
 // together, and each looks for its place in the run where it lies, 64 pairs at a time.  (All units, beginnings and all, are below
-// 2^30: the entry point sees to that.)
+// 2^30: the entry point sees to that.  Groups that overlap, as offsets that go backwards have them, may have more between them: their sums
+// end at what groups have that do not, the place that is found is one of some pair all the same, and as much of the list lies behind it as
+// behind the place in the sums.)
 template <bool WEIGHTS, int ROWS, int START, int VIEW = kAll, class SHARES>
 __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int workers, int least, int few, int* lds, int& begin, int& end, SHARES& shares) {
   const int pairs = a.c.n_seq * a.c.n_kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const auto add = [&]() {
+    if constexpr (VIEW == kGroups) return UnitSums{a.view.most_listed};
+    else return PlainSums{};
+  }();
   const bool together = pairs > 512;
   const int me = together ? threadIdx.x : lane, each = together ? (pairs + kThreads - 1) / kThreads : (pairs + 63) / 64;
   const int first = min(me * each, pairs), last = min(first + each, pairs);
@@ -142,17 +148,17 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
   for (int p = first; p < last; ++p) {
     len = a.c.lens[p];
     pair_units<WEIGHTS, ROWS, VIEW>(a, pair_rows<false, VIEW>(a, p), len, tiles, units);
-    mine += tiles * (units + START);
+    mine = add(mine, tiles * (units + START));
   }
-  int sum = lane_sums(mine);
+  int sum = lane_sums(mine, add);
   int total = __builtin_amdgcn_readlane(sum, 63);
   if (together) {
     if (lane == 63) lds[wave] = total;
     __syncthreads();
     total = 0;
     for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) sum += lds[w];
-      total += lds[w];
+      if (w < wave) sum = add(sum, lds[w]);
+      total = add(total, lds[w]);
     }
     lds[kWaves + threadIdx.x] = sum;
     __syncthreads();
@@ -184,7 +190,7 @@ __device__ __forceinline__ Item locate(const CacheAttnArgs& a, int worker, int w
       tiles = units = 0;
       if (p < pairs) pair_units<WEIGHTS, ROWS, VIEW>(a, pair_rows<false, VIEW>(a, p), len, tiles, units);
       mine = tiles * (units + START);
-      sum = before + lane_sums(mine);
+      sum = add(before, lane_sums(mine, add));
       left = begin - (sum - mine);
       here = left >= 0 && left < mine;
       if (__ballot(here) || p0 + 64 >= pairs) break;

@@ -44,6 +44,7 @@ struct CacheView {
   int32_t most_units;              // of 64 tokens, that a tile of rows sees at most, and one more
   const int32_t* groups;           // [sequences of the cache + 1]
   int32_t members;                 // sequences of the step
+  int32_t most_listed;             // units of all groups, beginnings and all, where no two of them overlap; below 2^30
   float *whole_o, *whole_ml;       // workspace: partial results of rows, [n_tokens][n_q_heads][128] and [2]
 };
 
@@ -99,13 +100,17 @@ __device__ __forceinline__ T scalar_load(const T* p) {
 }
 
 // Sums over the lanes up to and with one's own.
-__device__ __forceinline__ int lane_sums(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // from 1, 2, 4, 8 lanes below in the row of 16
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // the last lane of a row to the next one, of 32 to the others
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+struct PlainSums {
+  constexpr int operator()(int x, int y) const { return x + y; }
+};
+template <class ADD = PlainSums>
+__device__ __forceinline__ int lane_sums(int x, ADD add = {}) {
+  x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));      // from 1, 2, 4, 8 lanes below in the row of 16
+  x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+  x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+  x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+  x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));     // the last lane of a row to the next one, of 32 to the others
+  x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
   return x;
 }
 

@@ -1,5 +1,5 @@
-// Which units of 64 keys a tile of query rows sees with a sliding window and first tokens that stay visible.  Plain arithmetic, the same
-// on the host and on the device.
+// Which units of 64 keys a tile of query rows sees with a sliding window and first tokens that stay visible, and sums of units that stay
+// numbers of 32 bits.  Plain arithmetic, the same on the host and on the device.
 #pragma once
 #include <cstdint>
 
@@ -32,5 +32,12 @@ constexpr Span window_span(int window, int n_sink, int first_row, int rows, int 
   x.count = end - x.skip;
   return x;
 }
+
+// Sums of units up to `most`, which is below 2^30, of addends up to it: the smaller of the true sum and `most`, in whatever order they are
+// added.
+struct UnitSums {
+  int most;
+  constexpr int operator()(int x, int y) const { return smaller(x + y, most); }
+};
 
 }  // namespace shplb

@@ -1,4 +1,5 @@
-"""Which units of the cache a tile of rows with windows looks up, on the host: the arithmetic that the kernels use, compiled by itself."""
+"""Which units of the cache a tile of rows with windows looks up, and where shares of a list of units begin, on the host: the arithmetic that the
+kernels use, compiled by itself."""
 import ctypes as C
 import itertools
 import shutil
@@ -16,11 +17,12 @@ extern "C" int span_units(int window, int n_sink, int first_row, int rows, int n
   for (int u = 0; u <= last && u < most; ++u) out[u] = x.unit(u);
   return x.count <= 0 ? -last - 1 : last + 1;
 }
+extern "C" int add_units(int x, int y, int most) { return UnitSums{most}(x, y); }
 """
 
 
 @pytest.fixture(scope="module")
-def units(tmp_path_factory, repo_root):
+def program(tmp_path_factory, repo_root):
     if shutil.which("g++") is None:
         pytest.skip("no g++")
     at = tmp_path_factory.mktemp("span")
@@ -28,7 +30,12 @@ def units(tmp_path_factory, repo_root):
     lib = at / "libspan.so"
     subprocess.run(["g++", "-std=c++17", "-O2", "-fwrapv", "-shared", "-fPIC", "-I", repo_root + "/paper_2603_10353_amd/csrc", str(at / "span.cpp"), "-o", str(lib)],
                    check=True)
-    call = C.CDLL(str(lib)).span_units
+    return C.CDLL(str(lib))
+
+
+@pytest.fixture(scope="module")
+def units(program):
+    call = program.span_units
 
     def of(window, n_sink, first_row, rows, n, group, length, room):
         """The units that are looked up, and whether there are any to attend to."""
@@ -65,3 +72,34 @@ def test_units_are_those_that_some_row_sees(units):
         got, some = units(window, n_sink, first_row, rows, n, group, length, room)
         assert all(0 <= u < room // 64 for u in got)
         assert seen <= set(got) and (not some or (min(got), max(got)) == (min(seen), max(seen))) and some == bool(seen)
+
+
+def place(begin, runs, before, add):
+    """Where unit `begin` of a list lies: the first of the consecutive addends whose sum passes it, and how far into it, as the kernels look for it."""
+    total = before
+    for i, mine in enumerate(runs):
+        total = add(total, mine)
+        left = begin - (total - mine)
+        if 0 <= left < mine:
+            return i, left
+    return None, 0
+
+
+@pytest.mark.parametrize("each", [300000000, 6552 * 8200, 2 ** 30 - 1])
+def test_shares_of_groups_that_overlap(program, each):
+    """The units of groups that overlap may pass 32 bits: every share begins in an addend, and the list goes on for as long as the sums do."""
+    most = 2 ** 30 - 1
+    add = lambda x, y: program.add_units(x, y, most)
+    runs = [5, 0, 17] + [each, 3] * 40
+    total = 0
+    for x in runs:
+        total = add(total, x)
+    assert total == min(sum(runs), most)
+    for worker in range(513):
+        begin = min(worker * (total // 512), total - 1)
+        i, left = place(begin, runs, 0, add)
+        assert i is not None and sum(runs[i:]) - left >= total - begin
+        for first in range(1, i):              # in two steps, as runs of several addends are looked through
+            before = add(0, min(sum(runs[:first]), most))
+            if before <= begin:
+                assert place(begin, runs[first:], before, add) == (i - first, left)

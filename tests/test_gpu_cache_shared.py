@@ -310,3 +310,56 @@ def test_samples_of_a_prompt_token_after_token():
         torch.cuda.synchronize()
         assert (again == out).all() and (again_lse == lse).all()
     dev.check_same(c)
+
+
+class Guarded:
+    """A buffer with a pattern in front of it and behind it."""
+    ROOM = 1 << 16
+
+    def __init__(self, n_bytes, fill):
+        self.all = torch.full((2 * self.ROOM + -(-n_bytes // 256) * 256,), 0xa5, dtype=torch.uint8, device=DEV)
+        self.end = self.ROOM + n_bytes
+        self.bytes = self.all[self.ROOM:self.end]
+        self.bytes.fill_(fill)
+
+    def check(self):
+        assert (self.all[:self.ROOM] == 0xa5).all() and (self.all[self.end:] == 0xa5).all()
+
+
+def guarded_call(pre, groups, dev, step, q, left):
+    """out, lse (0x41414141 where nothing was written), the workspace's bytes being `left`: nothing around them is written."""
+    T, heads = q.shape[0], q.shape[1]
+    out, lse, ws = (Guarded(n, f) for n, f in ((T * heads * D * 2, 0x41), (T * heads * 4, 0x41),
+                                              (S.shplb_cache_attn_shared_workspace_bytes(pre.cache, dev.cache, step), left)))
+    o, l = out.bytes.view(torch.bfloat16).view(T, heads, D), lse.bytes.view(torch.float32).view(heads, T)
+    S.shplb_cache_attn_shared(pre.cache, cu_of(groups), dev.cache, step, q, o, l, ws.bytes, stream())
+    torch.cuda.synchronize()
+    for x in (out, lse, ws):
+        x.check()
+    return o, l
+
+
+OVERLAPPING = {  # prefixes, tokens of each, KV heads, sequences, query heads: rows of a prefix's tile as the names say
+    "rows_16": (600, 150, 2, 40, 8),
+    "rows_32": (20, 200, 2, 50, 16),
+    "rows_128": (50, 5120, 1, 700, 4),
+}
+
+
+@FORMATS
+@pytest.mark.parametrize("name", OVERLAPPING)
+def test_groups_that_overlap(name, fmt):
+    """cu_prefix that goes to and fro, so that half of the prefixes have all sequences: many times the work that the call is sized for.  It ends, and
+    nothing outside is written; sequences behind the last group are what they are without."""
+    n_pre, tokens, hkv, n, hq = OVERLAPPING[name]
+    rng = np.random.default_rng(17)
+    prefix = filled(rng, [[tokens] * hkv], 64, fmt, spare=0)
+    c = filled(rng, [[20] * hkv] * (n + 3), 64, fmt)
+    prefix.table, prefix.lens = np.repeat(prefix.table, n_pre, 0), np.repeat(prefix.lens, n_pre, 0)
+    pre, dev = Device(prefix), Device(c)
+    q, q64 = bf16(rng.standard_normal((n + 3, hq, D)))
+    step, cu = step_of(dev, [1] * (n + 3), hq, False)
+    groups = [n * (x % 2) for x in range(n_pre + 1)]
+    o, l = guarded_call(pre, groups, dev, step, q.to(DEV), 0x7f)
+    want = orc.cache_shared(prefix, [0], c, q64, cu, np.arange(hq) * hkv // hq)
+    check(want, o.double().cpu().numpy(), l.double().cpu().numpy(), slice(n, n + 3), 84, HALF, LIFT)
