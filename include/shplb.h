@@ -234,7 +234,9 @@ SHPLB_API int32_t shplb_sparse_attn_prefill_split(const shplb_problem* p, const 
  *     before they are added up.  Results are bit-identical from run to run; in calls of at most as many
  *     rows (of 128 queries) as there are compute units a sum may be taken in another order than in larger ones.
  *   - A key or value that is infinite or NaN reaches the tokens that see it, and no others.  (Where there are such values, rows near
- *     them are worked on twice.)
+ *     them are worked on twice, and so are those whose scores, times log2(e), are 2^22 or more.)
+ *   - Scores and sums past fp32's range count as infinite.  The sum of probabilities times values is taken before it is divided by
+ *     that of the probabilities.
  *   q, k, v: device bf16; out: device bf16, strides as Q, in other memory than q, k and v;
  *   lse_out: device fp32 [n_q_heads, T], natural logarithm of the softmax denominators, or NULL.
  * Errors: SHPLB_E_NULL, SHPLB_E_SHAPE, SHPLB_E_UNSUPPORTED as above; SHPLB_E_BUDGET (window < 1 or n_sink < 0). */

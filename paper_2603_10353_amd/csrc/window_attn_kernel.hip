@@ -27,6 +27,8 @@
 //    with masks are looked through for such values, and where there are some, they are counted apart, but only once an item has come out
 //    with a sum that is not finite, as it does whenever there are some; it is then worked on again.  (Looked through at once: 777 tokens
 //    13.7 us, 13.1 so, 48 sequences 132 and 127.)
+//  - a reference is a rounded product, a probability's exponent a multiply-add: from references of 2^31 on the two can differ by 128, and
+//    probabilities be infinite or all 0.  An item with a reference of 2^22 or more is worked on again, too, with products rounded alike.
 #include <algorithm>
 
 #include "attn_common.h"
@@ -94,7 +96,8 @@ __device__ __forceinline__ const char* uniform(const char* p) {
                                        uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32)))) << 32);
 }
 
-// One item; whether a sum came out that is not finite.  CAREFUL: values that are not finite are told apart from zeros by what sees them.
+// One item; whether it is to be worked on again, CAREFUL: a sum came out that is not finite, or a reference that is far out.  Then values that
+// are not finite are told apart from zeros by what sees them, and scores are rounded as references are.
 // lds: two stages of K, two of V; s_bad: -1.
 template <int QG, bool CAREFUL>
 __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowItem& it, char* lds, int& s_bad) {
@@ -148,6 +151,7 @@ __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowIte
   int u = 0;                                 // the tile; tile u is in stage u mod 2
   f32x4 sc[QG][MT], acc[QG][8];
   float m_ref[QG], l_run[QG];
+  const float to_log2 = CAREFUL ? 1.0f : a.scale_log2;           // what scores are multiplied by beside their reference
   int q_pos[QG];                           // (queries behind the end of the sequence: the last one again)
 #pragma unroll
   for (int qg = 0; qg < QG; ++qg) {
@@ -280,8 +284,8 @@ __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowIte
       for (int x = 0; x < 2 * QG * MT; ++x) {       // two probabilities of a query group, the groups in turn
         const int qg = x % QG, mt = x / (2 * QG), c = x / QG % 2;
         const float m_use = m_ref[qg] == -INFINITY ? 0.0f : m_ref[qg];
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qg][mt][2 * c], a.scale_log2, -m_use));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qg][mt][2 * c + 1], a.scale_log2, -m_use));
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qg][mt][2 * c], to_log2, -m_use));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qg][mt][2 * c + 1], to_log2, -m_use));
         pk[qg][mt][c] = pack_bf16(p0, p1);
         sum[qg][0] += p0;
         sum[qg][1] += p1;
@@ -290,6 +294,15 @@ __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowIte
       for (int qg = 0; qg < QG; ++qg) rs[qg] = sum[qg][0] + sum[qg][1];
     };
     if (mine) {
+      if constexpr (CAREFUL) {
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            sc[qg][mt] *= a.scale_log2;
+            asm volatile("" : "+v"(sc[qg][mt]));               // rounded: not part of a multiply-add
+          }
+      }
       probabilities();
       // The reference was fixed by earlier tiles: it is too low for this one where a probability, and with it the sum, came out
       // large, or where there was none.  Then it is raised to the tile's maximum.
@@ -297,7 +310,7 @@ __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowIte
       if (__any(too_low(0) || too_low(QG - 1))) {
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg) {
-          const float m_tile = quad_max(tile_max(qg)) * a.scale_log2;
+          const float m_tile = quad_max(tile_max(qg)) * to_log2;
           const float m_new = fmaxf(m_ref[qg], m_tile);
           const float alpha = m_new == m_ref[qg] ? 1.0f : __builtin_amdgcn_exp2f(m_ref[qg] - m_new);
           m_ref[qg] = m_new;
@@ -404,10 +417,14 @@ __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowIte
     step(std::false_type{});               // (the last tile is never plain)
   }
   __builtin_amdgcn_s_setprio(0);
-  float odd = 0.0f;                          // NaN if there is such a sum
+  bool again = false;
   if constexpr (!CAREFUL) {
+    float odd = 0.0f;                        // NaN if there is such a sum
 #pragma unroll
     for (int x = 0; x < 32 * QG; ++x) odd = __builtin_fmaf(acc[x >> 5][x >> 2 & 7][x & 3], 0.0f, odd);
+    again = odd != 0.0f;
+#pragma unroll
+    for (int qg = 0; qg < QG; ++qg) again |= fabsf(m_ref[qg]) >= 0x1p22f;
   }
 
   // ---- out: a lane has dims 16 dt + 4 hi + r of its queries; neighbours trade, and a lane stores eight dims at a time
@@ -430,24 +447,24 @@ __device__ __forceinline__ bool attend_item(const WindowArgs& a, const WindowIte
       if (valid) *reinterpret_cast<u32x4*>(dst + 32 * p) = u32x4{e0, e1, o0, o1};
     }
   }
-  return __ballot(odd != 0.0f) != 0;
+  return __ballot(again) != 0;
 }
 
 // QG: groups of 16 queries of a wave.
 template <int QG>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_attn_kernel(WindowArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
-  __shared__ int s_bad, s_odd;               // the last step whose values are not all finite; whether some sum is not
+  __shared__ int s_bad, s_again;             // the last step whose values are not all finite; whether the item is worked on again
   if (threadIdx.x == 0) {
     s_bad = -1;
-    s_odd = 0;
+    s_again = 0;
   }
   const int in_lap = int(uint32_t(blockIdx.x) % uint32_t(a.lap)), place = int(blockIdx.x) - in_lap + in_lap % kXcds * (a.lap / kXcds) + in_lap / kXcds;
   if (place >= a.items) return;
   const WindowItem it = window_item<64 * QG>(a, place);
-  if (attend_item<QG, false>(a, it, lds, s_bad) && threadIdx.x % 64 == 0) s_odd = 1;
+  if (attend_item<QG, false>(a, it, lds, s_bad) && threadIdx.x % 64 == 0) s_again = 1;
   __syncthreads();
-  if (s_odd != 0) attend_item<QG, true>(a, it, lds, s_bad);      // (and writes the outputs again)
+  if (s_again != 0) attend_item<QG, true>(a, it, lds, s_bad);      // (and writes the outputs again)
 }
 
 }  // namespace

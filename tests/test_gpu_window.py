@@ -214,3 +214,30 @@ def test_a_window_no_sequence_is_longer_than_is_causal_attention():
     out, l = call(p, 0, T, q, k, v)
     assert np.abs(out - dense.double().cpu().numpy()).max() <= 2e-2
     assert np.abs(l - lse.double().cpu().numpy()).max() <= 4e-3
+
+
+@pytest.mark.parametrize("hq", [2, 64], ids=["few_rows", "many_rows"])
+@pytest.mark.parametrize("order", ["any", "rising", "below_zero"])
+@pytest.mark.parametrize("size", [10, 13, 15, 16, 20, 40, 55])
+def test_scores_that_a_rounding_moves_by_more_than_one(size, order, hq):
+    """Keys are whole multiples of one vector of 2^size and -2^size, queries likewise: scores are sums without rounding, multiples of 128 * 2^(2 size) *
+    scale > 2^20, so that only the keys of the largest multiple that a query sees count, all alike: their probabilities are 1 / how many, what is left
+    are the roundings of a probability and of the output (2^-8 each), and of the largest score, its product with the scale and the logarithm (2^-22
+    of it in all)."""
+    rng = np.random.default_rng([24, size])
+    T, n_sink, window = 700, 3, 130
+    sign = rng.choice([-1.0, 1.0], D)
+    times = rng.integers(1, 100, (T, 2))
+    if order == "rising":
+        times = np.sort(times, 0)
+    if order == "below_zero":
+        times = -times
+    k = times[:, :, None] * sign * 2.0 ** size
+    q = rng.integers(1, 4, (T, 2, 1)) * sign * 2.0 ** size
+    (q, q64), (k, k64), (v, v64) = bf16(q), bf16(k), bf16(rng.standard_normal((T, 2, D)))
+    out, lse = call(S.Problem([0, T], hq, 2, 128), n_sink, window, q.repeat_interleave(hq // 2, 1).to(DEV), k.to(DEV), v.to(DEV))
+    want = orc.window_attention(q64, k64, v64, [0, T], n_sink, window, [0, 1])
+    heads = [0, hq - 1]
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+    assert (np.abs(out[:, heads] - want.out) <= 2.0 ** -8 * np.abs(want.out) + 2.0 ** -8 * (1 + 2.0 ** -8) * want.size + 1e-30).all()
+    assert (np.abs(lse[heads] - want.lse) <= 2.0 ** -22 * np.abs(want.lse)).all()
