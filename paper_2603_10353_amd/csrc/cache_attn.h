@@ -30,7 +30,6 @@
 // 6 to join; a sequence of 777 tokens 10 us, of which the launch and three reads that wait for one another are eight.
 #pragma once
 #include "cache_common.h"
-#include "cache_span.h"
 
 namespace shplb {
 namespace {
@@ -122,9 +121,9 @@ __device__ __forceinline__ void pair_units(const CacheAttnArgs& a, int rows, int
 
 // What the rows first_row .. first_row + ROWS - 1 of n tokens see with windows.
 template <int VIEW, int ROWS>
-__device__ __forceinline__ Span span_of(const CacheAttnArgs& a, int first_row, int n, int group, int len) {
+__device__ __forceinline__ Span span_of(const CacheAttnArgs& a, int first_row, int n, int group, bool good, int len) {
   if constexpr (VIEW != kWindow) return {};
-  else return window_span(a.view.window, a.view.n_sink, first_row, ROWS, n, group, len, a.c.max_pages << a.c.block_log2);
+  else return window_span(a.view.window, a.view.n_sink, first_row, ROWS, n, group, good ? len : 0);
 }
 
 // The place where a worker's share [begin, end) of all units begins.  Shares are of `least` units at least, if there are more
@@ -714,7 +713,7 @@ __device__ __forceinline__ void attend_shares(const CacheAttnArgs& a, int least,
     int u_end = good && len > 0 ? u1 : 0;
     // units behind what the tile's last row sees are none (a step that is a whole prompt: half of them)
     if (!kOwn && VIEW == kAll) u_end = min(u_end, (max(len - n + 1 + (min(first_row + kRows, n * group) - 1) / group, 0) + kUnit - 1) / kUnit);
-    const Span span = span_of<VIEW, kRows>(a, first_row, n, group, len);
+    const Span span = span_of<VIEW, kRows>(a, first_row, n, group, good, len);
     int u_last = u1 - 1;
     if (VIEW == kWindow) {
       u_end = min(u_end, span.count);
@@ -989,7 +988,7 @@ __global__ __launch_bounds__(64 * kWholeWaves, 2) void cache_whole_kernel(CacheA
   // (the page table is read up to its end: what is looked up does not wait for the length)
   const int rows = n * group, seen_before = len - n + 1;
   if (rows == 0 && !WEIGHTS) return;
-  const Span span = span_of<VIEW, 16>(a, 0, n, max(group, 1), len);
+  const Span span = span_of<VIEW, 16>(a, 0, n, max(group, 1), good, len);
   const int units = !good ? 0 : VIEW == kWindow ? span.count : (len + kUnit - 1) / kUnit;
   const int last = VIEW == kWindow ? span.last(units) : ((a.c.max_pages << a.c.block_log2) / kUnit) - 1;
   Flight f;

@@ -7,6 +7,7 @@
 // so does everything read from the page.
 #pragma once
 #include "attn_common.h"
+#include "cache_span.h"
 
 namespace shplb {
 
@@ -128,7 +129,7 @@ __device__ __forceinline__ void step_tokens(const StepArgs& t, int s, int& row0,
 }
 
 // Whether a head's length is one that its page table row can hold.
-__device__ __forceinline__ bool good_length(const CacheArgs& c, int len) { return len >= 0 && len <= c.max_pages << c.block_log2; }
+__device__ __forceinline__ bool good_length(const CacheArgs& c, int len) { return length_fits(len, c.max_pages << c.block_log2); }
 
 constexpr uint32_t kNanBits = 0x7fc00000u;
 

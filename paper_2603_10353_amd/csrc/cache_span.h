@@ -19,10 +19,13 @@ struct Span {
   constexpr int last(int u1) const { return larger(smaller(u1, count) - 1, 0); }
 };
 
-// Of rows first_row .. first_row + rows - 1 of n tokens with `group` rows each, the last ones of a head of `len` tokens, whose table has room
-// for so many.  Of a length that cannot be: none, as of length 0 (the units are places in the table, and the first one is looked up in any case).
-constexpr Span window_span(int window, int n_sink, int first_row, int rows, int n, int group, int len, int room) {
-  const int held = len >= 0 && len <= room ? len : 0, before = held - n + 1, first = first_row / group, last = (smaller(first_row + rows, n * group) - 1) / group;
+// Whether a length is one that a head's row of the page table has room for.
+constexpr bool length_fits(int len, int room) { return len >= 0 && len <= room; }
+
+// Of rows first_row .. first_row + rows - 1 of n tokens with `group` rows each, the last ones of a head that holds `held` tokens: its length,
+// but of one that cannot be 0 (the units are places in the table, and the first one is looked up in any case).
+constexpr Span window_span(int window, int n_sink, int first_row, int rows, int n, int group, int held) {
+  const int before = held - n + 1, first = first_row / group, last = (smaller(first_row + rows, n * group) - 1) / group;
   Span x{};
   x.low_first = before + first - window;
   x.low_last = before + last - window;

@@ -12,7 +12,7 @@ PROGRAM = """
 #include "cache_span.h"
 using namespace shplb;
 extern "C" int span_units(int window, int n_sink, int first_row, int rows, int n, int group, int len, int room, int u1, int* out, int most) {
-  const Span x = window_span(window, n_sink, first_row, rows, n, group, len, room);
+  const Span x = window_span(window, n_sink, first_row, rows, n, group, length_fits(len, room) ? len : 0);
   const int last = x.last(u1);
   for (int u = 0; u <= last && u < most; ++u) out[u] = x.unit(u);
   return x.count <= 0 ? -last - 1 : last + 1;
