@@ -203,7 +203,7 @@ int32_t shplb_cache_attn_workspace_bytes(const shplb_cache* cache, const shplb_s
 
 int32_t shplb_cache_attn(const shplb_cache* cache, const shplb_step* step, const void* q, void* out, float* lse_out,
                          const float* weight_in, float* weight_out, void* workspace, void* stream) {
-  CacheAttnArgs a;
+  CacheAttnArgs a{};
   int64_t most_rows;
   if (int32_t st = check_cache(cache, &a.c)) return st;
   if (int32_t st = check_queries(cache, step, &a.groups, &most_rows)) return st;
