@@ -363,3 +363,69 @@ def test_groups_that_overlap(name, fmt):
     o, l = guarded_call(pre, groups, dev, step, q.to(DEV), 0x7f)
     want = orc.cache_shared(prefix, [0], c, q64, cu, np.arange(hq) * hkv // hq)
     check(want, o.double().cpu().numpy(), l.double().cpu().numpy(), slice(n, n + 3), 84, HALF, LIFT)
+
+
+def without_order(prefix, groups, c, q64, cut, most_new):
+    """What rows get where cu_tokens (cut) and cu_prefix are in no order, as far as it is defined: those of one sequence, of one prefix's rows at most.
+    A sequence's rows begin at its offset and are max_tokens at most, a prefix's go from the offset of its first sequence to that of the one
+    behind its last; rows of a sequence outside of its prefix's are NaN.  Returns it, and of each row what it is: -1 of no sequence, 1 defined."""
+    T, heads = q64.shape[:2]
+    inside = lambda x: min(max(int(x), 0), T)
+    owners, fronts = ([[] for _ in range(T)] for _ in "of")
+    for s in range(len(cut) - 1):
+        a = inside(cut[s])
+        b = a + min(max(min(int(cut[s + 1]), T) - a, 0), most_new)
+        for r in range(a, b):
+            owners[r].append((s, r - a, b - a))
+    for g in range(len(groups) - 1):
+        if groups[g] < groups[g + 1]:
+            for r in range(inside(cut[groups[g]]), inside(cut[groups[g + 1]])):
+                fronts[r].append(g)
+    want, kind = orc.Result(q64), np.zeros(T, int)
+    for r in range(T):
+        if not owners[r]:
+            kind[r] = -1
+        if len(owners[r]) != 1 or len(fronts[r]) > 1:
+            continue
+        kind[r] = 1
+        s, j, n = owners[r][0]
+        of = [g for g in range(len(groups) - 1) if groups[g] <= s < groups[g + 1]]
+        if of and fronts[r] != of:
+            want.out[r], want.lse[:, r] = np.nan, np.nan
+            continue
+        parts = [orc._values_at(prefix, g, 0, np.arange(int(prefix.lens[g, 0]))) for g in of]
+        length = int(c.lens[s, 0])
+        parts.append([x[:max(0, length - n + 1 + j)] for x in orc._values_at(c, s, 0, np.arange(length))])
+        k, v = (np.concatenate([p[x] for p in parts]) for x in (0, 1))
+        for h in range(heads):
+            want.put(r, h, q64[r, h], k, v, D ** -0.5, True)
+    return want, kind
+
+
+@FORMATS
+@pytest.mark.parametrize("n,new,heads,room", [(40, 1, 2, 2), (40, 6, 4, 2), (150, 1, 4, 4), (150, 6, 4, 4), (150, 6, 4, 40)],
+                         ids=["rows_16", "rows_32", "rows_128", "rows_128_drafts_in_little", "rows_128_drafts"])
+def test_offsets_in_no_order(n, new, heads, room, fmt):
+    """cu_tokens in no order, whatever the workspace holds: rows of one sequence and of one prefix at most are right, those of none stay as they were,
+    and nothing is written around the buffers."""
+    rng = np.random.default_rng([25, n, new])
+    large = n > 100
+    prefix = filled(rng, [[300], [70], [1]], 64, fmt, max_pages=4000 if large else 5)
+    c = filled(rng, rng.integers(0, 120, (n, 1)), 64, fmt, max_pages=room)
+    pre, dev = Device(prefix), Device(c)
+    T = new * n
+    q, q64 = bf16(rng.standard_normal((T, heads, D)))
+    groups = [0, n // 3, n // 2, n - 5]
+    met = np.zeros(3, int)
+    for left in (0xff, 0x7f, 0x01):
+        cut = rng.integers(-9, T + 9, n + 1).astype(np.int32)
+        ends = np.array([0, n // 3, n // 2, n - 5])
+        cut[ends] = np.sort(cut[ends])         # the prefixes' rows are in order
+        step = S.Step(n, heads, 1, T, 2 * new, torch.from_numpy(cut).to(DEV))
+        want, kind = without_order(prefix, groups, c, q64, cut, 2 * new)
+        o, l = guarded_call(pre, groups, dev, step, q.to(DEV), left)
+        assert (o[torch.from_numpy(kind < 0).to(DEV)].view(torch.uint8) == 0x41).all()
+        rows = np.flatnonzero(kind == 1)
+        check(want, o.double().cpu().numpy(), l.double().cpu().numpy(), rows, 420, HALF, LIFT)
+        met += [(kind < 0).sum(), np.isnan(want.out[rows, 0, 0]).sum(), np.isfinite(want.out[rows, 0, 0]).sum()]
+    assert (met > 0).all()
