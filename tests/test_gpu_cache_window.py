@@ -265,3 +265,19 @@ def test_lengths_that_cannot_be(fmt, group, n_sink, window, pages):
     whole = [s for s in range(len(lens)) if np.isfinite(want.out[8 * s:8 * s + 8]).all()]
     assert whole == [0, 3, 8] and np.isnan(want.out[8:24]).all() and np.isnan(want.out[32:64]).all()
     check(want, *call(dev, step, n_sink, window, q.to(DEV)), slice(0, n), 64 * pages, HALF, LIFT)
+
+
+@pytest.mark.parametrize("fmt,block", [(cache_oracle.E4M3, 128), (cache_oracle.INT8, 64)], ids=["e4m3", "int8"])
+@pytest.mark.parametrize("n,new,window", [(32, 4, 2400), (64, 8, 4400), (65, 8, 4474)], ids=["128_tiles", "512_tiles", "520_tiles_of_the_longest"])
+def test_tiles_of_longer_windows_a_workgroup_each(n, new, window, fmt, block):
+    """Windows of more than 2048 tokens and so many tiles of 32 rows that each is a workgroup's: up to 18 units a wave.  A few sequences are long."""
+    rng = np.random.default_rng([26, n])
+    lens = rng.integers(1, 90, (n, 1))
+    lens[[0, n // 2, n - 1], 0] = [5000, window + 1, 4700]
+    c = filled(rng, lens, block, fmt)
+    forget(rng, c, np.full(n, new), 3, window)
+    dev = Device(c)
+    q, q64 = bf16(rng.standard_normal((n * new, 32, D)))
+    step, cu = step_of(dev, [new] * n, 32, False)
+    out, lse = call(dev, step, 3, window, q.to(DEV))
+    check(orc.cache_window(c, q64, cu, [0] * 32, 3, window), out, lse, slice(0, n * new), 5000, HALF, LIFT)
