@@ -6,7 +6,7 @@ import torch
 import paper_2603_10353_amd as S
 from cache_harness import D, DEV, Device, bf16, filled, step_of, strided
 from oracle import cache_oracle, window_oracle as orc
-from window_harness import check, in_a_large_pool
+from window_harness import check, check_far, far_apart, in_a_large_pool
 
 pytestmark = pytest.mark.gpu
 E4M3, INT8 = cache_oracle.E4M3, cache_oracle.INT8
@@ -429,3 +429,21 @@ def test_offsets_in_no_order(n, new, heads, room, fmt):
         check(want, o.double().cpu().numpy(), l.double().cpu().numpy(), rows, 420, HALF, LIFT)
         met += [(kind < 0).sum(), np.isnan(want.out[rows, 0, 0]).sum(), np.isfinite(want.out[rows, 0, 0]).sum()]
     assert (met > 0).all()
+
+
+@FORMATS
+@pytest.mark.parametrize("n,room", [(2, 0), (12, 0), (60, 4000)], ids=["rows_8", "rows_48", "rows_240_in_128"])
+@pytest.mark.parametrize("size", [(10, 10), (15, 16), (16, 20), (40, 40), (100, -30), (-60, 115)])
+def test_scores_that_a_rounding_moves_by_more_than_one(size, n, room, fmt):
+    """... those of the prefix the largest for some, of its own tokens for others."""
+    rng = np.random.default_rng([28, *(abs(x) for x in size)])
+    for order in ("any", "rising", "below_zero"):
+        prefix, c = filled(rng, [[700]], 64, fmt, max_pages=max(room, 12)), filled(rng, [[9 + x % 100] for x in range(n)], 64, fmt)
+        for x in (prefix, c):
+            cu = np.concatenate([[0], np.cumsum(x.lens[:, 0])])
+            cache_oracle.append(x, bf16(far_apart(rng, (int(cu[-1]), 1), size[0], order))[1], bf16(rng.standard_normal((int(cu[-1]), 1, D)))[1], cu)
+        pre, dev = Device(prefix), Device(c)
+        q, q64 = bf16(far_apart(rng, (n, 4), size[1], "any"))
+        step, cu = step_of(dev, [1] * n, 4, False)
+        want = orc.cache_shared(prefix, [0, n], c, q64, cu, [0] * 4)
+        check_far(want, *call(pre, [0, n], dev, step, q.to(DEV)), slice(0, n), HALF)

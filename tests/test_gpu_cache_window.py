@@ -6,7 +6,7 @@ import torch
 import paper_2603_10353_amd as S
 from cache_harness import D, DEV, Device, bf16, filled, step_of, strided
 from oracle import cache_oracle, window_oracle as orc
-from window_harness import check, in_a_large_pool
+from window_harness import check, check_far, far_apart, in_a_large_pool
 
 pytestmark = pytest.mark.gpu
 FORMATS = pytest.mark.parametrize("fmt", [cache_oracle.E4M3, cache_oracle.INT8], ids=["e4m3", "int8"])
@@ -281,3 +281,22 @@ def test_tiles_of_longer_windows_a_workgroup_each(n, new, window, fmt, block):
     step, cu = step_of(dev, [new] * n, 32, False)
     out, lse = call(dev, step, 3, window, q.to(DEV))
     check(orc.cache_window(c, q64, cu, [0] * 32, 3, window), out, lse, slice(0, n * new), 5000, HALF, LIFT)
+
+
+@FORMATS
+@pytest.mark.parametrize("order", ["any", "rising", "below_zero"])
+@pytest.mark.parametrize("size", [(10, 10), (15, 16), (16, 20), (40, 40), (100, -30), (-60, 115)])
+def test_scores_that_a_rounding_moves_by_more_than_one(size, order, fmt):
+    rng = np.random.default_rng([27, *(abs(x) for x in size)])
+    lens = [[700, 3100], [90, 64]]
+    c = filled(rng, lens, 64, fmt)
+    n = np.max(lens, 1)
+    cu = [0, n[0], n.sum()]
+    cache_oracle.append(c, bf16(far_apart(rng, (int(n.sum()), 2), size[0], order))[1], bf16(rng.standard_normal((int(n.sum()), 2, D)))[1], cu)
+    dev = Device(c)
+    for new in (2, 12):
+        q, q64 = bf16(far_apart(rng, (2 * new, 4), size[1], "any"))
+        step, cu = step_of(dev, [new, new], 4, False)
+        for window in (100, 3000):
+            want = orc.cache_window(c, q64, cu, [0, 0, 1, 1], 2, window)
+            check_far(want, *call(dev, step, 2, window, q.to(DEV)), slice(0, 2 * new), HALF)

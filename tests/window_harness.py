@@ -48,3 +48,21 @@ def in_a_large_pool(c):
     dev.cache = S.Cache(dev.k_pages, dev.v_pages, dev.k_scale, dev.v_scale, dev.table, dev.lens, dev.n_seq, dev.n_kv_heads, c.block,
                         dev.max_pages, behind + c.n_pages, S.SHPLB_CACHE_E4M3 if c.fmt == cache_oracle.E4M3 else S.SHPLB_CACHE_INT8)
     return dev
+
+
+def far_apart(rng, shape, size, order):
+    """Multiples 1 .. 14 of one vector of 2^size and -2^size (for keys: shape (tokens, heads)): products with others of the kind are sums without
+    rounding, in the cache's formats, too, and no two of them that differ are closer than a fourteenth."""
+    times = rng.integers(1, 15, shape)
+    if order == "rising":
+        times = np.sort(times, 0)
+    return times[..., None] * (1.0 - 2.0 * (np.arange(D) % 3 == 0)) * 2.0 ** size * (-1.0 if order == "below_zero" else 1.0)
+
+
+def check_far(want, got_out, got_lse, rows, half_probability):
+    """Against the oracle's Result where scores are those of far_apart(), times 2^20 and more, so that only the largest ones of a row count, all of them alike:
+    what rounds is a probability, the output (2^-8), and, of the largest score, its products with the scales, the logarithm and their sum (2^-22 of it)."""
+    out, lse, a, b = want.out[rows], want.lse[:, rows], got_out[rows], got_lse[:, rows]
+    assert np.isfinite(a).all() and np.isfinite(b).all()
+    assert (np.abs(a - out) <= 2.0 ** -8 * np.abs(out) + half_probability * (1 + 2.0 ** -8) * want.size[rows] + 1e-30).all()
+    assert (np.abs(b - lse) <= 2.0 ** -22 * np.abs(lse)).all()
