@@ -9,7 +9,7 @@ namespace {
 // ---- windows.  A step's work does not grow with the context: a head has the units of its window and of its first tokens, and how the
 // work is divided follows from them like that of cache_attn_kernel.hip from a table's room.  Bound by reading with few rows (128 sequences
 // x 8 heads, a window of 4096: 148 us, 5.7 TB/s of what is seen), by VALU work with many (codes to fp16 for every 32 rows: 8 sequences x 32 tokens x 28/4
-// int8 heads, a window of 2000: 28 to 30 us).  128 rows at a time, as prefixes below have them, are 40 there, and 15 to 70% slower in smaller
+// int8 heads, a window of 2000: 27 to 30 us).  128 rows at a time, as prefixes below have them, are 40 there, and 15 to 70% slower in smaller
 // calls: windows are short, and an item of 128 rows has too few of their units to pay for its beginning.
 template <int FMT>
 int32_t launch_window(const CacheAttnArgs& a, int rows, int most_rows, int compute_units, hipStream_t stream) {
@@ -36,13 +36,13 @@ int32_t launch_window(const CacheAttnArgs& a, int rows, int most_rows, int compu
 
 // ---- shared prefixes.  The rows of all sequences that share a prefix are rows of one item: its keys are read once for many of them.
 // Prefixes and own tokens are attended to in one launch or two, either divided like the cache of cache_attn_kernel.hip; all results are
-// partial ones, which a last launch joins.  Prefixes are bound by the products and what feeds them (of 128 rows x 8 heads x 32768 tokens
+// partial ones, which a last launch joins.  Prefixes are bound by the products and what feeds them (of 512 rows x 8 heads x 32768 tokens
 // the units take 65 us, 1.05 PFLOP/s, and 22 go to beginnings, results and the last shares' wait), own tokens by reading.
 
 // Rows of a prefix's item.  Up to 48 of them are worked on like those of a cache, 16 or 32 at a time: codes come from memory
 // into registers, and are turned to fp16 for each tile by itself.  More rows: 128 at a time, 32 of each wave, whose workgroup turns the
 // codes of 64 keys to fp16 once, in LDS, while the products of the last ones are done; the tile is that of window_attn_kernel.hip, in
-// fp16.
+// fp16.  (Its 256 registers are not enough for an item's beginning and end: 33 are spilled there, none in the loop over units.)
 constexpr int kPrefixRows = 128, kPrefixStart = 4;
 
 struct PrefixLds {
@@ -555,7 +555,8 @@ int64_t prefix_slot_rows(int32_t rows) { return rows == kPrefixRows ? int64_t(2)
 
 int32_t launch_cache_attn_shared(const CacheAttnArgs& own, const CacheAttnArgs& pre, int32_t most_rows, int32_t rows_pre, int32_t compute_units, hipStream_t stream) {
   const int grid = min(kCacheMaxWorkers / kWaves, compute_units * 2), rows = cache_attn_rows(most_rows);
-  // Small calls, by what the tables have room for, go in one launch: four sequences behind 2048 tokens x 8 heads 15 us, 23 in two launches,
+  // Small calls, by what the tables have room for, go in one launch: four sequences behind 2048 tokens x 8 heads 15 us, 23 in two launches (14 and 20
+  // later, the second with a table that has room for 131072 tokens, be it the prefix's or the sequences'),
   // 8 prefixes of 8192 tokens with four of 1500 each 70 and 71, 32 of 4096 154 and 138.
   const auto units = [](const CacheAttnArgs& a, int64_t tiles) { return a.c.n_kv_heads * tiles * (((int64_t(a.c.max_pages) << a.c.block_log2) + kUnit - 1) / kUnit); };
   const int64_t most_heads = own.t.max_tokens > 0 ? most_rows / own.t.max_tokens : 1;

@@ -5,9 +5,10 @@
 //   s_t = (q . k_t) * scale * log2(e),  m a reference near max s,  l = sum 2^(s_t - m),  out = sum 2^(s_t - m) v_t / l,  lse = (m + log2 l) ln 2,
 //
 // in one pass over the keys.  Bound by the products: 512 FLOP for every query head and visible pair, window / (1 + 1 / G) of them for
-// every byte of Q, K, V and the output.  32768 tokens x 32/8 heads with a window of 4096 take 1.87 to 1.95 ms on several cards, 1.09 to 1.13
-// PFLOP/s of visible pairs; 131072 with one of 1024 2.5 to 2.6 ms (20 key tiles an item, of which 15 are seen whole).  Short calls are
-// bound by an item's chain of tiles: 777 tokens x 32 heads, a window of 256, 12 us.
+// every byte of Q, K, V and the output.  32768 tokens x 32/8 heads with a window of 4096 take 1.87 to 2.00 ms on several cards, 1.06 to 1.13
+// PFLOP/s of visible pairs, 1.09 to 1.17 of all that is multiplied (the tile loop of attn_pipe_kernel.hip reaches 1.29 at this length); 131072 with one
+// of 1024 2.5 to 2.7 ms, 0.97 to 1.04 of all (18.9 key tiles an item, of which 5 have masks for some wave).  Short calls are bound by an item's chain of
+// tiles: 777 tokens x 32 heads, a window of 256, 12 us.
 //
 // Split.  A work item is a tile of 64 QG queries of one head; it goes through the 64-key tiles that any of its queries sees: those
 // of the first tokens, then those of the window (tile u of the item is key tile u below `sinks`, u + skip from there on).  Items cost
